@@ -629,15 +629,157 @@ oq_status oq_llama_block_forward(const oq_llama_desc* desc, const void* h0,
                                  void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * The deployed weight-activation block (Sec. 4.3: WxAy models, quantised linear
+ * inputs and quantised keys and values), in the order a block runs them:
+ *   oq_rmsnorm_quant -> oq_int8_linear (q, k, v) -> oq_kv_append ->
+ *   oq_kv_attend -> oq_act_fakequant_fwd -> oq_int8_linear (o) -> oq_rmsnorm_quant ...
+ * None of them allocates, and all can be captured into a graph.
+ *
+ * oq_rmsnorm_quant: the residual addition, RMSNorm and the per-token quantiser
+ * of oq_act_fakequant_fwd in one pass.
+ *   X [T, D] (x_dt); R [T, D] (r_dt) | NULL
+ *   H [T, D] (x_dt) | NULL = X + R rounded to x_dt (needs R; may be X or R itself)
+ *   y = (H rstd) gain + bias,  rstd = 1 / sqrt(mean(H^2) + eps), of H as stored:
+ *   the result equals the addition followed by a call without R
+ *   gain [D] fp32, bias [D] fp32 | NULL (oq_let_absorb's outputs, or the norm's own)
+ *   bits in [2, 8] (| OQ_ACT_SYM) or 16 = no quantisation (X_dq = y, no codes)
+ *   X_dq [T, D] (dq_dt) | NULL;  codes [T, D] u8 | NULL;  h, z [T] fp32 | NULL
+ * The squares are summed in fp64.  A row in which some y is not finite gets
+ * h = NaN, z = 0 and zero codes.  D a multiple of 8, at most 32768.
+ */
+oq_status oq_rmsnorm_quant(const void* X, oq_dtype x_dt, const void* R, oq_dtype r_dt, int64_t T,
+                           int64_t D, const float* gain, const float* bias, float eps, int bits,
+                           void* H, void* X_dq, oq_dtype dq_dt, uint8_t* codes, float* h, float* z,
+                           hipStream_t stream);
+
+/* oq_int8_pack: weight codes [c_out, c_in] u8 -> the operand layout of
+ * oq_int8_linear and the channels' sums.
+ *   packed : int8, R * C bytes with R = c_out rounded up to 16 and C = c_in
+ *            rounded up to 64: code - 128 (zeros in the padding) in blocks of 16
+ *            channels x 64 inputs, block (channel / 16) * (C / 64) + input / 64;
+ *            byte 256 g + 16 r + b of a block is channel 16 i + r, input
+ *            64 j + 16 g + b
+ *   wsum   : int32 [c_out] = sum over inputs of (code - 128)
+ * c_in a multiple of 16, at most 65536 (else OQ_ERR_UNSUPPORTED).
+ */
+oq_status oq_int8_pack(const uint8_t* codes, int64_t c_out, int64_t c_in, int8_t* packed,
+                       int32_t* wsum, hipStream_t stream);
+
+/* oq_int8_linear: Y[t, o] = h_x[t] h_w[o] sum_c (x[t,c] - z_x[t]) (w[o,c] - z_w[o]) + B[o],
+ * Eq. 4 with both factors as Eq. 2's codes, on 8-bit integer matrix cores.
+ *   x     : u8 [n_tok, c_in] codes of any bit width up to 8 with h_x, z_x [n_tok]
+ *           fp32 (oq_rmsnorm_quant, oq_act_fakequant_fwd)
+ *   packed, wsum : oq_int8_pack's outputs;  h_w, z_w [c_out] fp32 (one group per
+ *           channel: group = c_in)
+ *   B     : fp32 [c_out] | NULL;  Y [n_tok, c_out] in y_dt
+ * Zero points are integers held in fp32.  The integer sum is exact, the zero
+ * points enter in fp64, and then one fp32 rounding each: the sum, h_x h_w, their
+ * product, the bias.  A token's outputs do not depend on the other tokens.
+ * Shapes as oq_int8_pack; n_tok or c_out = 0 is a no-op that accepts NULL.
+ */
+oq_status oq_int8_linear(const uint8_t* x, const float* h_x, const float* z_x, int64_t n_tok,
+                         int64_t c_in, const int8_t* packed, const int32_t* wsum, const float* h_w,
+                         const float* z_w, const float* B, int64_t c_out, void* Y, oq_dtype y_dt,
+                         hipStream_t stream);
+
+/* RoPE angles for oq_kv_append: tab [n_pos, head_dim / 2, 2] fp32 = (cos, sin) of
+ * pos * base^(-2p/head_dim), evaluated in fp64 (the block step's angles). */
+oq_status oq_rope_table(int64_t n_pos, int head_dim, float base, float* tab, hipStream_t stream);
+
+/* A paged key/value cache in 8 bits.  A sequence's token t is row t % page of
+ * its page t / page.  A full page is int8 codes with one step per page, head and
+ * tensor: the symmetric 8-bit quantiser over the block's page * head_dim values,
+ * h = max(max|x| / 127, 1e-5), code = rint(x * (1/h)).  The open page and the one
+ * before it are bf16 rows in the sequence's window (page p in half p % 2).  A
+ * page is quantised once, from its bf16 rows, so its codes do not depend on how
+ * its tokens arrived; the newest tokens can be dropped, back to the start of the
+ * page before the last, by lowering `length`.  A page or window that several
+ * sequences of one append write is a race; full pages may be shared by any.
+ * Layouts (lane = 16 g + r):
+ *   K codes  [page/16][d/64][g][r][16]: token 16 a + r, channel 64 j + 16 g + b
+ *   V codes  [page/32][d/32][g][r][2][8]: channel 32 j + 16 hh + r; element e: token
+ *            32 c + 16 (e / 4) + 4 g + e % 4
+ *   K window [page][d];  V window [page/32][d/16][g][r][8]: channel 16 j + r, tokens
+ *            as in V codes
+ * head_dim 64 or 128; page a multiple of 32, at most 128. */
+typedef struct {
+  int n_pages, n_slots, page, kv_heads, head_dim;
+  int8_t* k_codes;                 /* [n_pages, kv_heads, page * head_dim]             */
+  int8_t* v_codes;
+  float* k_scale;                  /* [n_pages, kv_heads]                              */
+  float* v_scale;
+  void* k_window;                  /* bf16 [n_slots, 2, kv_heads, page * head_dim]     */
+  void* v_window;
+} oq_kv_cache;
+
+/* A ragged batch of new tokens; the arrays are int32 DEVICE memory (4-byte
+ * aligned), read when the kernels run, so a captured call follows their contents.
+ * Sequence i's new tokens are rows q_start[i] .. q_start[i+1] - 1 of the batch's
+ * tensors and take positions length[i] ...; `length` is that before the batch
+ * for oq_kv_append, oq_kv_attend and oq_kv_read alike.  A sequence whose entries
+ * do not fit (a row range outside [0, T] or longer than max_q, a length that with
+ * the new tokens passes max_pages * page, a slot outside the cache) is not cached
+ * and its outputs are NaN (rows outside every range are left as they were); a
+ * page number outside the pool reads as NaN and is not written. */
+typedef struct {
+  int n_seq, max_pages, max_q;     /* max_q: at least the largest number of new tokens */
+  int64_t tokens;                  /* T, the rows of Q, K, V and the outputs           */
+  const int32_t* table;            /* [n_seq, max_pages] page numbers                  */
+  const int32_t* slot;             /* [n_seq] window of each sequence | NULL: 0, 1, .. */
+  const int32_t* length;           /* [n_seq] tokens in the cache                      */
+  const int32_t* q_start;          /* [n_seq + 1]                                      */
+} oq_kv_batch;
+
+/* oq_kv_append: what lies between the q/k/v products and the attention, and the
+ * cache's write.  q~ = RoPE(q) / s_a, k~ = RoPE(k) * s_a (Eq. 5; the block step's
+ * order of operations), bf16; Q~ goes to Q_out, K~ and V into the cache.
+ *   Q [T, heads d], K, V [T, kv_heads d] (in_dt), rows ld_q, ld_k, ld_v elements
+ *   apart (columns of one product's output will do): 16-byte aligned, ld a
+ *   multiple of 8
+ *   rope  : [n_rope, head_dim / 2, 2] (oq_rope_table) | NULL = no rotation; a position
+ *           >= n_rope gives NaN
+ *   s_a   : [kv_heads d] fp32 | NULL;   Q_out : bf16 [T, heads d] */
+oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,
+                       const void* K, int64_t ld_k, const void* V, int64_t ld_v, oq_dtype in_dt,
+                       int heads, const float* rope, int64_t n_rope, const float* s_a, void* Q_out,
+                       hipStream_t stream);
+
+/* oq_kv_attend: causal attention of the batch's new tokens over the cache that
+ * holds them (after oq_kv_append): O = softmax(Q K^T / sqrt(d)) V per head, the
+ * token at position p seeing positions 0 .. p, query head h reading key head
+ * h / (heads / kv_heads).  Products on bf16 matrix cores (codes are exact in
+ * bf16; probabilities times the page's V step enter as bf16), sums and softmax
+ * statistics fp32.
+ *   Q bf16 [T, heads d], rows ld_q apart;  O bf16 [T, heads d];  LSE fp32 [heads, T]
+ *   | NULL: log-sum-exp of a row's logits in base 2, as oq_attention_fwd's
+ * A row that sees a key or value that is not finite, or any token of a page that
+ * holds one, is NaN; others are not touched by it.  The work of a row is split
+ * over its tokens where there are few rows, by a rule on (n_seq, heads, kv_heads,
+ * max_q, max_pages * page) alone.  Workspace: oq_kv_attend_workspace_size. */
+oq_status oq_kv_attend_workspace_size(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads,
+                                      size_t* bytes);
+oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,
+                       int heads, void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* oq_kv_read: cached rows as values.  Positions begin[i] .. length[i] + new - 1 of
+ * sequence i go to rows row_start[i] .. row_start[i+1] - 1 (int32 device arrays;
+ * rows past either end are not written) of K and V [rows, kv_heads d] (out_dt; NULL
+ * = not wanted).  max_rows: at least the largest number of rows of a sequence. */
+oq_status oq_kv_read(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* begin,
+                     const int32_t* row_start, int64_t rows, int max_rows, void* K, void* V,
+                     oq_dtype out_dt, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Kernel timing on the launching stream (HIP events around each launch).
  * Kinds: 0 forward GEMM, 1 weight-gradient GEMM, 2 input-gradient GEMM,
  * 3 LWC forward, 4 LWC backward, 5 activation quant forward, 6 activation
  * quant backward, 7 transposes, 8 other, 9 the packed linear, 10 attention
- * forward, 11 attention backward.  oq_profile_read synchronises the
+ * forward, 11 attention backward, 12 the 8-bit linear, 13 the 8-bit cache's
+ * attention.  oq_profile_read synchronises the
  * recorded events and returns launch count, total milliseconds and the
  * algorithmic work (FLOP for GEMMs, bytes for the others) of that kind.
  */
-#define OQ_PROF_KINDS 12
+#define OQ_PROF_KINDS 14
 oq_status oq_profile_enable(int on);
 oq_status oq_profile_reset(void);
 oq_status oq_profile_read(int kind, int64_t* launches, double* total_ms, double* work);

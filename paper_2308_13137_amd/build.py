@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "liboq.so")
 SOURCES = ["gemm.hip", "packed_linear_b23.hip", "packed_linear_b45.hip", "packed_linear_b67.hip",
-           "quant.hip", "misc.hip", "packed.hip", "attention.hip", "block_ops.hip", "api.hip"]
+           "quant.hip", "misc.hip", "packed.hip", "attention.hip", "block_ops.hip",
+           "norm_quant.hip", "int8_linear.hip", "kv_cache.hip", "api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -14,6 +14,7 @@
 #include "oq.h"
 #include "oq_internal.h"
 #include "packed.h"
+#include "serve.h"
 
 namespace {
 
@@ -2190,6 +2191,235 @@ oq_status oq_llama_calibrate(const oq_llama_desc* d, int n_samples, int epochs,
                                               ws_bytes, st);
       if (e != OQ_OK) return e;
     }
+  return OQ_OK;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ serving operators
+namespace {
+
+oq_status check_cache(const oq_kv_cache* c, const oq_kv_batch* b) {
+  OQ_REQ(c && b, "cache and batch are required");
+  if ((c->head_dim != 64 && c->head_dim != 128) || c->page <= 0 || c->page % 32 || c->page > 128)
+    return fail(OQ_ERR_UNSUPPORTED, "head_dim=%d (need 64 or 128), page=%d (need 32, 64, 96 or 128)",
+                c->head_dim, c->page);
+  OQ_REQ(c->n_pages > 0 && c->n_slots > 0 && c->kv_heads > 0 && c->kv_heads <= 65535,
+         "bad cache n_pages=%d n_slots=%d kv_heads=%d", c->n_pages, c->n_slots, c->kv_heads);
+  OQ_REQ(c->k_codes && c->v_codes && c->k_scale && c->v_scale && c->k_window && c->v_window,
+         "every tensor of the cache is required");
+  OQ_REQ(aligned16(c->k_codes) && aligned16(c->v_codes) && aligned16(c->k_scale) && aligned16(c->v_scale) &&
+             aligned16(c->k_window) && aligned16(c->v_window),
+         "cache pointers must be 16-byte aligned");
+  OQ_REQ(b->n_seq >= 0 && b->n_seq <= 65535 && b->max_pages > 0 && b->max_q >= 0 && b->tokens >= 0,
+         "bad batch n_seq=%d max_pages=%d max_q=%d tokens=%lld", b->n_seq, b->max_pages, b->max_q,
+         (long long)b->tokens);
+  OQ_REQ(b->tokens <= INT32_MAX && int64_t(b->max_pages) * c->page <= INT32_MAX - 65536 &&
+             b->max_q <= b->tokens,
+         "tokens=%lld, max_q=%d, max_pages * page = %lld: at most 2^31 positions, max_q at most tokens",
+         (long long)b->tokens, b->max_q, (long long)b->max_pages * c->page);
+  if (b->n_seq > 0)
+    OQ_REQ(b->table && b->length && b->q_start, "table, length and q_start are required");
+  OQ_REQ(((reinterpret_cast<uintptr_t>(b->table) | reinterpret_cast<uintptr_t>(b->slot) |
+           reinterpret_cast<uintptr_t>(b->length) | reinterpret_cast<uintptr_t>(b->q_start)) & 3u) == 0,
+         "the batch's arrays must be 4-byte aligned");
+  return OQ_OK;
+}
+
+CacheArgs cache_args(const oq_kv_cache* c, const oq_kv_batch* b) {
+  CacheArgs a;
+  a.kc = c->k_codes;
+  a.vc = c->v_codes;
+  a.ks = c->k_scale;
+  a.vs = c->v_scale;
+  a.kw = static_cast<uint16_t*>(c->k_window);
+  a.vw = static_cast<uint16_t*>(c->v_window);
+  a.n_pages = c->n_pages;
+  a.n_slots = c->n_slots;
+  a.P = c->page;
+  a.Hkv = c->kv_heads;
+  a.d = c->head_dim;
+  a.table = b->table;
+  a.slot = b->slot;
+  a.length = b->length;
+  a.q_start = b->q_start;
+  a.n_seq = b->n_seq;
+  a.max_pages = b->max_pages;
+  a.max_q = b->max_q;
+  a.T = b->tokens;
+  return a;
+}
+
+oq_status check_heads(const oq_kv_cache* c, int heads) {
+  OQ_REQ(heads > 0 && heads % c->kv_heads == 0, "heads=%d must be a multiple of kv_heads=%d", heads,
+         c->kv_heads);
+  return OQ_OK;
+}
+
+int attend_splits(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
+  if (b->n_seq == 0 || b->max_q == 0) return 1;
+  return cache_attend_splits(b->n_seq, c->kv_heads, heads, b->max_q, int64_t(b->max_pages) * c->page);
+}
+size_t attend_ws(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
+  const int s = attend_splits(c, b, heads);
+  return s > 1 ? size_t(s) * size_t(b->tokens) * size_t(heads) * size_t(c->head_dim + 2) * 4 : 0;
+}
+
+#define OQ_TRY(expr)              \
+  do {                            \
+    oq_status s_ = (expr);        \
+    if (s_ != OQ_OK) return s_;   \
+  } while (0)
+
+}  // namespace
+
+extern "C" {
+
+oq_status oq_rmsnorm_quant(const void* X, oq_dtype x_dt, const void* R, oq_dtype r_dt, int64_t T,
+                           int64_t D, const float* gain, const float* bias, float eps, int bits,
+                           void* H, void* X_dq, oq_dtype dq_dt, uint8_t* codes, float* h, float* z,
+                           hipStream_t st) {
+  const bool sym = (bits & OQ_ACT_SYM) != 0;
+  const int nb = bits & ~OQ_ACT_SYM;
+  OQ_REQ(dtype_ok(x_dt) && (!R || dtype_ok(r_dt)) && (!X_dq || dtype_ok(dq_dt)), "bad dtype");
+  OQ_REQ(T >= 0 && D > 0 && D % 8 == 0, "bad shape T=%lld D=%lld (need D %% 8 == 0)", (long long)T,
+         (long long)D);
+  if (D > NORM_MAX_D) return fail(OQ_ERR_UNSUPPORTED, "D=%lld > %lld", (long long)D, (long long)NORM_MAX_D);
+  if (nb != 16 && (nb < 2 || nb > 8)) return fail(OQ_ERR_UNSUPPORTED, "bits=%d (need 2..8 or 16)", nb);
+  OQ_REQ(!(sym && nb == 16), "OQ_ACT_SYM needs a bit width of 2..8");
+  OQ_REQ(nb != 16 || (!codes && !h && !z), "16 bits have no codes, h or z");
+  OQ_REQ(eps >= 0.0f && std::isfinite(eps), "bad eps");
+  OQ_REQ(!H || R, "H is the sum with R: it needs R");
+  if (T == 0) return OQ_OK;
+  OQ_REQ(X && gain, "X and gain are required");
+  for (const void* p : {X, R, static_cast<const void*>(gain), static_cast<const void*>(bias),
+                        static_cast<const void*>(H), static_cast<const void*>(X_dq),
+                        static_cast<const void*>(codes), static_cast<const void*>(h),
+                        static_cast<const void*>(z)})
+    OQ_REQ(aligned16(p), "pointers must be 16-byte aligned");
+  const double n = double(T) * D;
+  ProfScope ps(PK_OTHER, st,
+               n * (esize(x_dt) * (H ? 2.0 : 1.0) + (R ? esize(r_dt) : 0) + (codes ? 1 : 0) +
+                    (X_dq ? esize(dq_dt) : 0)));
+  OQ_HIP(rmsnorm_quant(X, x_dt == OQ_BF16, R, r_dt == OQ_BF16, T, D, gain, bias, eps, nb, sym, H, X_dq,
+                       dq_dt == OQ_BF16, codes, h, z, st),
+         "rmsnorm_quant");
+  return OQ_OK;
+}
+
+oq_status oq_int8_pack(const uint8_t* codes, int64_t c_out, int64_t c_in, int8_t* packed, int32_t* wsum,
+                       hipStream_t st) {
+  OQ_REQ(c_out >= 0 && c_in > 0 && c_in % 16 == 0, "bad shape c_out=%lld c_in=%lld (need c_in %% 16 == 0)",
+         (long long)c_out, (long long)c_in);
+  if (c_in > I8_MAX_C_IN || c_out > INT32_MAX - 256)
+    return fail(OQ_ERR_UNSUPPORTED, "c_in=%lld > %lld or c_out=%lld", (long long)c_in, (long long)I8_MAX_C_IN,
+                (long long)c_out);
+  if (c_out == 0) return OQ_OK;
+  OQ_REQ(codes && packed && wsum, "codes, packed and wsum are required");
+  OQ_REQ(aligned16(codes) && aligned16(packed) && aligned16(wsum), "pointers must be 16-byte aligned");
+  ProfScope ps(PK_OTHER, st, 2.0 * double(c_out) * c_in);
+  OQ_HIP(int8_pack(codes, c_out, c_in, packed, wsum, st), "int8_pack");
+  return OQ_OK;
+}
+
+oq_status oq_int8_linear(const uint8_t* x, const float* h_x, const float* z_x, int64_t n_tok, int64_t c_in,
+                         const int8_t* packed, const int32_t* wsum, const float* h_w, const float* z_w,
+                         const float* B, int64_t c_out, void* Y, oq_dtype y_dt, hipStream_t st) {
+  OQ_REQ(dtype_ok(y_dt), "bad Y dtype");
+  OQ_REQ(n_tok >= 0 && c_out >= 0 && c_in > 0 && c_in % 16 == 0,
+         "bad shape n_tok=%lld c_in=%lld c_out=%lld (need c_in %% 16 == 0)", (long long)n_tok, (long long)c_in,
+         (long long)c_out);
+  if (c_in > I8_MAX_C_IN || c_out > INT32_MAX - 256 || n_tok > (1 << 22))
+    return fail(OQ_ERR_UNSUPPORTED, "c_in=%lld > %lld, c_out=%lld or n_tok=%lld > 4194304", (long long)c_in,
+                (long long)I8_MAX_C_IN, (long long)c_out, (long long)n_tok);
+  if (n_tok == 0 || c_out == 0) return OQ_OK;
+  OQ_REQ(x && h_x && z_x && packed && wsum && h_w && z_w && Y, "every tensor but B is required");
+  OQ_REQ(aligned16(x) && aligned16(h_x) && aligned16(z_x) && aligned16(packed) && aligned16(wsum) &&
+             aligned16(h_w) && aligned16(z_w) && aligned16(B) && aligned16(Y),
+         "pointers must be 16-byte aligned");
+  ProfScope ps(PK_INT8_LINEAR, st, 2.0 * double(n_tok) * c_in * c_out);
+  const I8Args a{x, h_x, z_x, n_tok, c_in, packed, wsum, h_w, z_w, B, c_out, Y};
+  OQ_HIP(int8_linear(a, y_dt == OQ_BF16, st), "int8_linear");
+  return OQ_OK;
+}
+
+oq_status oq_rope_table(int64_t n_pos, int head_dim, float base, float* tab, hipStream_t st) {
+  OQ_REQ(n_pos >= 0 && n_pos <= (1 << 24) && head_dim > 0 && head_dim % 2 == 0 && head_dim <= 1024 &&
+             base > 0.0f && std::isfinite(base),
+         "bad n_pos=%lld, head_dim=%d or base", (long long)n_pos, head_dim);
+  if (n_pos == 0) return OQ_OK;
+  OQ_REQ(tab && aligned16(tab), "tab (16-byte aligned) is required");
+  ProfScope ps(PK_OTHER, st, 4.0 * double(n_pos) * head_dim);
+  OQ_HIP(rope_table(int(n_pos), head_dim, base, tab, st), "rope_table");
+  return OQ_OK;
+}
+
+oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,
+                       const void* K, int64_t ld_k, const void* V, int64_t ld_v, oq_dtype in_dt, int heads,
+                       const float* rope, int64_t n_rope, const float* s_a, void* Q_out, hipStream_t st) {
+  OQ_TRY(check_cache(cache, batch));
+  OQ_TRY(check_heads(cache, heads));
+  OQ_REQ(dtype_ok(in_dt), "bad input dtype");
+  const int64_t wq = int64_t(heads) * cache->head_dim, wk = int64_t(cache->kv_heads) * cache->head_dim;
+  OQ_REQ(ld_q >= wq && ld_k >= wk && ld_v >= wk && ld_q % 8 == 0 && ld_k % 8 == 0 && ld_v % 8 == 0,
+         "rows ld_q=%lld ld_k=%lld ld_v=%lld: multiples of 8, at least the widths %lld and %lld",
+         (long long)ld_q, (long long)ld_k, (long long)ld_v, (long long)wq, (long long)wk);
+  OQ_REQ(!rope || n_rope > 0, "an empty rope table");
+  if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
+  OQ_REQ(Q && K && V && Q_out, "Q, K, V and Q_out are required");
+  OQ_REQ(aligned16(Q) && aligned16(K) && aligned16(V) && aligned16(rope) && aligned16(s_a) && aligned16(Q_out),
+         "pointers must be 16-byte aligned");
+  ProfScope ps(PK_OTHER, st, double(batch->tokens) * ((wq + 2.0 * wk) * esize(in_dt) + 2.0 * wq + 2.0 * wk));
+  OQ_HIP(cache_append(cache_args(cache, batch), Q, ld_q, K, ld_k, V, ld_v, in_dt == OQ_BF16, heads, rope, n_rope,
+                      s_a, static_cast<uint16_t*>(Q_out), st),
+         "kv_append");
+  return OQ_OK;
+}
+
+oq_status oq_kv_attend_workspace_size(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads,
+                                      size_t* bytes) {
+  OQ_REQ(bytes, "bytes is required");
+  OQ_TRY(check_cache(cache, batch));
+  OQ_TRY(check_heads(cache, heads));
+  *bytes = attend_ws(cache, batch, heads);
+  return OQ_OK;
+}
+
+oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,
+                       int heads, void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t st) {
+  OQ_TRY(check_cache(cache, batch));
+  OQ_TRY(check_heads(cache, heads));
+  OQ_REQ(ld_q >= int64_t(heads) * cache->head_dim && ld_q % 8 == 0,
+         "rows ld_q=%lld: a multiple of 8, at least heads * head_dim", (long long)ld_q);
+  if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
+  OQ_REQ(Q && O, "Q and O are required");
+  OQ_REQ(aligned16(Q) && aligned16(O) && aligned16(LSE) && aligned16(ws), "pointers must be 16-byte aligned");
+  const size_t need = attend_ws(cache, batch, heads);
+  if (need && (!ws || ws_bytes < need))
+    return fail(OQ_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws ? ws_bytes : size_t(0), need);
+  ProfScope ps(PK_CACHE_ATTN, st, 4.0 * double(batch->tokens) * heads * cache->head_dim);
+  OQ_HIP(cache_attend(cache_args(cache, batch), static_cast<const uint16_t*>(Q), ld_q, heads,
+                      static_cast<uint16_t*>(O), LSE, static_cast<float*>(ws),
+                      attend_splits(cache, batch, heads), st),
+         "kv_attend");
+  return OQ_OK;
+}
+
+oq_status oq_kv_read(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* begin,
+                     const int32_t* row_start, int64_t rows, int max_rows, void* K, void* V, oq_dtype out_dt,
+                     hipStream_t st) {
+  OQ_TRY(check_cache(cache, batch));
+  OQ_REQ(dtype_ok(out_dt), "bad output dtype");
+  OQ_REQ(rows >= 0 && rows <= INT32_MAX && max_rows >= 0, "bad rows=%lld or max_rows=%d", (long long)rows,
+         max_rows);
+  if (batch->n_seq == 0 || max_rows == 0 || rows == 0 || (!K && !V)) return OQ_OK;
+  OQ_REQ(begin && row_start, "begin and row_start are required");
+  OQ_REQ(((reinterpret_cast<uintptr_t>(begin) | reinterpret_cast<uintptr_t>(row_start)) & 3u) == 0,
+         "begin and row_start must be 4-byte aligned");
+  OQ_REQ(aligned16(K) && aligned16(V), "pointers must be 16-byte aligned");
+  ProfScope ps(PK_OTHER, st, 2.0 * double(rows) * cache->kv_heads * cache->head_dim * (1 + esize(out_dt)));
+  OQ_HIP(cache_read(cache_args(cache, batch), begin, row_start, rows, max_rows, K, V, out_dt == OQ_BF16, st),
+         "kv_read");
   return OQ_OK;
 }
 

@@ -1,0 +1,193 @@
+// The residual addition, RMSNorm and per-token activation quantiser of a
+// deployed block in one pass over the row:
+//   H = X + R (rounded to X's type),  y = (H rstd) g + b,  rstd = 1/sqrt(mean H^2 + eps)
+//   h = max((max y - min y)/(2^N - 1), 1e-5), z = -rint(min y (1/h)),
+//   code = clamp(rint(y (1/h)) + z, 0, 2^N - 1)
+// (or the symmetric quantiser).  The norm is that of H as stored, so the call
+// equals the addition followed by the norm of what the addition left.  g and b
+// are the norm's gain and shift after LET is absorbed into them.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "serve.h"
+
+namespace oq {
+namespace {
+
+// One workgroup per row, the row in registers (CH chunks of 8 per thread)
+// between its three uses: the sum of squares, the range, the codes.  Squares
+// are summed in fp64: a bf16 or fp32 row of any finite values has a finite
+// mean square there.
+template <typename TX, typename TR, int NTH, int CH>
+__global__ __launch_bounds__(NTH) void norm_quant_kernel(
+    const TX* X, const TR* R, int64_t T, int64_t D,
+    const float* __restrict__ gain, const float* __restrict__ bias, float eps, int bits, bool sym,
+    TX* Hout, void* __restrict__ xdq, bool dq_bf16, uint8_t* __restrict__ codes,
+    float* __restrict__ hout, float* __restrict__ zout) {
+  constexpr int NW = NTH / 64;
+  __shared__ double s_sum[NW];
+  __shared__ float s_rng[3][NW];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int nch = int(D / 8);
+  const bool quant = bits < 16;
+  const float qmax = quant ? float((1 << bits) - 1) : 0.0f;
+  for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
+    float v[CH][8];
+    double ss = 0.0;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int j = tid + NTH * k;
+      if (j < nch) {
+        load8(X + row * D + 8 * j, v[k]);
+        if (R) {
+          float r[8];
+          load8(R + row * D + 8 * j, r);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            v[k][e] = v[k][e] + r[e];
+            if constexpr (sizeof(TX) == 2) v[k][e] = bf2f(f2bf(v[k][e]));
+          }
+          if (Hout) store8(Hout + row * D + 8 * j, v[k]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = __builtin_fma(double(v[k][e]), double(v[k][e]), ss);
+      }
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) ss += __shfl_xor(ss, off);
+    if (lane == 0) s_sum[wave] = ss;
+    __syncthreads();
+    ss = s_sum[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) ss += s_sum[w];
+    const float rs = float(1.0 / sqrt(ss / double(D) + double(eps)));
+    float mx = -INFINITY, mn = INFINITY, bad = 0.0f;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int j = tid + NTH * k;
+      if (j < nch) {
+        float g[8];
+        load8(gain + 8 * j, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] * rs * g[e];
+        if (bias) {
+          load8(bias + 8 * j, g);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] + g[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          mx = fmaxf(mx, v[k][e]);
+          mn = fminf(mn, v[k][e]);
+          bad = __builtin_fmaf(v[k][e], 0.0f, bad);       // NaN once a value is not finite
+        }
+      }
+    }
+    if (!quant) {
+      if (xdq) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+          const int j = tid + NTH * k;
+          if (j < nch) {
+            if (dq_bf16) store8(static_cast<uint16_t*>(xdq) + row * D + 8 * j, v[k]);
+            else store8(static_cast<float*>(xdq) + row * D + 8 * j, v[k]);
+          }
+        }
+      }
+      __syncthreads();
+      continue;
+    }
+    mx = wave_max(mx);
+    mn = wave_min(mn);
+    bad = wave_sum(bad);
+    if (lane == 0) {
+      s_rng[0][wave] = mx;
+      s_rng[1][wave] = mn;
+      s_rng[2][wave] = bad;
+    }
+    __syncthreads();
+    mx = s_rng[0][0];
+    mn = s_rng[1][0];
+    bad = s_rng[2][0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) {
+      mx = fmaxf(mx, s_rng[0][w]);
+      mn = fminf(mn, s_rng[1][w]);
+      bad += s_rng[2][w];
+    }
+    QParams p;
+    if (sym) {
+      int iab;
+      float sgn;
+      p = make_sym_qparams(mx, 0, mn, 0, float((1 << (bits - 1)) - 1), iab, sgn);
+    } else {
+      p = make_qparams(mx, mn, 1.0f, 1.0f, qmax);
+    }
+    // a row with a value that is not finite has no range: its step is NaN (so
+    // is everything computed from its codes), its codes are zeros
+    const bool fine = bad == 0.0f;
+    if (!fine) {
+      p.h = NAN;
+      p.z = 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int j = tid + NTH * k;
+      if (j < nch) {
+        float q[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = fine ? quant_elem(v[k][e], p, qmax).q : 0.0f;
+        if (codes) store8_codes(codes + row * D + 8 * j, q);
+        if (xdq) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) q[e] = dequant(q[e], p);
+          if (dq_bf16) store8(static_cast<uint16_t*>(xdq) + row * D + 8 * j, q);
+          else store8(static_cast<float*>(xdq) + row * D + 8 * j, q);
+        }
+      }
+    }
+    if (tid == 0) {
+      if (hout) hout[row] = p.h;
+      if (zout) zout[row] = p.z;
+    }
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+hipError_t rmsnorm_quant(const void* X, bool x_bf16, const void* R, bool r_bf16, int64_t T, int64_t D,
+                         const float* gain, const float* bias, float eps, int bits, bool sym, void* H,
+                         void* X_dq, bool dq_bf16, uint8_t* codes, float* h, float* z, hipStream_t st) {
+  if (T == 0) return hipSuccess;
+  const dim3 grid(unsigned(std::min<int64_t>(T, 1 << 20)));
+  auto go = [&](auto tx, auto tr, auto nth, auto ch) {
+    using TX = decltype(tx);
+    using TR = decltype(tr);
+    constexpr int NTH = decltype(nth)::value, CH = decltype(ch)::value;
+    hipLaunchKernelGGL((norm_quant_kernel<TX, TR, NTH, CH>), grid, dim3(NTH), 0, st,
+                       static_cast<const TX*>(X), static_cast<const TR*>(R), T, D, gain, bias, eps, bits,
+                       sym, static_cast<TX*>(H), X_dq, dq_bf16, codes, h, z);
+  };
+  auto by_d = [&](auto tx, auto tr) {
+    const int64_t nch = D / 8;
+    if (nch <= 256) go(tx, tr, std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+    else if (nch <= 512) go(tx, tr, std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
+    else if (nch <= 1024) go(tx, tr, std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+    else if (nch <= 2048) go(tx, tr, std::integral_constant<int, 512>{}, std::integral_constant<int, 4>{});
+    else go(tx, tr, std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
+  };
+  if (x_bf16) {
+    if (r_bf16) by_d(uint16_t{}, uint16_t{});
+    else by_d(uint16_t{}, float{});
+  } else {
+    if (r_bf16) by_d(float{}, uint16_t{});
+    else by_d(float{}, float{});
+  }
+  return hipGetLastError();
+}
+
+}  // namespace oq

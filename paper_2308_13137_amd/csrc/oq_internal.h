@@ -9,7 +9,7 @@ namespace oq {
 enum ProfKind {
   PK_GEMM_FWD = 0, PK_GEMM_WGRAD = 1, PK_GEMM_DGRAD = 2, PK_LWC_FWD = 3, PK_LWC_BWD = 4,
   PK_ACT_FWD = 5, PK_ACT_BWD = 6, PK_TRANSPOSE = 7, PK_OTHER = 8,
-  PK_ATTN_FWD = 10, PK_ATTN_BWD = 11
+  PK_ATTN_FWD = 10, PK_ATTN_BWD = 11, PK_INT8_LINEAR = 12, PK_CACHE_ATTN = 13
 };
 
 // Kernel timing: when enabled, brackets a launch with events on its stream.
