@@ -3,9 +3,11 @@
 // (both int8) and z' = z - 128,
 //   sum_c (q_x - z_x)(q_w - z_w) = sum a b - z_x' (sum b - K z_w') - z_w' sum a,
 // where sum a b is exact in int32, sum b comes with the packed weight and
-// sum a is formed beside the product.  The correction is fp64 (its terms are
+// sum a = sum q_x - 128 K is formed beside the product.  The correction is fp64 (its terms are
 // larger than the result), the two scales and the bias fp32.
 #include <math.h>
+
+#include <type_traits>
 
 #include "common.h"
 #include "serve.h"
@@ -19,97 +21,386 @@ constexpr uint32_t FLIP = 0x80808080u;      // code -> code - 128 as int8, four 
 OQ_DEV i32x4_t mfma_i8(i32x4_t a, i32x4_t b, i32x4_t c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
-OQ_DEV i32x4_t flip(uint4 v) {
-  return i32x4_t{int(v.x ^ FLIP), int(v.y ^ FLIP), int(v.z ^ FLIP), int(v.w ^ FLIP)};
+OQ_DEV i32x4_t flip(i32x4_t v) {
+  return i32x4_t{int(uint32_t(v[0]) ^ FLIP), int(uint32_t(v[1]) ^ FLIP), int(uint32_t(v[2]) ^ FLIP),
+                 int(uint32_t(v[3]) ^ FLIP)};
 }
-OQ_DEV int sum_bytes(i32x4_t v, int s) {
+// s + the sum of 16 codes (bytes as unsigned): v_sad_u8 against zero, one
+// instruction per four (a dot product with ones measured 10-13% of the tiled
+// kernel's time, this next to nothing).
+OQ_DEV uint32_t sum_codes(i32x4_t v, uint32_t s) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_sdot4(v[i], 0x01010101, s, false);
+  for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_sad_u8(uint32_t(v[i]), 0u, s);
   return s;
 }
 
-// Four channels n .. n + 3 of token t from their accumulators.
-template <bool YBF>
-OQ_DEV void store_out(const I8Args& a, int64_t t, int64_t n, i32x4_t acc, int sx, float hx, double zx) {
-  float y[4];
+// Channels n .. n + 3 (past the last: the last) as the epilogue needs them.
+struct Chan {
+  double zw[4], c[4];        // z_w', sum b - K z_w'
+  float hw[4], b[4];
+};
+OQ_DEV Chan load_chan(const I8Args& a, int64_t n) {
+  Chan k;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int64_t c = n + i < a.N ? n + i : a.N - 1;
-    const double zw = double(a.zw[c]) - 128.0;
-    const double s = double(acc[i]) - zx * (double(a.wsum[c]) - double(a.K) * zw) - zw * double(sx);
-    y[i] = float(s) * (hx * a.hw[c]);
-    if (a.bias) y[i] = y[i] + a.bias[c];
+    const int64_t o = min(n + i, a.N - 1);
+    k.zw[i] = double(a.zw[o]) - 128.0;
+    k.c[i] = double(a.wsum[o]) - double(a.K) * k.zw[i];
+    k.hw[i] = a.hw[o];
+    k.b[i] = a.bias ? a.bias[o] : 0.0f;
   }
+  return k;
+}
+// Channels n .. n + 3 of token t from their integer sums, sum a, h_x and z_x'.
+// (Stores of four need rows of a multiple of four.)
+template <bool YBF>
+OQ_DEV void store_out(const I8Args& a, int64_t t, int64_t n, const Chan& k, i32x4_t acc, int sx, float hx,
+                      double zx) {
+  float y[4];
+  const double s = double(sx);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const double v = __builtin_fma(-zx, k.c[i], __builtin_fma(-k.zw[i], s, double(acc[i])));
+    y[i] = float(v) * (hx * k.hw[i]);
+    if (a.bias) y[i] = y[i] + k.b[i];
+  }
+  const bool four = (a.N & 3) == 0 && n + 4 <= a.N;
   if (YBF) {
     uint16_t* p = static_cast<uint16_t*>(a.y) + t * a.N + n;
-    if ((a.N & 3) == 0 && n + 4 <= a.N) {
+    if (four) {
       *reinterpret_cast<uint2*>(p) = make_uint2(f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
     } else {
+#pragma unroll
       for (int i = 0; i < 4; ++i)
         if (n + i < a.N) p[i] = f2bf(y[i]);
     }
   } else {
     float* p = static_cast<float*>(a.y) + t * a.N + n;
-    if ((a.N & 3) == 0 && n + 4 <= a.N) {
+    if (four) {
       *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
     } else {
+#pragma unroll
       for (int i = 0; i < 4; ++i)
         if (n + i < a.N) p[i] = y[i];
     }
   }
 }
 
-// 16 channels x 16 R tokens per workgroup, the K range split over the waves.
-template <int R, bool YBF>
-__global__ __launch_bounds__(256) void i8_small_kernel(I8Args a) {
-  __shared__ i32x4_t s_acc[4][R][64];
-  __shared__ int s_sum[4][R][64];
+// ------------------------------------------------------------------ few tokens
+// 16 C channels x 16 R tokens per workgroup, the K range dealt to its eight
+// waves in one piece each: the weights stream from HBM once, each fragment one
+// 1-KiB load straight into the matrix instruction's registers, U k-steps of
+// them in flight per wave.
+constexpr int SW = 8;                     // waves per workgroup
+template <int C, int R, int U, bool YBF>
+__global__ __launch_bounds__(64 * SW) void i8_small_kernel(I8Args a) {
+  __shared__ i32x4_t s_acc[SW][C * R][64];
+  __shared__ uint32_t s_sum[SW][R][64];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r = lane & 15, g = lane >> 4;
-  const int64_t n0 = 16 * int64_t(blockIdx.x), t0 = 16 * R * int64_t(blockIdx.y);
+  const int64_t nb = i8_rows(a.N) / 16, blk = int64_t(C) * blockIdx.x, t0 = 16 * R * int64_t(blockIdx.y);
   const int kt = int(i8_cols(a.K) / 64);
-  const int per = (kt + 3) / 4;
+  const int per = (kt + SW - 1) / SW;
   const int k0 = wave * per, k1 = min(kt, k0 + per);
-  const uint4* wp = reinterpret_cast<const uint4*>(a.w) + (int64_t(blockIdx.x) * kt) * 64 + lane;
+  const i32x4_t* wp[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    wp[c] = reinterpret_cast<const i32x4_t*>(a.w) + min(blk + c, nb - 1) * kt * 64 + lane;
   const uint8_t* xp[R];
 #pragma unroll
-  for (int j = 0; j < R; ++j) xp[j] = a.x + min(t0 + 16 * j + r, a.T - 1) * a.K;
-  i32x4_t acc[R];
-  int sx[R];
+  for (int j = 0; j < R; ++j) xp[j] = a.x + min(t0 + 16 * j + r, a.T - 1) * a.K + 16 * g;
+  i32x4_t acc[C][R];
+  uint32_t sx[R];
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    acc[j] = i32x4_t{0, 0, 0, 0};
     sx[j] = 0;
-  }
-  for (int k = k0; k < k1; ++k) {
-    const uint4 w = wp[64 * k];
-    const i32x4_t wf = {int(w.x), int(w.y), int(w.z), int(w.w)};
-    const int64_t col = 64 * int64_t(k) + 16 * g;
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-      i32x4_t x = {0, 0, 0, 0};
-      if (col < a.K) x = flip(*reinterpret_cast<const uint4*>(xp[j] + col));
-      acc[j] = mfma_i8(wf, x, acc[j]);
-      sx[j] = sum_bytes(x, sx[j]);
-    }
+    for (int c = 0; c < C; ++c) acc[c][j] = i32x4_t{0, 0, 0, 0};
   }
+  // k-steps k .. k + U - 1, each one clamped into the range when TAIL
+  auto steps = [&](int k, auto tail) {
+    constexpr bool TAIL = decltype(tail)::value;
+    i32x4_t w[U][C], x[U][R];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int kk = TAIL ? min(k + i, k1 - 1) : k + i;
+#pragma unroll
+      for (int c = 0; c < C; ++c) w[i][c] = wp[c][64 * kk];
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        const bool in = !TAIL || 64 * int64_t(kk) + 16 * g < a.K;
+        x[i][j] = *reinterpret_cast<const i32x4_t*>(xp[j] + (in ? 64 * int64_t(kk) : -16 * g));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (TAIL && k + i >= k1) break;
+      const bool in = !TAIL || 64 * int64_t(k + i) + 16 * g < a.K;
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        // (columns past K: the packed weight has zeros there)
+        const i32x4_t f = flip(x[i][j]);
+        const uint32_t s = sum_codes(x[i][j], sx[j]);
+        sx[j] = in ? s : sx[j];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          acc[c][j] = mfma_i8(w[i][c], f, acc[c][j]);
+      }
+    }
+  };
+  int k = k0;
+  for (; k + U < k1; k += U) steps(k, std::false_type{});
+  if (k < k1) steps(k, std::true_type{});
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    s_acc[wave][j][lane] = acc[j];
+#pragma unroll
+    for (int c = 0; c < C; ++c) s_acc[wave][c * R + j][lane] = acc[c][j];
     s_sum[wave][j][lane] = sx[j];
   }
   __syncthreads();
-  for (int j = wave; j < R; j += 4) {
-    i32x4_t c = {0, 0, 0, 0};
-    int s = 0;
+  for (int q = wave; q < C * R; q += SW) {
+    const int c = q / R, j = q % R;
+    const int64_t t = t0 + 16 * j + r, n = 16 * (blk + c) + 4 * g;
+    if (t >= a.T || n >= a.N) continue;
+    const Chan kc = load_chan(a, n);
+    i32x4_t v = {0, 0, 0, 0};
+    uint32_t s = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      c += s_acc[w][j][lane];
+    for (int w = 0; w < SW; ++w) {
+      v += s_acc[w][q][lane];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) s += s_sum[w][j][16 * q + r];
+      for (int e = 0; e < 4; ++e) s += s_sum[w][j][16 * e + r];
     }
-    const int64_t t = t0 + 16 * j + r, n = n0 + 4 * g;
-    if (t < a.T && n < a.N) store_out<YBF>(a, t, n, c, s, a.hx[t], double(a.zx[t]) - 128.0);
+    store_out<YBF>(a, t, n, kc, v, int(s) - 128 * int(a.K), a.hx[t], double(a.zx[t]) - 128.0);
+  }
+}
+
+// ------------------------------------------------------------------ many tokens
+// 256 channels x 256 tokens per workgroup, stages of 128 inputs (two k-steps of
+// 64), eight waves of 128 x 64.  Both operands come to LDS by asynchronous
+// copies: the channels in matrix-operand order, as the weight is packed; the
+// tokens as rows of 128 bytes (a copy fetches whole cache lines), chunk c of row
+// r at slot c ^ (r & 7) ^ ((r >> 4) & 1), free of bank conflicts for the fragment
+// reads.  Tokens' tiles in three buffers, channels' in two, as the bf16 product.
+typedef __attribute__((address_space(3))) const char lds_cchar;
+constexpr int BT = 256;                   // tile side
+constexpr int TNT = 512;                  // threads
+constexpr int GROUP = 8;                  // tile rows swept together
+
+OQ_DEV void dma16_s(const void* base, uint32_t vofs, uint32_t lds_addr) {
+  const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds_addr);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(m0v), "v"(vofs), "s"(base)
+      : "memory");
+}
+OQ_DEV void wait_vm0() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+OQ_DEV void wait_vm4() { asm volatile("s_waitcnt vmcnt(4)" ::: "memory"); }
+OQ_DEV i32x4_t frag(lds_cchar* tile, int block, int kk, int lane) {
+  typedef __attribute__((address_space(3))) const i32x4_t lds_v4;
+  return *(lds_v4*)(tile + (2 * block + kk) * 1024 + 16 * lane);
+}
+OQ_DEV i32x4_t tok_frag(lds_cchar* tile, int block, int kk, int lane) {
+  typedef __attribute__((address_space(3))) const i32x4_t lds_v4;
+  const int row = 16 * block + (lane & 15), c = 4 * kk + (lane >> 4);
+  return *(lds_v4*)(tile + row * 128 + 16 * (c ^ (row & 7) ^ ((row >> 4) & 1)));
+}
+// One k-step: 8 groups of four matrix instructions; the next step's 12 fragment
+// reads in groups 0..5, one asynchronous copy in each even group when DMA, and
+// the next token fragments' conversion and sums (of lanes with `in`) in the last two.
+template <bool DMA>
+OQ_DEV void i8_step(i32x4_t (&acc)[8][4], uint32_t (&sx)[4], const i32x4_t (&au)[8], const i32x4_t (&bu)[4],
+                    lds_cchar* ra, lds_cchar* rb, int kk, int wm, int wn, int lane, i32x4_t (&ad)[8],
+                    i32x4_t (&bd)[4], const void* src, const uint32_t (&off)[4], uint32_t wr, int wave) {
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    if (g < 2) {
+      bd[2 * g] = tok_frag(rb, 4 * wn + 2 * g, kk, lane);
+      bd[2 * g + 1] = tok_frag(rb, 4 * wn + 2 * g + 1, kk, lane);
+    } else if (g < 6) {
+      ad[2 * g - 4] = frag(ra, 8 * wm + 2 * g - 4, kk, lane);
+      ad[2 * g - 3] = frag(ra, 8 * wm + 2 * g - 3, kk, lane);
+    } else {
+      // (every lane's columns are inside K here: the last stage is not read so)
+#pragma unroll
+      for (int j = 2 * g - 12; j < 2 * g - 10; ++j) {
+        sx[j] = sum_codes(bd[j], sx[j]);
+        bd[j] = flip(bd[j]);
+      }
+    }
+    if constexpr (DMA) {
+      if ((g & 1) == 0) dma16_s(src, off[g >> 1], wr + (8 * (g >> 1) + wave) * 1024);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[g][j] = mfma_i8(au[g], bu[j], acc[g][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <bool YBF>
+__global__ __launch_bounds__(TNT, 1) void i8_tile_kernel(I8Args a, int tiles_m, int tiles_n) {
+  __shared__ uint4 lds[5 * 2048];         // tokens at 0, 32, 64 KiB, channels at 96, 128 KiB
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int r = lane & 15, g4 = lane >> 4;
+  // contiguous tiles per XCD, GROUP tile rows swept column by column
+  const int nblk = gridDim.x, bid = blockIdx.x;
+  const int xcd = bid & 7, local = bid >> 3, q = nblk >> 3, rem = nblk & 7;
+  const int L = xcd * q + min(xcd, rem) + local;
+  const int group_sz = GROUP * tiles_n;
+  const int gr = L / group_sz, first_m = gr * GROUP;
+  const int gm = min(GROUP, tiles_m - first_m), li = L - gr * group_sz;
+  const int64_t n0 = int64_t(first_m + li % gm) * BT, t0 = int64_t(li / gm) * BT;
+
+  const int kt = int(i8_cols(a.K) / 64), ns = (kt + 1) / 2;
+  const int64_t nb = i8_rows(a.N) / 16;
+  const int8_t* wbase = a.w + (n0 / 16) * kt * 1024;
+  const uint8_t* xbase = a.x + t0 * a.K;
+  // copy i of this wave fills 1 KiB of either tile: operand block 4 i + wave / 2,
+  // k-step wave % 2 of the channels; rows 8 (8 i + wave) .. + 7 of the tokens, lane
+  // l the chunk of row l / 8 that belongs in slot l % 8
+  uint32_t aoff[4], boff[4];
+  const int half = wave & 1;
+  int chunk[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int b = 4 * i + (wave >> 1);
+    aoff[i] = uint32_t(min(int64_t(b), nb - 1 - n0 / 16) * kt * 1024 + half * 1024 + 16 * lane);
+    const int row = 8 * (8 * i + wave) + (lane >> 3);
+    chunk[i] = (lane & 7) ^ (row & 7) ^ ((row >> 4) & 1);
+    boff[i] = uint32_t(min(int64_t(row), a.T - 1 - t0) * a.K + 16 * chunk[i]);
+  }
+  // the last stage: a k-step or columns past the end are read from the stage's
+  // first ones instead (which the row has); the packed zeros and the sums'
+  // masks leave them out
+  auto last = [&](int st) {
+    if (st == ns - 1) {
+      if (2 * st + half >= kt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) aoff[i] -= 1024;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (128 * int64_t(st) + 16 * chunk[i] >= a.K) boff[i] -= uint32_t(16 * chunk[i]);
+    }
+  };
+  const uint32_t lds0 = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(&lds[0])));
+  lds_cchar* lbase = (lds_cchar*)(&lds[0]);
+  const int wm = wave >> 2, wn = wave & 3;
+  auto b_lds = [&](int s) { return lds0 + uint32_t(s % 3) * 32768u; };
+  auto a_lds = [&](int s) { return lds0 + 98304u + uint32_t(s & 1) * 32768u; };
+  auto b_tile = [&](int s) { return lbase + (s % 3) * 32768; };
+  auto a_tile = [&](int s) { return lbase + 98304 + (s & 1) * 32768; };
+  // (offsets of the stage are added to the bases; the last stage's are changed first)
+  auto copy_a = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dma16_s(wbase + int64_t(s) * 2048, aoff[i], a_lds(s) + (8 * i + wave) * 1024);
+  };
+  auto copy_b = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dma16_s(xbase + int64_t(s) * 128, boff[i], b_lds(s) + (8 * i + wave) * 1024);
+  };
+  // token fragments of k-step k as int8, with their sums: columns past K do not count
+  auto take_b = [&](i32x4_t (&b)[4], uint32_t (&sx)[4], int k) {
+    const bool in = 64 * int64_t(k) + 16 * g4 < a.K;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t s = sum_codes(b[j], sx[j]);
+      sx[j] = in ? s : sx[j];
+      b[j] = flip(b[j]);
+    }
+  };
+  auto read = [&](i32x4_t (&x)[8], i32x4_t (&y)[4], int st, int kk) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = frag(a_tile(st), 8 * wm + i, kk, lane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = tok_frag(b_tile(st), 4 * wn + j, kk, lane);
+  };
+  i32x4_t acc[8][4];
+  uint32_t sx[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
+  auto mul = [&](const i32x4_t (&x)[8], const i32x4_t (&y)[4]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = mfma_i8(x[i], y[j], acc[i][j]);
+  };
+
+  last(0);
+  copy_a(0);
+  copy_b(0);
+  wait_vm0();
+  __syncthreads();
+  i32x4_t a0[8], b0[4], a1[8], b1[4];
+  read(a0, b0, 0, 0);
+  take_b(b0, sx, 0);
+  if (ns > 1) {
+    last(1);
+    copy_a(1);
+    copy_b(1);
+  }
+  // iteration s: the first k-step copies the tokens of stage s + 2 (their buffer
+  // held stage s - 1), the second the channels of stage s + 2 (held stage s, whose
+  // last reads end at the middle barrier), which waits for stage s + 1 with the
+  // tokens of stage s + 2 still in flight.  The last two stages run below.
+  int s = 0;
+  for (; s + 2 < ns; ++s) {
+    last(s + 2);
+    i8_step<true>(acc, sx, a0, b0, a_tile(s), b_tile(s), 1, wm, wn, lane, a1, b1, xbase + int64_t(s + 2) * 128,
+                  boff, b_lds(s + 2), wave);
+    wait_vm4();
+    __syncthreads();
+    i8_step<true>(acc, sx, a1, b1, a_tile(s + 1), b_tile(s + 1), 0, wm, wn, lane, a0, b0,
+                  wbase + int64_t(s + 2) * 2048, aoff, a_lds(s + 2), wave);
+  }
+  for (; s < ns; ++s) {
+    if (2 * s + 1 < kt) {
+      read(a1, b1, s, 1);
+      take_b(b1, sx, 2 * s + 1);
+    }
+    mul(a0, b0);
+    if (s + 1 < ns) wait_vm0();
+    __syncthreads();
+    if (s + 1 < ns) {
+      read(a0, b0, s + 1, 0);
+      take_b(b0, sx, 2 * s + 2);
+    }
+    if (2 * s + 1 < kt) mul(a1, b1);
+  }
+  // a token's sum: its four lanes hold every k-step's quarter
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    sx[j] += __shfl_xor(sx[j], 16);
+    sx[j] += __shfl_xor(sx[j], 32);
+  }
+  float hx[4];
+  double zx[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t t = min(t0 + 64 * wn + 16 * j + r, a.T - 1);
+    hx[j] = a.hx[t];
+    zx[j] = double(a.zx[t]) - 128.0;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t n = n0 + 128 * wm + 16 * i + 4 * g4;
+    if (n < a.N) {
+      const Chan kc = load_chan(a, n);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t t = t0 + 64 * wn + 16 * j + r;
+        if (t < a.T) store_out<YBF>(a, t, n, kc, acc[i][j], int(sx[j]) - 128 * int(a.K), hx[j], zx[j]);
+      }
+    }
   }
 }
 
@@ -117,22 +408,25 @@ __global__ __launch_bounds__(256) void i8_pack_kernel(const uint8_t* __restrict_
                                                       int64_t K, int8_t* __restrict__ packed,
                                                       int32_t* __restrict__ wsum) {
   // one workgroup per block row of 16 channels; thread t: row t % 16, chunks t / 16 + 16 i
-  __shared__ int s_sum[256];
+  __shared__ uint32_t s_sum[256];
   const int r = threadIdx.x & 15, c0 = threadIdx.x >> 4;
   const int64_t n = 16 * int64_t(blockIdx.x) + r;
   const int64_t kt = (K + 63) / 64;
-  int s = 0;
+  uint32_t s = 0;
   for (int64_t c = c0; c < 4 * kt; c += 16) {
     i32x4_t v = {0, 0, 0, 0};
-    if (n < N && 16 * c < K) v = flip(*reinterpret_cast<const uint4*>(codes + n * K + 16 * c));
-    s = sum_bytes(v, s);
+    if (n < N && 16 * c < K) {
+      v = *reinterpret_cast<const i32x4_t*>(codes + n * K + 16 * c);
+      s = sum_codes(v, s);
+      v = flip(v);
+    }
     reinterpret_cast<i32x4_t*>(packed)[(int64_t(blockIdx.x) * kt + c / 4) * 64 + 16 * (c & 3) + r] = v;
   }
   s_sum[threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.x < 16 && n < N) {
     for (int q = 1; q < 16; ++q) s += s_sum[16 * q + r];
-    wsum[n] = s;
+    wsum[n] = int(s) - 128 * int(K);
   }
 }
 
@@ -147,9 +441,33 @@ hipError_t int8_pack(const uint8_t* codes, int64_t c_out, int64_t c_in, int8_t* 
 }
 
 hipError_t int8_linear(const I8Args& a, bool y_bf16, hipStream_t st) {
-  const dim3 grid(unsigned(i8_rows(a.N) / 16), unsigned((a.T + 63) / 64));
-  if (y_bf16) hipLaunchKernelGGL((i8_small_kernel<4, true>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((i8_small_kernel<4, false>), grid, dim3(256), 0, st, a);
+  const int64_t nb = i8_rows(a.N) / 16;
+  if (a.T > 256) {
+    const int tm = int((a.N + BT - 1) / BT), tn = int((a.T + BT - 1) / BT);
+    const dim3 grid(unsigned(tm) * unsigned(tn));
+    if (y_bf16) hipLaunchKernelGGL((i8_tile_kernel<true>), grid, dim3(TNT), 0, st, a, tm, tn);
+    else hipLaunchKernelGGL((i8_tile_kernel<false>), grid, dim3(TNT), 0, st, a, tm, tn);
+    return hipGetLastError();
+  }
+  auto go = [&](auto c, auto r, auto u) {
+    constexpr int Cc = decltype(c)::value, Rc = decltype(r)::value, Uc = decltype(u)::value;
+    const dim3 grid(unsigned((nb + Cc - 1) / Cc), unsigned((a.T + 16 * Rc - 1) / (16 * Rc)));
+    if (y_bf16) hipLaunchKernelGGL((i8_small_kernel<Cc, Rc, Uc, true>), grid, dim3(64 * SW), 0, st, a);
+    else hipLaunchKernelGGL((i8_small_kernel<Cc, Rc, Uc, false>), grid, dim3(64 * SW), 0, st, a);
+  };
+  auto by_c = [&](auto r, auto u1, auto u2) {
+    if (nb >= 512) go(std::integral_constant<int, 2>{}, r, u2);
+    else go(std::integral_constant<int, 1>{}, r, u1);
+  };
+  const std::integral_constant<int, 1> i1{};
+  const std::integral_constant<int, 2> i2{};
+  const std::integral_constant<int, 3> i3{};
+  const std::integral_constant<int, 4> i4{};
+  const std::integral_constant<int, 8> i8{};
+  if (a.T <= 16) by_c(i1, i8, i4);
+  else if (a.T <= 32) by_c(i2, i4, i4);
+  else if (a.T <= 48) by_c(i3, i4, i4);
+  else by_c(i4, i4, i4);
   return hipGetLastError();
 }
 
