@@ -87,92 +87,62 @@ OQ_DEV void store_out(const I8Args& a, int64_t t, int64_t n, const Chan& k, i32x
 }
 
 // ------------------------------------------------------------------ few tokens
-// 16 C channels x 16 R tokens per workgroup, the K range dealt to its eight
-// waves in one piece each: the weights stream from HBM once, each fragment one
-// 1-KiB load straight into the matrix instruction's registers, U k-steps of
-// them in flight per wave.
-constexpr int SW = 8;                     // waves per workgroup
-template <int C, int R, int U, bool YBF>
+// 16 channels x 16 tokens per workgroup, the K range dealt to its 16 waves in
+// one piece each: every weight fragment is one 1-KiB load straight into the
+// matrix instruction's registers, U k-steps of them in flight per wave (a
+// compute unit needs some 32 KiB in flight to draw its share of HBM's rate).
+constexpr int SW = 16;                    // waves per workgroup
+template <int U, bool YBF>
 __global__ __launch_bounds__(64 * SW) void i8_small_kernel(I8Args a) {
-  __shared__ i32x4_t s_acc[SW][C * R][64];
-  __shared__ uint32_t s_sum[SW][R][64];
+  __shared__ i32x4_t s_acc[SW][64];
+  __shared__ uint32_t s_sum[SW][64];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r = lane & 15, g = lane >> 4;
-  const int64_t nb = i8_rows(a.N) / 16, blk = int64_t(C) * blockIdx.x, t0 = 16 * R * int64_t(blockIdx.y);
   const int kt = int(i8_cols(a.K) / 64);
   const int per = (kt + SW - 1) / SW;
   const int k0 = wave * per, k1 = min(kt, k0 + per);
-  const i32x4_t* wp[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-    wp[c] = reinterpret_cast<const i32x4_t*>(a.w) + min(blk + c, nb - 1) * kt * 64 + lane;
-  const uint8_t* xp[R];
-#pragma unroll
-  for (int j = 0; j < R; ++j) xp[j] = a.x + min(t0 + 16 * j + r, a.T - 1) * a.K + 16 * g;
-  i32x4_t acc[C][R];
-  uint32_t sx[R];
-#pragma unroll
-  for (int j = 0; j < R; ++j) {
-    sx[j] = 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c) acc[c][j] = i32x4_t{0, 0, 0, 0};
-  }
-  // k-steps k .. k + U - 1, each one clamped into the range when TAIL
+  const i32x4_t* wp = reinterpret_cast<const i32x4_t*>(a.w) + int64_t(blockIdx.x) * kt * 64 + lane;
+  const uint8_t* xp = a.x + min(int64_t(r), a.T - 1) * a.K + 16 * g;
+  i32x4_t acc = {0, 0, 0, 0};
+  uint32_t sx = 0;
+  // k-steps k .. k + U - 1; TAIL: those past the wave's range and the columns past
+  // K (where the packed weight is zero) are read from inside and do not count
   auto steps = [&](int k, auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
-    i32x4_t w[U][C], x[U][R];
+    i32x4_t w[U], x[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int kk = TAIL ? min(k + i, k1 - 1) : k + i;
-#pragma unroll
-      for (int c = 0; c < C; ++c) w[i][c] = wp[c][64 * kk];
-#pragma unroll
-      for (int j = 0; j < R; ++j) {
-        const bool in = !TAIL || 64 * int64_t(kk) + 16 * g < a.K;
-        x[i][j] = *reinterpret_cast<const i32x4_t*>(xp[j] + (in ? 64 * int64_t(kk) : -16 * g));
-      }
+      w[i] = wp[64 * kk];
+      const bool in = !TAIL || 64 * kk + 16 * g < a.K;
+      x[i] = *reinterpret_cast<const i32x4_t*>(xp + (in ? 64 * kk : -16 * g));
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       if (TAIL && k + i >= k1) break;
-      const bool in = !TAIL || 64 * int64_t(k + i) + 16 * g < a.K;
-#pragma unroll
-      for (int j = 0; j < R; ++j) {
-        // (columns past K: the packed weight has zeros there)
-        const i32x4_t f = flip(x[i][j]);
-        const uint32_t s = sum_codes(x[i][j], sx[j]);
-        sx[j] = in ? s : sx[j];
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          acc[c][j] = mfma_i8(w[i][c], f, acc[c][j]);
-      }
+      const uint32_t s = sum_codes(x[i], sx);
+      sx = !TAIL || 64 * (k + i) + 16 * g < a.K ? s : sx;
+      acc = mfma_i8(w[i], flip(x[i]), acc);
     }
   };
   int k = k0;
   for (; k + U < k1; k += U) steps(k, std::false_type{});
   if (k < k1) steps(k, std::true_type{});
-#pragma unroll
-  for (int j = 0; j < R; ++j) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) s_acc[wave][c * R + j][lane] = acc[c][j];
-    s_sum[wave][j][lane] = sx[j];
-  }
+  s_acc[wave][lane] = acc;
+  s_sum[wave][lane] = sx;
   __syncthreads();
-  for (int q = wave; q < C * R; q += SW) {
-    const int c = q / R, j = q % R;
-    const int64_t t = t0 + 16 * j + r, n = 16 * (blk + c) + 4 * g;
-    if (t >= a.T || n >= a.N) continue;
-    const Chan kc = load_chan(a, n);
-    i32x4_t v = {0, 0, 0, 0};
-    uint32_t s = 0;
+  const int64_t n = 16 * int64_t(blockIdx.x) + 4 * g;
+  if (wave > 0 || r >= a.T || n >= a.N) return;
+  const Chan kc = load_chan(a, n);
+  acc = i32x4_t{0, 0, 0, 0};
+  sx = 0;
 #pragma unroll
-    for (int w = 0; w < SW; ++w) {
-      v += s_acc[w][q][lane];
+  for (int w = 0; w < SW; ++w) {
+    acc += s_acc[w][lane];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s += s_sum[w][j][16 * e + r];
-    }
-    store_out<YBF>(a, t, n, kc, v, int(s) - 128 * int(a.K), a.hx[t], double(a.zx[t]) - 128.0);
+    for (int e = 0; e < 4; ++e) sx += s_sum[w][16 * e + r];
   }
+  store_out<YBF>(a, r, n, kc, acc, int(sx) - 128 * int(a.K), a.hx[r], double(a.zx[r]) - 128.0);
 }
 
 // ------------------------------------------------------------------ many tokens
@@ -404,6 +374,162 @@ __global__ __launch_bounds__(TNT, 1) void i8_tile_kernel(I8Args a, int tiles_m, 
   }
 }
 
+// ------------------------------------------------------------------ a medium number of tokens
+// 16 MB channels x 16 NB tokens per workgroup, the same stages of 128 inputs in
+// a ring of S: S - 1 stages are in flight or in use while one is computed, so the
+// copies' latency is hidden also where a compute unit has one workgroup.
+template <int N>
+OQ_DEV void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+template <int MB, int NB, int WM, int WN, int KG, int S, bool YBF>
+__global__ __launch_bounds__(64 * WM * WN * KG) void i8_ring_kernel(I8Args a, int tiles_m, int tiles_n) {
+  constexpr int GW = WM * WN;                      // waves of one K group
+  constexpr int CA = 2 * MB / GW, CB = 2 * NB / GW;
+  constexpr int MT = MB / WM, NT = NB / WN;
+  constexpr int SUB = (MB + NB) * 2048, STAGE = KG * SUB;
+  static_assert(CA * GW == 2 * MB && CB * GW == 2 * NB && GW % 2 == 0, "whole copies per wave");
+  static_assert((KG - 1) * GW * 64 * (MT * NT * 16 + NT * 4) <= S * STAGE, "the groups' sums fit the ring");
+  __shared__ uint4 lds[S * STAGE / 16];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int kg = (tid >> 6) / GW, wave = (tid >> 6) % GW;
+  const int r = lane & 15, g4 = lane >> 4;
+  // contiguous tiles per XCD, token tiles fastest: a weight tile is fetched once
+  const int nblk = gridDim.x, bid = blockIdx.x;
+  const int xcd = bid & 7, local = bid >> 3, q = nblk >> 3, rem = nblk & 7;
+  const int L = xcd * q + min(xcd, rem) + local;
+  const int64_t n0 = int64_t(L / tiles_n) * (16 * MB), t0 = int64_t(L % tiles_n) * (16 * NB);
+  const int kt = int(i8_cols(a.K) / 64), ns = (kt + 2 * KG - 1) / (2 * KG);
+  const int64_t nb = i8_rows(a.N) / 16;
+  const int8_t* wbase = a.w + (n0 / 16) * kt * 1024;
+  const uint8_t* xbase = a.x + t0 * a.K;
+  uint32_t aoff[CA], boff[CB];
+  int chunk[CB];
+  const int half = wave & 1;
+#pragma unroll
+  for (int i = 0; i < CA; ++i) {
+    const int b = (GW * i + wave) >> 1;
+    aoff[i] = uint32_t(min(int64_t(b), nb - 1 - n0 / 16) * kt * 1024 + kg * 2048 + half * 1024 + 16 * lane);
+  }
+#pragma unroll
+  for (int i = 0; i < CB; ++i) {
+    const int row = 8 * (GW * i + wave) + (lane >> 3);
+    chunk[i] = (lane & 7) ^ (row & 7) ^ ((row >> 4) & 1);
+    boff[i] = uint32_t(min(int64_t(row), a.T - 1 - t0) * a.K + kg * 128 + 16 * chunk[i]);
+  }
+  const uint32_t lds0 = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(&lds[0])));
+  lds_cchar* lbase = (lds_cchar*)(&lds[0]);
+  auto copy = [&](int st) {
+    if (st == ns - 1) {
+      // past the end: the weight's last k-step and the row's first columns of the
+      // stage instead (both exist); neither is used
+      const int k = 2 * (st * KG + kg) + half;
+      if (k >= kt) {
+#pragma unroll
+        for (int i = 0; i < CA; ++i) aoff[i] -= uint32_t(k - (kt - 1)) * 1024;
+      }
+#pragma unroll
+      for (int i = 0; i < CB; ++i)
+        if (128 * int64_t(st * KG + kg) + 16 * chunk[i] >= a.K) boff[i] -= uint32_t(kg * 128 + 16 * chunk[i]);
+    }
+    const uint32_t at = lds0 + uint32_t(st % S) * STAGE + uint32_t(kg) * SUB;
+#pragma unroll
+    for (int i = 0; i < CA; ++i) dma16_s(wbase + int64_t(st) * (KG * 2048), aoff[i], at + (GW * i + wave) * 1024);
+#pragma unroll
+    for (int i = 0; i < CB; ++i)
+      dma16_s(xbase + int64_t(st) * (KG * 128), boff[i], at + MB * 2048 + (GW * i + wave) * 1024);
+  };
+  const int wm = wave / WN, wn = wave % WN;
+  i32x4_t acc[MT][NT];
+  uint32_t sx[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    sx[j] = 0;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i][j] = i32x4_t{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int st = 0; st < S - 1; ++st)
+    if (st < ns) copy(st);
+  for (int st = 0; st < ns; ++st) {
+    // stage st has landed once only the S - 2 later ones are outstanding
+    if (st + S - 2 < ns) wait_vm<(S - 2) * (CA + CB)>();
+    else wait_vm<0>();
+    __syncthreads();                       // every wave is done with stage st - 1
+    if (st + S - 1 < ns) copy(st + S - 1);
+    lds_cchar* at = lbase + (st % S) * STAGE + kg * SUB;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      const int k = 2 * (st * KG + kg) + kk;
+      if (k < kt) {
+        i32x4_t x[MT], y[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) y[j] = tok_frag(at + MB * 2048, NT * wn + j, kk, lane);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[i] = frag(at, MT * wm + i, kk, lane);
+        const bool in = 64 * int64_t(k) + 16 * g4 < a.K;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const uint32_t s = sum_codes(y[j], sx[j]);
+          sx[j] = in ? s : sx[j];
+          y[j] = flip(y[j]);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = mfma_i8(x[i], y[j], acc[i][j]);
+      }
+    }
+  }
+  if constexpr (KG > 1) {
+    // the K groups' sums, in the ring's memory
+    i32x4_t* pa = reinterpret_cast<i32x4_t*>(&lds[0]);
+    uint32_t* ps = reinterpret_cast<uint32_t*>(&lds[(KG - 1) * GW * MT * NT * 64]);
+    __syncthreads();
+    if (kg > 0) {
+      const int w = (kg - 1) * GW + wave;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        ps[(w * NT + j) * 64 + lane] = sx[j];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) pa[((w * MT + i) * NT + j) * 64 + lane] = acc[i][j];
+      }
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int k = 0; k < KG - 1; ++k) {
+      const int w = k * GW + wave;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        sx[j] += ps[(w * NT + j) * 64 + lane];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[i][j] += pa[((w * MT + i) * NT + j) * 64 + lane];
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    sx[j] += __shfl_xor(sx[j], 16);
+    sx[j] += __shfl_xor(sx[j], 32);
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t n = n0 + 16 * (MT * wm + i) + 4 * g4;
+    if (n < a.N) {
+      const Chan kc = load_chan(a, n);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int64_t t = t0 + 16 * (NT * wn + j) + r;
+        if (t < a.T)
+          store_out<YBF>(a, t, n, kc, acc[i][j], int(sx[j]) - 128 * int(a.K), a.hx[t], double(a.zx[t]) - 128.0);
+      }
+    }
+  }
+}
+
 __global__ __launch_bounds__(256) void i8_pack_kernel(const uint8_t* __restrict__ codes, int64_t N,
                                                       int64_t K, int8_t* __restrict__ packed,
                                                       int32_t* __restrict__ wsum) {
@@ -440,34 +566,52 @@ hipError_t int8_pack(const uint8_t* codes, int64_t c_out, int64_t c_in, int8_t* 
   return hipGetLastError();
 }
 
+namespace {
+
+template <int MB, int NB, int WM, int WN, int KG, int S>
+void launch_ring(const I8Args& a, bool y_bf16, hipStream_t st) {
+  const int tm = int((a.N + 16 * MB - 1) / (16 * MB)), tn = int((a.T + 16 * NB - 1) / (16 * NB));
+  const dim3 grid(unsigned(tm) * unsigned(tn)), blk(64 * WM * WN * KG);
+  if (y_bf16) hipLaunchKernelGGL((i8_ring_kernel<MB, NB, WM, WN, KG, S, true>), grid, blk, 0, st, a, tm, tn);
+  else hipLaunchKernelGGL((i8_ring_kernel<MB, NB, WM, WN, KG, S, false>), grid, blk, 0, st, a, tm, tn);
+}
+
+}  // namespace
+
 hipError_t int8_linear(const I8Args& a, bool y_bf16, hipStream_t st) {
-  const int64_t nb = i8_rows(a.N) / 16;
-  if (a.T > 256) {
+  // Kernels by tokens and channels (us, one graph of launches over weights that
+  // do not stay in the caches, inputs x channels):
+  //   up to 16 tokens and 4,096 channels, 16 channels a workgroup (all of them run
+  //   at once, with every load of a token's weights in flight): 6.9 against the
+  //   ring's 8.1 (1 token, 4,096 x 4,096), 12.7 against 15 (11,008 x 4,096); at
+  //   6,144 channels 10.1 against 8.9;
+  if (a.T <= 16 && a.N <= 4096) {
+    const dim3 grid(unsigned(i8_rows(a.N) / 16));
+    if (y_bf16) hipLaunchKernelGGL((i8_small_kernel<8, true>), grid, dim3(64 * SW), 0, st, a);
+    else hipLaunchKernelGGL((i8_small_kernel<8, false>), grid, dim3(64 * SW), 0, st, a);
+    return hipGetLastError();
+  }
+  //   else the smallest tile whose workgroups all run at once on 256 compute units
+  //   (4,096 x 4,096, 64 tokens: 32 x 32 9.0, 64 x 32 10.9, 64 x 64 14.5; 256
+  //   tokens: 28.7, 19.8, 14.7 and 128 x 64 20.6; 5,120 x 13,824, 256 tokens: 128 x
+  //   64 52, 128 x 128 36, 256 x 256 63): small tiles split K over more waves and
+  //   larger ones read the operands fewer times; two 128 x 128 workgroups fit a
+  //   compute unit with rings of two stages (8,192 x 28,672, 256 tokens: 90
+  //   against 123 by 256 x 256 tiles);
+  //   256 x 256 tiles beyond (1,024 tokens, 4,096 x 11,008: 61 against 75)
+  auto tiles = [&](int ch, int tok) { return ((a.N + ch - 1) / ch) * ((a.T + tok - 1) / tok); };
+  if (tiles(32, 32) <= 256) launch_ring<2, 2, 2, 1, 4, 4>(a, y_bf16, st);
+  else if (tiles(64, 32) <= 256) launch_ring<4, 2, 2, 2, 2, 4>(a, y_bf16, st);
+  else if (tiles(64, 64) <= 256) launch_ring<4, 4, 2, 2, 2, 4>(a, y_bf16, st);
+  else if (tiles(128, 64) <= 256) launch_ring<8, 4, 4, 2, 1, 4>(a, y_bf16, st);
+  else if (tiles(128, 128) <= 256) launch_ring<8, 8, 2, 4, 1, 4>(a, y_bf16, st);
+  else if (tiles(128, 128) <= 512) launch_ring<8, 8, 2, 4, 1, 2>(a, y_bf16, st);   // two per compute unit
+  else {
     const int tm = int((a.N + BT - 1) / BT), tn = int((a.T + BT - 1) / BT);
     const dim3 grid(unsigned(tm) * unsigned(tn));
     if (y_bf16) hipLaunchKernelGGL((i8_tile_kernel<true>), grid, dim3(TNT), 0, st, a, tm, tn);
     else hipLaunchKernelGGL((i8_tile_kernel<false>), grid, dim3(TNT), 0, st, a, tm, tn);
-    return hipGetLastError();
   }
-  auto go = [&](auto c, auto r, auto u) {
-    constexpr int Cc = decltype(c)::value, Rc = decltype(r)::value, Uc = decltype(u)::value;
-    const dim3 grid(unsigned((nb + Cc - 1) / Cc), unsigned((a.T + 16 * Rc - 1) / (16 * Rc)));
-    if (y_bf16) hipLaunchKernelGGL((i8_small_kernel<Cc, Rc, Uc, true>), grid, dim3(64 * SW), 0, st, a);
-    else hipLaunchKernelGGL((i8_small_kernel<Cc, Rc, Uc, false>), grid, dim3(64 * SW), 0, st, a);
-  };
-  auto by_c = [&](auto r, auto u1, auto u2) {
-    if (nb >= 512) go(std::integral_constant<int, 2>{}, r, u2);
-    else go(std::integral_constant<int, 1>{}, r, u1);
-  };
-  const std::integral_constant<int, 1> i1{};
-  const std::integral_constant<int, 2> i2{};
-  const std::integral_constant<int, 3> i3{};
-  const std::integral_constant<int, 4> i4{};
-  const std::integral_constant<int, 8> i8{};
-  if (a.T <= 16) by_c(i1, i8, i4);
-  else if (a.T <= 32) by_c(i2, i4, i4);
-  else if (a.T <= 48) by_c(i3, i4, i4);
-  else by_c(i4, i4, i4);
   return hipGetLastError();
 }
 

@@ -121,33 +121,44 @@ def test_linear(T, K, N, out):
     check_linear(T, K, N, out, bias=T % 2 == 1, seed=T + K + N)
 
 
+# one size for each tile of the kernels' rule, with row and channel counts that end inside a tile
+TILES = [(9, 3001), (17, 100), (31, 9002), (64, 9001), (61, 20003), (128, 20008), (131, 20002), (300, 30001)]
+
+
+@pytest.mark.parametrize("T,N", TILES)
+@pytest.mark.parametrize("K", [16, 64, 144, 208, 1040, 2064])
+def test_linear_every_tile(T, N, K):
+    """Inner sizes from less than one k-step to several ring turns, whole and ragged."""
+    check_linear(T, K, N, BF if K == 208 else F32, bias=K == 144, seed=K)
+
+
 @pytest.mark.parametrize("T", [1, 40, 300])
 @pytest.mark.parametrize("top,zspread", [(3, 0.0), (15, 5.0), (63, 1000.0), (255, 30000.0)])
 def test_linear_widths_and_far_zero_points(T, top, zspread):
     check_linear(T, 528, 144, F32, top=top, zspread=zspread, seed=top)
 
 
-@pytest.mark.parametrize("T", [1, 20, 256])
-def test_linear_extreme_codes(T):
+@pytest.mark.parametrize("T,N", [(1, 32), (20, 32), (256, 32), (20, 9000), (60, 20000), (300, 30000)])
+def test_linear_extreme_codes(T, N):
     """All codes 0 against all 255 at the largest width: the sum is the largest that can be."""
-    K, N = 65536, 32
+    K = 65536
     for a, b in ((0, 0), (255, 255), (0, 255)):
         codes = torch.full((T, K), a, dtype=torch.uint8, device="cuda")
         w = torch.full((N, K), b, dtype=torch.uint8, device="cuda")
         one, zero = torch.ones(T, device="cuda"), torch.full((T,), 128.0, device="cuda")
+        ones, zeros = torch.ones(N, device="cuda"), torch.full((N,), 128.0, device="cuda")
         packed, wsum = oq.int8_pack(w)
         assert (wsum == K * (b - 128)).all()
-        y = oq.int8_linear(codes, one, zero, packed, wsum, one[:1].expand(N).contiguous(),
-                           zero[:1].expand(N).contiguous())
+        y = oq.int8_linear(codes, one, zero, packed, wsum, ones, zeros)
         want = float(K * (a - 128) * (b - 128))
         assert (y.double() - want).abs().max() <= F24 * abs(want)
 
 
 def test_linear_rows_do_not_depend_on_the_batch():
-    codes, h, z, w, hw, zw, B = linear_case(9, 700, 528, 200)
+    codes, h, z, w, hw, zw, B = linear_case(9, 700, 528, 9000)
     packed, wsum = oq.int8_pack(w)
     full = oq.int8_linear(codes, h, z, packed, wsum, hw, zw, B=B)
-    for a, b in ((0, 1), (0, 16), (0, 37), (64, 164), (0, 300)):
+    for a, b in ((0, 1), (0, 16), (0, 30), (0, 37), (64, 164), (0, 300)):
         part = oq.int8_linear(codes[a:b].contiguous(), h[a:b].clone(), z[a:b].clone(), packed, wsum, hw, zw, B=B)
         assert torch.equal(part, full[a:b])
 
