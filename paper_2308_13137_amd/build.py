@@ -35,7 +35,8 @@ FLAGS = [
 
 # per source: the attention kernels keep their accumulators in VGPRs (the
 # matrix instructions read and write them there, no AGPR copies around each)
-EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+_VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+EXTRA = {"attention.hip": _VGPR_FORM, "kv_cache.hip": _VGPR_FORM}
 
 
 def _compile(src):

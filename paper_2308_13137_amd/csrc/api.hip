@@ -2256,12 +2256,12 @@ oq_status check_heads(const oq_kv_cache* c, int heads) {
   return OQ_OK;
 }
 
-int attend_splits(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
-  if (b->n_seq == 0 || b->max_q == 0) return 1;
-  return cache_attend_splits(b->n_seq, c->kv_heads, heads, b->max_q, int64_t(b->max_pages) * c->page);
+AttendPlan attend_plan(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
+  if (b->n_seq == 0 || b->max_q == 0) return AttendPlan{16, 0, 1, 1};
+  return cache_attend_plan(b->n_seq, c->kv_heads, heads, b->max_q, int64_t(b->max_pages) * c->page);
 }
-size_t attend_ws(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
-  const int s = attend_splits(c, b, heads);
+size_t attend_ws(const oq_kv_cache* c, const oq_kv_batch* b, const AttendPlan& p, int heads) {
+  const int s = std::max(p.few, p.many);
   return s > 1 ? size_t(s) * size_t(b->tokens) * size_t(heads) * size_t(c->head_dim + 2) * 4 : 0;
 }
 
@@ -2381,7 +2381,7 @@ oq_status oq_kv_attend_workspace_size(const oq_kv_cache* cache, const oq_kv_batc
   OQ_REQ(bytes, "bytes is required");
   OQ_TRY(check_cache(cache, batch));
   OQ_TRY(check_heads(cache, heads));
-  *bytes = attend_ws(cache, batch, heads);
+  *bytes = attend_ws(cache, batch, attend_plan(cache, batch, heads), heads);
   return OQ_OK;
 }
 
@@ -2394,13 +2394,16 @@ oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const
   if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
   OQ_REQ(Q && O, "Q and O are required");
   OQ_REQ(aligned16(Q) && aligned16(O) && aligned16(LSE) && aligned16(ws), "pointers must be 16-byte aligned");
-  const size_t need = attend_ws(cache, batch, heads);
+  const AttendPlan plan = attend_plan(cache, batch, heads);
+  const double groups = double(batch->max_q) * heads * batch->n_seq;
+  if (plan.tile_rows && groups * plan.many >= double(INT32_MAX))
+    return fail(OQ_ERR_UNSUPPORTED, "n_seq * max_q * heads = %.0f: too many rows for one call", groups);
+  const size_t need = attend_ws(cache, batch, plan, heads);
   if (need && (!ws || ws_bytes < need))
     return fail(OQ_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws ? ws_bytes : size_t(0), need);
   ProfScope ps(PK_CACHE_ATTN, st, 4.0 * double(batch->tokens) * heads * cache->head_dim);
   OQ_HIP(cache_attend(cache_args(cache, batch), static_cast<const uint16_t*>(Q), ld_q, heads,
-                      static_cast<uint16_t*>(O), LSE, static_cast<float*>(ws),
-                      attend_splits(cache, batch, heads), st),
+                      static_cast<uint16_t*>(O), LSE, static_cast<float*>(ws), plan, st),
          "kv_attend");
   return OQ_OK;
 }

@@ -256,6 +256,20 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int3
 }
 
 // ------------------------------------------------------------------ attention
+// Query x key products on bf16 operands (codes are exact in bf16), weight x
+// value products on f16 operands: codes are exact in f16 too, and a weight
+// times its page's V step, over a power of two no smaller than any step so far
+// (vref), is at most 1 and keeps 11 bits there (8 in bf16: the output's error
+// against 64 bits was 2.5e-3 with bf16 weights and is 1.7e-3, a bf16 rounding's
+// own, with f16 ones).  It enters times 2^15, so what f16 cannot hold is below
+// 2^-40 of the largest.  The window's rows are bf16, of any size: their weights
+// enter as a pair of bf16 terms, in the same unit.
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+
+OQ_DEV f32x4_t mfma_h(f16x8_t a, f16x8_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
 // int8 -> bf16, exact: eight codes of two dwords.
 OQ_DEV bf16x8_t codes_bf16(unsigned a, unsigned b) {
   u32x4_t w;
@@ -268,236 +282,608 @@ OQ_DEV bf16x8_t codes_bf16(unsigned a, unsigned b) {
   }
   return __builtin_bit_cast(bf16x8_t, w);
 }
-
-// Is one of eight bf16 values not finite?
-OQ_DEV bool not_finite(u32x4_t w) {
-  bool b = false;
+// int8 -> f16, exact: code + 128 as the low bits of 1024, then minus 1152.
+OQ_DEV f16x8_t codes_f16(unsigned a, unsigned b) {
+  u32x4_t w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) b = b || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-  return b;
+  for (int i = 0; i < 4; ++i) {
+    const unsigned v = (i < 2 ? a : b) ^ 0x80808080u;
+    const unsigned h = __builtin_amdgcn_perm(0x64646464u, v, (i & 1) ? 0x04030402u : 0x04010400u);
+    const f16x2_t f = __builtin_bit_cast(f16x2_t, h) - f16x2_t{(_Float16)1152.0f, (_Float16)1152.0f};
+    w[i] = __builtin_bit_cast(unsigned, f);
+  }
+  return __builtin_bit_cast(f16x8_t, w);
+}
+OQ_DEV unsigned pack_f16(float a, float b) {
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2_t{a, b}, f16x2_t));
 }
 
-// One workgroup: 16 R rows (query x head of the group) of one key head, chunks
-// of 32 tokens dealt to the four waves; each wave runs its own online softmax
-// in registers, the four are joined in LDS and the splits by a second kernel.
+// The smallest power of two no smaller than a positive finite x.
+OQ_DEV float pow2_above(float x) { return __uint_as_float((__float_as_uint(x) + 0x7fffffu) & 0x7f800000u); }
+OQ_DEV float pow2_inv(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
+constexpr float VREF0 = 7.62939453125e-06f;              // 2^-17, below any step
+constexpr float WUNIT = 32768.0f;                        // weights are in units of vref / WUNIT
+
+// 32 tokens of a full page as they lie in memory, with the page's steps.
+template <int DH>
+struct Codes {
+  u32x4_t k[DH / 32], v[DH / 32];
+  float ks, vs;
+  OQ_DEV void load(const CacheArgs& c, int id, int u, int tin, int lane) {
+    const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
+    ks = id < 0 ? NAN : c.ks[blk];
+    vs = id < 0 ? NAN : c.vs[blk];
+    const int64_t at = blk * c.P * DH + tin * DH;
+    const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(c.kc + at) + lane;
+    const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(c.vc + at) + lane;
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j) k[j] = kp[64 * j];
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j) v[j] = vp[64 * j];
+  }
+};
+
+// 32 tokens of the open page, one bf16 operand at a time.  Rows behind the
+// sequence's end are whatever the window holds: their values become zeros (their
+// scores are masked).  A value that is not finite would reach every row of the
+// product, those that do not see its token too: it enters as zero and its token
+// is marked in `bad` (a bit per token), as are those of keys that are not
+// finite; rows that see a marked token are made NaN.
+template <int DH>
+struct Window {
+  const uint16_t* k;
+  const u32x4_t* v;
+  int left, lane;                                        // tokens of the chunk inside the sequence
+  OQ_DEV Window(const CacheArgs& c, const Seq& s, int u, int t0, int total, int ln) : left(total - t0), lane(ln) {
+    const int pg = t0 / c.P, tin = t0 - pg * c.P;
+    const int64_t at = ((int64_t(s.slot) * 2 + (pg & 1)) * c.Hkv + u) * c.P * DH + int64_t(tin) * DH;
+    k = c.kw + at;
+    v = reinterpret_cast<const u32x4_t*>(c.vw + at) + ln;
+  }
+  OQ_DEV u32x4_t key(int a, int ks, unsigned& bad) const {
+    const int r = lane & 15, g = lane >> 4, tok = 16 * a + r;
+    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(k + tok * DH + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1));
+    bool inf = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      inf = inf || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+    if (inf && tok < left) bad |= 1u << tok;
+    return w;
+  }
+  OQ_DEV u32x4_t value(int j, unsigned& bad) const {
+    const int g = lane >> 4;
+    u32x4_t w = v[64 * j];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int tok = 16 * (e >> 2) + 4 * g + (e & 3);
+      const unsigned mask = 0xffffu << (16 * (e & 1));
+      const bool out = tok >= left, inf = ((w[e >> 1] >> (16 * (e & 1))) & 0x7f80u) == 0x7f80u;
+      if (inf && !out) bad |= 1u << tok;
+      if (out || inf) w[e >> 1] &= ~mask;
+    }
+    return w;
+  }
+};
+OQ_DEV unsigned wave_or(unsigned bad) {
+  if (__any(bad != 0))
+    for (int off = 1; off < 64; off <<= 1) bad |= __shfl_xor(bad, off);
+  return bad;
+}
+
+// A row's running softmax: the maximum m of its logits in base 2, rounded up to
+// an integer (so it seldom moves), and the sum l of its weights 2^(t - m).  A lane
+// holds NTILE 16-token tiles of one row's scores; four lanes share a row.  Returns
+// the factor that the row's numerators need.
+template <int NTILE>
+OQ_DEV float softmax_step(f32x4_t (&st)[NTILE], float& m, float& l) {
+  float mt = -INFINITY;
+#pragma unroll
+  for (int a = 0; a < NTILE; ++a)
+    mt = fmaxf(fmaxf(mt, fmaxf(st[a][0], st[a][1])), fmaxf(st[a][2], st[a][3]));
+  mt = fmaxf(mt, __shfl_xor(mt, 16));
+  mt = fmaxf(mt, __shfl_xor(mt, 32));
+  const float mn = fmaxf(m, ceilf(mt));
+  const float off = mn == -INFINITY ? 0.0f : mn;         // no token seen yet: weights 2^-inf = 0
+  float ls = 0.0f;
+#pragma unroll
+  for (int a = 0; a < NTILE; ++a)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      st[a][q] = __builtin_amdgcn_exp2f(st[a][q] - off);
+      ls += st[a][q];
+    }
+  ls += __shfl_xor(ls, 16);
+  ls += __shfl_xor(ls, 32);
+  const float alpha = mn == m ? 1.0f : m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+  l = l * alpha + ls;
+  m = mn;
+  return alpha;
+}
+
+// The query rows of one key head (query x head of the group) in matrix operands.
+template <int DH>
+OQ_DEV void load_q(bf16x8_t (&qf)[DH / 32], const uint16_t* Q, int64_t ldq, const Seq& s, int u, int G, int row,
+                   int g) {
+  const uint16_t* qp = Q + (int64_t(s.b) + row / G) * ldq + int64_t(u * G + row % G) * DH;
+#pragma unroll
+  for (int k = 0; k < DH / 32; ++k)
+    qf[k] = __builtin_bit_cast(bf16x8_t,
+                               *reinterpret_cast<const u32x4_t*>(qp + 64 * (k >> 1) + 16 * g + 8 * (k & 1)));
+}
+
+// Where a row's result goes: the output, or a split's share for cache_join_kernel
+// (numerators, then (m, l) of every row).
+struct Out {
+  uint16_t* O;
+  float *LSE, *part;
+  int splits, split, H;
+  int64_t T, ml;                     // ml: where the (m, l) pairs begin, in floats
+};
+OQ_DEV void put_ml(const Out& o, int64_t t, int64_t hd, float m, float l) {
+  if (o.splits == 1) {
+    if (o.LSE) o.LSE[hd * o.T + t] = m + log2f(l);
+  } else {
+    const int64_t at = (int64_t(o.split) * o.T + t) * o.H + hd;
+    reinterpret_cast<float2*>(o.part + o.ml)[at] = make_float2(m, l);
+  }
+}
+OQ_DEV void put4(const Out& o, int64_t t, int64_t hd, int DH, int ch, float4 x, float l) {
+  if (o.splits == 1) {
+    const float inv = 1.0f / l;
+    *reinterpret_cast<uint2*>(o.O + (t * o.H + hd) * DH + ch) =
+        make_uint2(f2bf2(x.x * inv, x.y * inv), f2bf2(x.z * inv, x.w * inv));
+  } else {
+    const int64_t at = (int64_t(o.split) * o.T + t) * o.H + hd;
+    *reinterpret_cast<float4*>(o.part + at * DH + ch) = x;
+  }
+}
+
+// Few rows (decoding): one workgroup takes 16 R rows of one key head and a split's
+// tokens, dealt to its four waves in chunks of 32.  Codes go from memory straight
+// into operand registers, the next chunk's in flight meanwhile; each wave has a
+// softmax of its own, the four are joined in LDS and the splits by a second kernel.
 //   S^T = K Q^T: a lane holds query row r, tokens 4 g + 0..3 of both 16-token
 //   tiles, which is the B operand of O^T = V^T P^T as it stands.
+// `rows_max`: sequences with more rows are the tile kernel's.
 template <int DH, int R>
-__global__ __launch_bounds__(256) void cache_attend_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
+__global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
                                                            int64_t ldq, int H, uint16_t* __restrict__ O,
                                                            float* __restrict__ LSE, float* __restrict__ part,
-                                                           int splits) {
+                                                           int splits, int parts) {
   constexpr int KS = DH / 32, JD = DH / 16;
   __shared__ float s_o[4][16 * R][DH + 4];
   __shared__ float s_ml[4][16 * R][2];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, g = lane >> 4;
-  const int split = int(blockIdx.x) % splits, rt = int(blockIdx.x) / splits, u = blockIdx.y, i = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int split = blockIdx.x, u = blockIdx.y, i = blockIdx.z;
   const int G = H / c.Hkv, P = c.P;
   const Seq s = seq_of(c, i);
-  const int rows = s.n * G, row0 = rt * 16 * R;
-  if (row0 >= rows) return;
+  const int rows = s.n * G;
+  if (rows == 0 || rows > 16 * R) return;
   const int total = s.ok ? s.L + s.n : 0;
-  const int closed = total / P * P;
   const float sc = 1.4426950408889634f / sqrtf(float(DH));
-  const int64_t win = int64_t(P) * DH;
 
   bf16x8_t qf[R][KS];
   int lim[R];                                            // the last token this lane's row sees
-#pragma unroll
-  for (int h = 0; h < R; ++h) {
-    const int row = min(row0 + 16 * h + r, rows - 1), j = row / G;
-    lim[h] = s.L + j;
-    const uint16_t* qp = Q + (int64_t(s.b) + j) * ldq + int64_t(u * G + row % G) * DH;
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-      qf[h][k] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(qp + 64 * (k >> 1) + 16 * g + 8 * (k & 1)));
-  }
   f32x4_t acc[R][JD];
-  float m[R], l[R];
+  float m[R], l[R], vref = VREF0;
 #pragma unroll
   for (int h = 0; h < R; ++h) {
+    const int row = min(16 * h + r, rows - 1);
+    lim[h] = s.L + row / G;
+    load_q<DH>(qf[h], Q, ldq, s, u, G, row, g);
     m[h] = -INFINITY;
     l[h] = 0.0f;
 #pragma unroll
     for (int j = 0; j < JD; ++j) acc[h][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  const int jmax = min(row0 + 16 * R - 1, rows - 1) / G;
-  const int seen = s.ok ? s.L + jmax + 1 : 0;            // tokens some row of the tile sees
-  const int nch = (seen + 31) / 32, per = (nch + splits - 1) / splits;
-  const int c1 = min(nch, (split + 1) * per);
-  for (int ch = split * per + wave; ch < c1; ch += 4) {
-    const int t0 = 32 * ch, pg = t0 / P, tin = t0 - pg * P;
-    bf16x8_t kf[2][KS], vf[JD];
-    float ks = 1.0f, vs = 1.0f;
-    unsigned badtok = 0;
-    if (t0 < closed) {
-      const int id = page_of(c, i, pg);
-      const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
-      ks = id < 0 ? NAN : c.ks[blk];
-      vs = id < 0 ? NAN : c.vs[blk];
-      const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(c.kc + blk * win + tin * DH) + lane;
-      const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(c.vc + blk * win + tin * DH) + lane;
+  const int nch = (total + 31) / 32, ncode = total / P * (P / 32), per = (nch + splits - 1) / splits;
+  const int c0 = split * per + wave, c1 = min(nch, (split + 1) * per), c1c = min(c1, ncode);
+  auto id_of = [&](int ch) { return ch < c1c ? page_of(c, i, 32 * ch / P) : -1; };
+  auto scores = [&](int h, const bf16x8_t (&kf)[2][KS], float f, int t0, f32x4_t (&st)[2]) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      st[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) st[a] = mfma(kf[a][k], qf[h][k], st[a]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) st[a][q] = t0 + 16 * a + 4 * g + q > lim[h] ? -INFINITY : st[a][q] * f;
+    }
+  };
+  auto rescale = [&](int h, float alpha) {
+    if (__any(alpha != 1.0f)) {
+#pragma unroll
+      for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * alpha;
+    }
+  };
+  int ch = c0;
+  if (ch < c1c) {
+    Codes<DH> nx;
+    nx.load(c, id_of(ch), u, 32 * ch % P, lane);
+    int idn = id_of(ch + 4);
+    for (; ch < c1c; ch += 4) {
+      const int t0 = 32 * ch;
+      Codes<DH> cur = nx;
+      if (ch + 4 < c1c) {
+        nx.load(c, idn, u, 32 * (ch + 4) % P, lane);
+        idn = id_of(ch + 8);
+      }
+      // a page that stands for NaN: rows that see it are NaN, its codes count for nothing
+      if (!(cur.ks < INFINITY && cur.vs < INFINITY)) {
+#pragma unroll
+        for (int h = 0; h < R; ++h)
+          if (lim[h] >= t0) l[h] = NAN;
+        cur.ks = cur.vs = 0.0f;
+      }
+      const float vr = fmaxf(vref, pow2_above(cur.vs));
+      const float vinv = pow2_inv(vr), vscale = cur.vs * vinv * WUNIT, shrink = vref * vinv;
+      bf16x8_t kf[2][KS];
 #pragma unroll
       for (int a = 0; a < 2; ++a)
 #pragma unroll
-        for (int j = 0; j < DH / 64; ++j) {
-          const u32x4_t w = kp[64 * (a * (DH / 64) + j)];
+        for (int j = 0; j < KS / 2; ++j) {
+          const u32x4_t w = cur.k[a * (KS / 2) + j];
           kf[a][2 * j] = codes_bf16(w[0], w[1]);
           kf[a][2 * j + 1] = codes_bf16(w[2], w[3]);
         }
+      f16x8_t pb[R];
 #pragma unroll
-      for (int j = 0; j < DH / 32; ++j) {
-        const u32x4_t w = vp[64 * j];
-        vf[2 * j] = codes_bf16(w[0], w[1]);
-        vf[2 * j + 1] = codes_bf16(w[2], w[3]);
+      for (int h = 0; h < R; ++h) {
+        f32x4_t st[2];
+        scores(h, kf, cur.ks * sc, t0, st);
+        rescale(h, softmax_step<2>(st, m[h], l[h]) * shrink);
+        u32x4_t w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = pack_f16(st[e >> 1][2 * (e & 1)] * vscale, st[e >> 1][2 * (e & 1) + 1] * vscale);
+        pb[h] = __builtin_bit_cast(f16x8_t, w);
       }
-    } else {
-      // the open page: rows behind the end are whatever the window holds
-      const int64_t at = ((int64_t(s.slot) * 2 + (pg & 1)) * c.Hkv + u) * win;
-      const uint16_t* kp = c.kw + at + int64_t(tin) * DH;
-      const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(c.vw + at + int64_t(tin) * DH) + lane;
+      vref = vr;
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
+      for (int j = 0; j < KS; ++j) {
+        const f16x8_t v0 = codes_f16(cur.v[j][0], cur.v[j][1]), v1 = codes_f16(cur.v[j][2], cur.v[j][3]);
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const u32x4_t w =
-              *reinterpret_cast<const u32x4_t*>(kp + (16 * a + r) * DH + 64 * (k >> 1) + 16 * g + 8 * (k & 1));
-          if (t0 + 16 * a + r < total && not_finite(w)) badtok |= 1u << (16 * a + r);
-          kf[a][k] = __builtin_bit_cast(bf16x8_t, w);
+        for (int h = 0; h < R; ++h) {
+          acc[h][2 * j] = mfma_h(v0, pb[h], acc[h][2 * j]);
+          acc[h][2 * j + 1] = mfma_h(v1, pb[h], acc[h][2 * j + 1]);
         }
-#pragma unroll
-      for (int j = 0; j < JD; ++j) {
-        u32x4_t w = vp[64 * j];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int tok = 16 * (e >> 2) + 4 * g + (e & 3);
-          const unsigned mask = 0xffffu << (16 * (e & 1));
-          const unsigned x = (w[e >> 1] >> (16 * (e & 1))) & 0x7fffu;
-          if (t0 + tok >= total) w[e >> 1] &= ~mask;
-          else if (x >= 0x7f80u) {                       // not finite: see below
-            badtok |= 1u << tok;
-            w[e >> 1] &= ~mask;
-          }
-        }
-        vf[j] = __builtin_bit_cast(bf16x8_t, w);
       }
     }
-    // a value that is not finite would reach every row of the product, those
-    // that do not see its token too: it enters as zero, and the rows that see
-    // it (or a key that is not finite) become NaN
-    if (__any(badtok != 0)) {
-      for (int off = 1; off < 64; off <<= 1) badtok |= __shfl_xor(badtok, off);
-      const int first = t0 + __ffs(int(badtok)) - 1;
+  }
+  if (ch < c1) {                                         // the open page's step is 1
+    const float vr = fmaxf(vref, 1.0f), shrink = vref * pow2_inv(vr);
 #pragma unroll
-      for (int h = 0; h < R; ++h)
-        if (lim[h] >= first) l[h] = NAN;
-    }
+    for (int h = 0; h < R; ++h)
+#pragma unroll
+      for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * shrink;
+    vref = vr;
+  }
+  for (; ch < c1; ch += 4) {
+    const int t0 = 32 * ch;
+    bf16x8_t kf[2][KS], vf[JD];
+    const Window<DH> win(c, s, u, t0, total, lane);
+    unsigned bad = 0;
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[a][k] = __builtin_bit_cast(bf16x8_t, win.key(a, k, bad));
+#pragma unroll
+    for (int j = 0; j < JD; ++j) vf[j] = __builtin_bit_cast(bf16x8_t, win.value(j, bad));
+    bad = wave_or(bad);
+    const float wunit = pow2_inv(vref) * WUNIT;
 #pragma unroll
     for (int h = 0; h < R; ++h) {
+      if (bad && lim[h] >= t0 + __ffs(int(bad)) - 1) l[h] = NAN;
       f32x4_t st[2];
-#pragma unroll
-      for (int a = 0; a < 2; ++a) {
-        st[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) st[a] = mfma(kf[a][k], qf[h][k], st[a]);
-      }
-      const float f = ks * sc;
-      float mt = -INFINITY;
-#pragma unroll
-      for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          st[a][q] = t0 + 16 * a + 4 * g + q > lim[h] ? -INFINITY : st[a][q] * f;
-          mt = fmaxf(mt, st[a][q]);
-        }
-      mt = fmaxf(mt, __shfl_xor(mt, 16));
-      mt = fmaxf(mt, __shfl_xor(mt, 32));
-      const float mn = fmaxf(m[h], ceilf(mt));
-      const float off = mn == -INFINITY ? 0.0f : mn;     // no token seen yet: weights 2^-inf = 0
-      float ls = 0.0f;
-      u32x4_t w;
+      scores(h, kf, sc, t0, st);
+      rescale(h, softmax_step<2>(st, m[h], l[h]));
+      u32x4_t wh, wl;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int a = e >> 1, q = 2 * (e & 1);
-        const float p0 = __builtin_amdgcn_exp2f(st[a][q] - off), p1 = __builtin_amdgcn_exp2f(st[a][q + 1] - off);
-        ls += p0 + p1;
-        // (a page whose step is NaN must not reach rows that see none of it)
-        w[e] = f2bf2(st[a][q] == -INFINITY ? 0.0f : p0 * vs, st[a][q + 1] == -INFINITY ? 0.0f : p1 * vs);
+        const float x = st[e >> 1][2 * (e & 1)] * wunit, y = st[e >> 1][2 * (e & 1) + 1] * wunit;
+        wh[e] = f2bf2(x, y);
+        wl[e] = f2bf2(x - __uint_as_float(wh[e] << 16), y - __uint_as_float(wh[e] & 0xffff0000u));
       }
-      const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, w);
-      ls += __shfl_xor(ls, 16);
-      ls += __shfl_xor(ls, 32);
-      if (__any(mn != m[h])) {
-        const float alpha = m[h] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[h] - mn);
-        l[h] *= alpha;
 #pragma unroll
-        for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * alpha;
+      for (int j = 0; j < JD; ++j) {
+        acc[h][j] = mfma(vf[j], __builtin_bit_cast(bf16x8_t, wh), acc[h][j]);
+        acc[h][j] = mfma(vf[j], __builtin_bit_cast(bf16x8_t, wl), acc[h][j]);
       }
-      l[h] += ls;
-      m[h] = mn;
-#pragma unroll
-      for (int j = 0; j < JD; ++j) acc[h][j] = mfma(vf[j], pb, acc[h][j]);
     }
   }
 #pragma unroll
   for (int h = 0; h < R; ++h) {
 #pragma unroll
     for (int j = 0; j < JD; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) s_o[wave][16 * h + r][16 * j + 4 * g + q] = acc[h][j][q];
+      *reinterpret_cast<f32x4_t*>(&s_o[wave][16 * h + r][16 * j + 4 * g]) = acc[h][j] * (vref / WUNIT);
     if (g == 0) {
       s_ml[wave][16 * h + r][0] = m[h];
       s_ml[wave][16 * h + r][1] = l[h];
     }
   }
   __syncthreads();
-  for (int e = tid; e < 16 * R * DH; e += 256) {
-    const int rr = e / DH, ch = e % DH, row = row0 + rr;
+  const Out out{O, LSE, part, splits, split, H, c.T, int64_t(parts) * c.T * H * DH};
+  for (int e = tid; e < 4 * R * DH; e += 256) {          // 16 R rows of DH / 4 fours
+    const int row = e / (DH / 4), c4 = 4 * (e % (DH / 4));
     if (row >= rows) break;
-    float mm = -INFINITY, ll = 0.0f, o = 0.0f;
-    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][rr][0]);
+    float mm = -INFINITY, ll = 0.0f;
+    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][row][0]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int w = 0; w < 4; ++w) {
-      const float mw = s_ml[w][rr][0];
+      const float mw = s_ml[w][row][0], lw = s_ml[w][row][1];
       const float f = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - mm);
-      ll += mw == -INFINITY ? s_ml[w][rr][1] : f * s_ml[w][rr][1];
-      o += f * s_o[w][rr][ch];
+      ll += mw == -INFINITY ? lw : f * lw;               // (no token, or NaN)
+      const float4 x = *reinterpret_cast<const float4*>(&s_o[w][row][c4]);
+      o = make_float4(o.x + f * x.x, o.y + f * x.y, o.z + f * x.z, o.w + f * x.w);
     }
     if (!s.ok) ll = NAN;
     const int64_t t = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
-    if (splits == 1) {
-      O[(t * H + hd) * DH + ch] = f2bf(o / ll);
-      if (LSE && ch == 0) LSE[hd * c.T + t] = mm + log2f(ll);
-    } else {
-      const int64_t at = (int64_t(split) * c.T + t) * H + hd;
-      part[at * DH + ch] = o;
-      if (ch == 0) {
-        float* ml = part + int64_t(splits) * c.T * H * DH + 2 * at;
-        ml[0] = mm;
-        ml[1] = ll;
-      }
-    }
+    put4(out, t, hd, DH, c4, o, ll);
+    if (c4 == 0) put_ml(out, t, hd, mm, ll);
   }
 }
 
-// Joins the splits of a row: one thread per output value.
+// Many rows (prompts): one workgroup takes 64 R rows of one key head, 16 R per wave,
+// over tiles of 64 tokens.  The waves turn a tile's codes into operands once, in
+// LDS, a tile ahead; the raw codes of the one after are in flight meanwhile.
+template <int DH, int R>
+__global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
+                                                                int64_t ldq, int H, uint16_t* __restrict__ O,
+                                                                float* __restrict__ LSE,
+                                                                float* __restrict__ part, int splits, int parts,
+                                                                int rows_min) {
+  constexpr int KS = DH / 32, JD = DH / 16, QW = 64 * R;
+  constexpr int TILE = 64 * DH / 8;                      // 16-byte pieces of one operand's tile
+  __shared__ u32x4_t s_k[2][TILE], s_v[2][TILE];
+  __shared__ float s_step[2][2][2];                      // [buffer][chunk](key step x scale, value step)
+  __shared__ unsigned s_bad[2][2][2];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // key heads fastest (an XCD keeps its heads' pages in its L2), longest rows first
+  const int G = H / c.Hkv, P = c.P;
+  const int ntile = (c.max_q * G + QW - 1) / QW;
+  int x = int(blockIdx.x);
+  const int u = x % c.Hkv;
+  x /= c.Hkv;
+  const int split = x % splits;
+  x /= splits;
+  const int i = x % c.n_seq, rt = ntile - 1 - x / c.n_seq;
+  const Seq s = seq_of(c, i);
+  const int rows = s.n * G, row0 = rt * QW;
+  if (rows < rows_min || row0 >= rows) return;
+  const int total = s.ok ? s.L + s.n : 0, closed = total / P * P;
+  const float sc = 1.4426950408889634f / sqrtf(float(DH));
+
+  bf16x8_t qf[R][KS];
+  int lim[R];
+  f32x4_t acc[R][JD];
+  float m[R], l[R], vref = VREF0;
+#pragma unroll
+  for (int h = 0; h < R; ++h) {
+    const int row = min(row0 + 16 * (R * wave + h) + r, rows - 1);
+    lim[h] = s.L + row / G;
+    load_q<DH>(qf[h], Q, ldq, s, u, G, row, g);
+    m[h] = -INFINITY;
+    l[h] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < JD; ++j) acc[h][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const int first_lim = s.L + row0 / G;                  // what every row of the tile sees
+  const int seen = s.ok ? s.L + min(row0 + QW - 1, rows - 1) / G + 1 : 0;
+  const int nt = (seen + 63) / 64, per = (nt + splits - 1) / splits;
+  const int k0 = split * per, k1 = min(nt, (split + 1) * per);
+  const int ntc = closed / 64;                           // tiles of full pages only
+  // this wave's share of a tile: half (wave % 2) of chunk wave / 2 of the keys and
+  // of the values, DH / 64 loads each
+  constexpr int NL = DH / 64;
+  const int cc = wave >> 1, hw = wave & 1;
+  u32x4_t rk[NL], rv[NL];
+  float ks = 0.0f, vs = 0.0f;
+  auto load = [&](int t) {                               // tile t, if its chunk is in a full page
+    const int t0 = 64 * t + 32 * cc;
+    if (t0 < closed) {
+      const int pg = t0 / P, id = page_of(c, i, pg);
+      const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
+      ks = id < 0 ? NAN : c.ks[blk];
+      vs = id < 0 ? NAN : c.vs[blk];
+      const int64_t at = blk * P * DH + (t0 - pg * P) * DH;
+      const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(c.kc + at) + 64 * NL * hw + lane;
+      const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(c.vc + at) + 64 * NL * hw + lane;
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        rk[j] = kp[64 * j];
+        rv[j] = vp[64 * j];
+      }
+    }
+  };
+  // operands of tile t into buffer b: fragment f of 64 lanes at 64 f, chunk cc's
+  // keys at tile a = 2 cc + hw, its values at 2 JD/2 fragments per half
+  auto store = [&](int t, int b) {
+    const int t0 = 64 * t + 32 * cc;
+    if (t0 < closed) {
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        u32x4_t* kd = &s_k[b][((2 * cc + hw) * KS + 2 * j) * 64 + lane];
+        kd[0] = __builtin_bit_cast(u32x4_t, codes_bf16(rk[j][0], rk[j][1]));
+        kd[64] = __builtin_bit_cast(u32x4_t, codes_bf16(rk[j][2], rk[j][3]));
+        u32x4_t* vd = &s_v[b][(cc * JD + 2 * (NL * hw + j)) * 64 + lane];
+        if (t < ntc) {
+          vd[0] = __builtin_bit_cast(u32x4_t, codes_f16(rv[j][0], rv[j][1]));
+          vd[64] = __builtin_bit_cast(u32x4_t, codes_f16(rv[j][2], rv[j][3]));
+        } else {
+          vd[0] = __builtin_bit_cast(u32x4_t, codes_bf16(rv[j][0], rv[j][1]));
+          vd[64] = __builtin_bit_cast(u32x4_t, codes_bf16(rv[j][2], rv[j][3]));
+        }
+      }
+      if (hw == 0 && lane == 0) {
+        const bool fine = ks < INFINITY && vs < INFINITY;
+        s_step[b][cc][0] = fine ? ks * sc : 0.0f;
+        s_step[b][cc][1] = fine ? vs : 0.0f;
+        s_bad[b][cc][0] = fine ? 0u : 1u;
+        s_bad[b][cc][1] = 0u;
+      }
+    } else {
+      // the open page: one of the chunk's waves takes its keys, one its values (past
+      // every row's limit zeros, any finite operands); one operand at a time, which
+      // keeps the registers of the loop for its products
+      unsigned bad = 0;
+      const Window<DH> win(c, s, u, min(t0, max(seen - 1, 0) / 32 * 32), total, lane);
+      const bool in = t0 < seen;
+      u32x4_t* dst = hw ? &s_v[b][cc * JD * 64 + lane] : &s_k[b][2 * cc * KS * 64 + lane];
+#pragma unroll 1
+      for (int f = 0; f < JD; ++f) {
+        u32x4_t w = {0u, 0u, 0u, 0u};
+        if (in) w = hw ? win.value(f, bad) : win.key(f / KS, f % KS, bad);
+        dst[64 * f] = w;
+      }
+      bad = wave_or(bad);
+      if (lane == 0) {
+        s_step[b][cc][hw] = hw ? 1.0f : in ? sc : 0.0f;
+        s_bad[b][cc][hw] = bad;
+      }
+    }
+  };
+  if (k0 < k1) {
+    load(k0);
+    store(k0, 0);
+    if (k0 + 1 < k1) load(k0 + 1);
+  }
+  // One tile.  TAIL: it reaches into the open page; values are bf16 operands and
+  // the weights pairs of bf16 terms, else f16 and one f16 term.  (Two loops: with
+  // both forms in one the registers of 128 rows x 128 channels do not suffice.)
+  auto tile = [&](int t, auto is_tail) {
+    constexpr bool TAIL = decltype(is_tail)::value;
+    const int b = (t - k0) & 1, t0 = 64 * t;
+    __syncthreads();                                     // tile t is in buffer b, the other is free
+    if (t + 1 < k1) {
+      store(t + 1, b ^ 1);
+      if (t + 2 < k1) load(t + 2);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4_t st[R][4];
+    const float f0 = s_step[b][0][0], f1 = s_step[b][1][0];
+    const unsigned bad0 = s_bad[b][0][0] | s_bad[b][0][1], bad1 = s_bad[b][1][0] | s_bad[b][1][1];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+#pragma unroll
+      for (int h = 0; h < R; ++h) st[h][a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, s_k[b][(a * KS + k) * 64 + lane]);
+#pragma unroll
+        for (int h = 0; h < R; ++h) st[h][a] = mfma(kf, qf[h][k], st[h][a]);
+      }
+#pragma unroll
+      for (int h = 0; h < R; ++h) st[h][a] = st[h][a] * (a < 2 ? f0 : f1);
+    }
+    if (t0 + 63 > first_lim) {
+#pragma unroll
+      for (int h = 0; h < R; ++h)
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (t0 + 16 * a + 4 * g + q > lim[h]) st[h][a][q] = -INFINITY;
+    }
+    if (bad0 | bad1) {
+      // (a full page that stands for NaN: from its chunk's first token on)
+#pragma unroll
+      for (int h = 0; h < R; ++h) {
+        if (bad0 && lim[h] >= t0 + __ffs(int(bad0)) - 1) l[h] = NAN;
+        if (bad1 && lim[h] >= t0 + 32 + __ffs(int(bad1)) - 1) l[h] = NAN;
+      }
+    }
+    const float vs0 = s_step[b][0][1], vs1 = s_step[b][1][1];
+    const float vr = fmaxf(vref, fmaxf(pow2_above(vs0), pow2_above(vs1)));
+    const float vinv = pow2_inv(vr), shrink = vref * vinv;
+    vref = vr;
+#pragma unroll
+    for (int h = 0; h < R; ++h) {
+      const float alpha = softmax_step<4>(st[h], m[h], l[h]) * shrink;
+      if (__any(alpha != 1.0f)) {
+#pragma unroll
+        for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * alpha;
+      }
+    }
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      const float vsc = (k2 ? vs1 : vs0) * vinv * WUNIT;
+      u32x4_t ph[R], pl[TAIL ? R : 1];
+#pragma unroll
+      for (int h = 0; h < R; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4_t p = st[h][2 * k2 + (e >> 1)];
+          const float p0 = p[2 * (e & 1)] * vsc, p1 = p[2 * (e & 1) + 1] * vsc;
+          if constexpr (TAIL) {
+            ph[h][e] = f2bf2(p0, p1);
+            pl[h][e] = f2bf2(p0 - __uint_as_float(ph[h][e] << 16), p1 - __uint_as_float(ph[h][e] & 0xffff0000u));
+          } else {
+            ph[h][e] = pack_f16(p0, p1);
+          }
+        }
+#pragma unroll
+      for (int j = 0; j < JD; ++j) {
+        const u32x4_t vf = s_v[b][(k2 * JD + j) * 64 + lane];
+#pragma unroll
+        for (int h = 0; h < R; ++h) {
+          if constexpr (TAIL) {
+            acc[h][j] = mfma(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, ph[h]), acc[h][j]);
+            acc[h][j] = mfma(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pl[h]), acc[h][j]);
+          } else {
+            acc[h][j] = mfma_h(__builtin_bit_cast(f16x8_t, vf), __builtin_bit_cast(f16x8_t, ph[h]), acc[h][j]);
+          }
+        }
+      }
+    }
+  };
+  int t = k0;
+  for (; t < min(k1, ntc); ++t) tile(t, std::false_type{});
+  for (; t < k1; ++t) tile(t, std::true_type{});
+  const Out out{O, LSE, part, splits, split, H, c.T, int64_t(parts) * c.T * H * DH};
+#pragma unroll
+  for (int h = 0; h < R; ++h) {
+    const int row = row0 + 16 * (R * wave + h) + r;
+    if (row >= rows) continue;
+    const float ll = s.ok ? l[h] : NAN;
+    const int64_t t = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
+#pragma unroll
+    for (int j = 0; j < JD; ++j) {
+      const f32x4_t o = acc[h][j] * (vref / WUNIT);
+      put4(out, t, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), ll);
+    }
+    if (g == 0) put_ml(out, t, hd, m[h], ll);
+  }
+}
+
+// Joins a row's splits: one thread per four output values.  Sequences of up to
+// `rows_few` rows have `few` splits, the others `many`.
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, int DH,
-                                                         const float* __restrict__ part, int splits,
-                                                         uint16_t* __restrict__ O, float* __restrict__ LSE) {
+                                                         const float* __restrict__ part, int parts, int few,
+                                                         int many, int rows_few, uint16_t* __restrict__ O,
+                                                         float* __restrict__ LSE) {
   const Seq s = seq_of(c, blockIdx.y);
   const int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (e >= int64_t(s.n) * H * DH) return;
-  const int64_t at = int64_t(s.b) * H + e / DH;
-  const int ch = int(e % DH);
-  const float* ml = part + int64_t(splits) * c.T * H * DH;
-  float mm = -INFINITY, ll = 0.0f, o = 0.0f;
-  for (int k = 0; k < splits; ++k) mm = fmaxf(mm, ml[2 * (k * c.T * H + at)]);
+  const int q4 = DH / 4;
+  if (e >= int64_t(s.n) * H * q4) return;
+  const int splits = s.n * (H / c.Hkv) <= rows_few ? few : many;
+  if (splits == 1) return;
+  const int64_t at = int64_t(s.b) * H + e / q4;
+  const int ch = 4 * int(e % q4);
+  const float2* ml = reinterpret_cast<const float2*>(part + int64_t(parts) * c.T * H * DH);
+  float mm = -INFINITY, ll = 0.0f;
+  for (int k = 0; k < splits; ++k) mm = fmaxf(mm, ml[k * c.T * H + at].x);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int k = 0; k < splits; ++k) {
-    const float mk = ml[2 * (k * c.T * H + at)], lk = ml[2 * (k * c.T * H + at) + 1];
-    const float f = mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - mm);
-    ll += mk == -INFINITY ? lk : f * lk;
-    if (mk != -INFINITY) o += f * part[(k * c.T * H + at) * DH + ch];
+    const float2 w = ml[k * c.T * H + at];
+    const bool none = w.x == -INFINITY;                  // no token in this split (or NaN)
+    const float f = none ? 0.0f : __builtin_amdgcn_exp2f(w.x - mm);
+    ll += none ? w.y : f * w.y;
+    const float4 x = *reinterpret_cast<const float4*>(part + (k * c.T * H + at) * DH + ch);
+    o = make_float4(o.x + f * x.x, o.y + f * x.y, o.z + f * x.z, o.w + f * x.w);
   }
-  O[at * DH + ch] = f2bf(o / ll);
+  const float inv = 1.0f / ll;
+  *reinterpret_cast<uint2*>(O + at * DH + ch) = make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
   if (LSE && ch == 0) LSE[(at % H) * c.T + at / H] = mm + log2f(ll);
 }
 
@@ -532,27 +918,50 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
   return hipGetLastError();
 }
 
-int cache_attend_splits(int n_seq, int Hkv, int H, int max_q, int64_t max_len) {
-  const int64_t tiles = (int64_t(max_q) * (H / Hkv) + 15) / 16;
-  const int64_t wgs = tiles * Hkv * n_seq, chunks = (max_len + 31) / 32;
-  const int64_t want = (1024 + wgs - 1) / wgs;
-  return int(std::max<int64_t>(1, std::min<int64_t>({want, chunks / 8, 64})));
+// How a call is cut up, from its sizes alone.  Rows of a key head: up to 32 go to
+// the row kernel, more to the tile kernel; a batch of prompts and decoding
+// sequences runs both, each on its own.
+AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int max_q, int64_t max_len) {
+  const int64_t rows = int64_t(max_q) * (H / Hkv), heads = int64_t(n_seq) * Hkv;
+  AttendPlan p;
+  p.tile_rows = rows <= 32 ? 0 : rows <= 64 ? 64 : 128;
+  p.row_rows = rows <= 16 ? 16 : rows <= 32 || n_seq > 1 ? 32 : 0;
+  auto cut = [](int64_t want, int64_t most) { return int(std::max<int64_t>(1, std::min(want, most))); };
+  p.few = p.row_rows ? cut((1024 + heads - 1) / heads, std::min<int64_t>(128, max_len / 256)) : 1;
+  const int64_t tiles = p.tile_rows ? (rows + p.tile_rows - 1) / p.tile_rows * heads : 0;
+  p.many = p.tile_rows ? cut(512 / std::max<int64_t>(1, tiles), std::min<int64_t>(64, max_len / 512)) : 1;
+  return p;
 }
 
 hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int H, uint16_t* O, float* LSE,
-                        float* ws, int splits, hipStream_t st) {
-  const int64_t rows = int64_t(c.max_q) * (H / c.Hkv);
-  auto go = [&](auto dh, auto rr) {
+                        float* ws, const AttendPlan& p, hipStream_t st) {
+  const int parts = std::max(p.few, p.many), G = H / c.Hkv;
+  auto few = [&](auto dh, auto rr) {
     constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
-    const dim3 grid(unsigned((rows + 16 * R - 1) / (16 * R) * splits), unsigned(c.Hkv), unsigned(c.n_seq));
-    hipLaunchKernelGGL((cache_attend_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, splits);
+    const dim3 grid(unsigned(p.few), unsigned(c.Hkv), unsigned(c.n_seq));
+    hipLaunchKernelGGL((cache_attend_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, p.few,
+                       parts);
   };
-  if (c.d == 64) go(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-  else go(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
+  auto many = [&](auto dh, auto rr) {
+    constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
+    const int64_t tiles = (int64_t(c.max_q) * G + 64 * R - 1) / (64 * R);
+    const dim3 grid(unsigned(tiles * c.n_seq * p.many * c.Hkv));
+    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws,
+                       p.many, parts, p.row_rows + 1);
+  };
+  auto by_rows = [&](auto dh) {
+    if (p.tile_rows == 64) many(dh, std::integral_constant<int, 1>{});
+    else if (p.tile_rows) many(dh, std::integral_constant<int, 2>{});
+    if (p.row_rows == 16) few(dh, std::integral_constant<int, 1>{});
+    else if (p.row_rows) few(dh, std::integral_constant<int, 2>{});
+  };
+  if (c.d == 64) by_rows(std::integral_constant<int, 64>{});
+  else by_rows(std::integral_constant<int, 128>{});
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || splits == 1) return e;
-  const dim3 grid(unsigned((int64_t(c.max_q) * H * c.d + 255) / 256), unsigned(c.n_seq));
-  hipLaunchKernelGGL(cache_join_kernel, grid, dim3(256), 0, st, c, H, c.d, ws, splits, O, LSE);
+  if (e != hipSuccess || parts == 1) return e;
+  const dim3 grid(unsigned((int64_t(c.max_q) * H * (c.d / 4) + 255) / 256), unsigned(c.n_seq));
+  hipLaunchKernelGGL(cache_join_kernel, grid, dim3(256), 0, st, c, H, c.d, ws, parts, p.few, p.many, p.row_rows,
+                     O, LSE);
   return hipGetLastError();
 }
 

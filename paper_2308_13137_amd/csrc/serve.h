@@ -56,8 +56,14 @@ hipError_t cache_append(const CacheArgs& c, const void* Q, int64_t ldq, const vo
                         const float* s_a, uint16_t* Qout, hipStream_t st);
 hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* row_start, int64_t rows,
                       int max_rows, void* K, void* V, bool bf16, hipStream_t st);
-int cache_attend_splits(int n_seq, int Hkv, int H, int max_q, int64_t max_len);
+struct AttendPlan {
+  int row_rows;    // rows of a workgroup of the row kernel (16, 32; 0: not used)
+  int tile_rows;   // rows of a workgroup of the tile kernel (64, 128; 0: not used)
+  int few, many;   // splits of a row's tokens in the two
+};
+AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int max_q, int64_t max_len);
+// ws: max(few, many) * T * H * (d + 2) fp32 where that is more than one split
 hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int H, uint16_t* O, float* LSE,
-                        float* ws, int splits, hipStream_t st);
+                        float* ws, const AttendPlan& p, hipStream_t st);
 
 }  // namespace oq

@@ -86,6 +86,12 @@ def attend64(q, k, v, before):
         # weights rounded to bf16 (half a step), sums of their products in fp32; a row's two sums
         # (numerator, denominator) both carry the scores' error; then one bf16 rounding
         av = p @ vv.abs()
-        tol[:, h] = av * (BF8 + 2 * es + 2 * len(kk) * F24) * 1.01 + out[:, h].abs() * BF8 * 1.01 + 1e-30
+        # what a 16-bit weight cannot hold: weights of full pages enter as f16 of at most 2^15 (the
+        # largest is over 2^13: a row's maximum is rounded up to an integer, a step to a power of two),
+        # so half a subnormal step, 2^-25, is at most 2^-38 of the largest weight times step; times a
+        # code of at most 127, and 127 steps are a page's largest value
+        small = len(kk) * 2.0 ** -38 * vv.abs().max()
+        tol[:, h] = (av * (BF8 + 2 * es + 2 * len(kk) * F24) * 1.01 + out[:, h].abs() * BF8 * 1.01 + small
+                     + 1e-30)
         lse[h] = torch.logsumexp(s, 1) * 1.4426950408889634
     return out, tol, lse
