@@ -2257,12 +2257,9 @@ oq_status check_heads(const oq_kv_cache* c, int heads) {
 }
 
 AttendPlan attend_plan(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
-  if (b->n_seq == 0 || b->max_q == 0) return AttendPlan{16, 0, 1, 1};
-  return cache_attend_plan(b->n_seq, c->kv_heads, heads, b->max_q, int64_t(b->max_pages) * c->page);
-}
-size_t attend_ws(const oq_kv_cache* c, const oq_kv_batch* b, const AttendPlan& p, int heads) {
-  const int s = std::max(p.few, p.many);
-  return s > 1 ? size_t(s) * size_t(b->tokens) * size_t(heads) * size_t(c->head_dim + 2) * 4 : 0;
+  if (b->n_seq == 0 || b->max_q == 0) return AttendPlan{16, 0, 1, 1, 0, 0};
+  return cache_attend_plan(b->n_seq, c->kv_heads, heads, b->tokens, b->max_q, int64_t(b->max_pages) * c->page,
+                           c->head_dim);
 }
 
 #define OQ_TRY(expr)              \
@@ -2381,7 +2378,8 @@ oq_status oq_kv_attend_workspace_size(const oq_kv_cache* cache, const oq_kv_batc
   OQ_REQ(bytes, "bytes is required");
   OQ_TRY(check_cache(cache, batch));
   OQ_TRY(check_heads(cache, heads));
-  *bytes = attend_ws(cache, batch, attend_plan(cache, batch, heads), heads);
+  const AttendPlan p = attend_plan(cache, batch, heads);
+  *bytes = (p.few_floats + p.many_floats) * 4;
   return OQ_OK;
 }
 
@@ -2398,7 +2396,7 @@ oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const
   const double groups = double(batch->max_q) * heads * batch->n_seq;
   if (plan.tile_rows && groups * plan.many >= double(INT32_MAX))
     return fail(OQ_ERR_UNSUPPORTED, "n_seq * max_q * heads = %.0f: too many rows for one call", groups);
-  const size_t need = attend_ws(cache, batch, plan, heads);
+  const size_t need = (plan.few_floats + plan.many_floats) * 4;
   if (need && (!ws || ws_bytes < need))
     return fail(OQ_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws ? ws_bytes : size_t(0), need);
   ProfScope ps(PK_CACHE_ATTN, st, 4.0 * double(batch->tokens) * heads * cache->head_dim);

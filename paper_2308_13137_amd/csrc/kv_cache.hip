@@ -370,32 +370,63 @@ OQ_DEV unsigned wave_or(unsigned bad) {
   return bad;
 }
 
-// A row's running softmax: the maximum m of its logits in base 2, rounded up to
-// an integer (so it seldom moves), and the sum l of its weights 2^(t - m).  A lane
-// holds NTILE 16-token tiles of one row's scores; four lanes share a row.  Returns
-// the factor that the row's numerators need.
-template <int NTILE>
-OQ_DEV float softmax_step(f32x4_t (&st)[NTILE], float& m, float& l) {
+// Four lanes (16 apart) share a query row: v of lane l combined over l ^ 16, l ^ 32.
+OQ_DEV float over16(float v, bool sum) {
+  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const float a = __uint_as_float(x[0]), b = __uint_as_float(x[1]);
+  return sum ? a + b : fmaxf(a, b);
+}
+OQ_DEV float over32(float v, bool sum) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const float a = __uint_as_float(x[0]), b = __uint_as_float(x[1]);
+  return sum ? a + b : fmaxf(a, b);
+}
+OQ_DEV float row_max(float v) { return over32(over16(v, false), false); }
+OQ_DEV float row_sum(float v) { return over32(over16(v, true), true); }
+
+// A chunk's factors: its scores' (key step x log2(e) / sqrt(d)), and its weights'
+// (value step over the unit), as an exponent and inverted.
+struct Step {
+  float f, lw, winv;
+};
+OQ_DEV Step step_of(float ks_sc, float vs, float vinv) {
+  const float w = vs * vinv * WUNIT;
+  return {ks_sc, __builtin_amdgcn_logf(w), 1.0f / w};
+}
+
+// A row's running softmax: m, the maximum of its logits in base 2 rounded up to an
+// integer (so it seldom moves), and l, this lane's share of the sum of its
+// weights 2^(t - m).  A lane holds the row's scores of NC chunks of 32 tokens (two
+// 16-token tiles each), masked ones -inf; they become the weights times their
+// chunk's factor, which the sum takes out again.  Returns the factor that the
+// row's numerators need.
+template <int NC>
+OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m, float& l) {
   float mt = -INFINITY;
 #pragma unroll
-  for (int a = 0; a < NTILE; ++a)
-    mt = fmaxf(fmaxf(mt, fmaxf(st[a][0], st[a][1])), fmaxf(st[a][2], st[a][3]));
-  mt = fmaxf(mt, __shfl_xor(mt, 16));
-  mt = fmaxf(mt, __shfl_xor(mt, 32));
-  const float mn = fmaxf(m, ceilf(mt));
+  for (int c = 0; c < NC; ++c) {
+    const f32x4_t x = st[2 * c], y = st[2 * c + 1];
+    const float a = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), b = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+    mt = fmaxf(mt, fmaxf(a, b) * sp[c].f);
+  }
+  const float mn = fmaxf(m, ceilf(row_max(mt)));
   const float off = mn == -INFINITY ? 0.0f : mn;         // no token seen yet: weights 2^-inf = 0
   float ls = 0.0f;
 #pragma unroll
-  for (int a = 0; a < NTILE; ++a)
+  for (int c = 0; c < NC; ++c) {
+    const float e = sp[c].lw - off;
+    float w = 0.0f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      st[a][q] = __builtin_amdgcn_exp2f(st[a][q] - off);
-      ls += st[a][q];
-    }
-  ls += __shfl_xor(ls, 16);
-  ls += __shfl_xor(ls, 32);
+    for (int a = 2 * c; a < 2 * c + 2; ++a)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        st[a][q] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[a][q], sp[c].f, e));
+        w += st[a][q];
+      }
+    ls = __builtin_fmaf(w, sp[c].winv, ls);
+  }
   const float alpha = mn == m ? 1.0f : m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
-  l = l * alpha + ls;
+  l = __builtin_fmaf(l, alpha, ls);
   m = mn;
   return alpha;
 }
@@ -411,30 +442,30 @@ OQ_DEV void load_q(bf16x8_t (&qf)[DH / 32], const uint16_t* Q, int64_t ldq, cons
                                *reinterpret_cast<const u32x4_t*>(qp + 64 * (k >> 1) + 16 * g + 8 * (k & 1)));
 }
 
-// Where a row's result goes: the output, or a split's share for cache_join_kernel
-// (numerators, then (m, l) of every row).
+// Where a row's result goes: the output, or a split's share for cache_join_kernel.
+// Shares: numerators [split][unit][row][DH], then (m, l) [split][unit][row]; a unit is
+// a workgroup's rows.
 struct Out {
   uint16_t* O;
   float *LSE, *part;
-  int splits, split, H;
-  int64_t T, ml;                     // ml: where the (m, l) pairs begin, in floats
+  int splits, H;
+  int64_t T, at, ml;                 // at: the workgroup's first share; ml: where the pairs begin, in floats
 };
-OQ_DEV void put_ml(const Out& o, int64_t t, int64_t hd, float m, float l) {
-  if (o.splits == 1) {
-    if (o.LSE) o.LSE[hd * o.T + t] = m + log2f(l);
-  } else {
-    const int64_t at = (int64_t(o.split) * o.T + t) * o.H + hd;
-    reinterpret_cast<float2*>(o.part + o.ml)[at] = make_float2(m, l);
-  }
+OQ_DEV Out out_of(uint16_t* O, float* LSE, float* part, int splits, int split, int H, int64_t T, int64_t units,
+                  int64_t unit, int unit_rows, int DH) {
+  return {O, LSE, part, splits, H, T, (split * units + unit) * unit_rows, splits * units * unit_rows * DH};
 }
-OQ_DEV void put4(const Out& o, int64_t t, int64_t hd, int DH, int ch, float4 x, float l) {
-  if (o.splits == 1) {
+OQ_DEV void put_ml(const Out& o, int row, int64_t t, int64_t hd, float m, float l) {
+  if (o.splits > 1) reinterpret_cast<float2*>(o.part + o.ml)[o.at + row] = make_float2(m, l);
+  else if (o.LSE) o.LSE[hd * o.T + t] = m + log2f(l);
+}
+OQ_DEV void put4(const Out& o, int row, int64_t t, int64_t hd, int DH, int ch, float4 x, float l) {
+  if (o.splits > 1) {
+    *reinterpret_cast<float4*>(o.part + (o.at + row) * DH + ch) = x;
+  } else {
     const float inv = 1.0f / l;
     *reinterpret_cast<uint2*>(o.O + (t * o.H + hd) * DH + ch) =
         make_uint2(f2bf2(x.x * inv, x.y * inv), f2bf2(x.z * inv, x.w * inv));
-  } else {
-    const int64_t at = (int64_t(o.split) * o.T + t) * o.H + hd;
-    *reinterpret_cast<float4*>(o.part + at * DH + ch) = x;
   }
 }
 
@@ -449,7 +480,7 @@ template <int DH, int R>
 __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
                                                            int64_t ldq, int H, uint16_t* __restrict__ O,
                                                            float* __restrict__ LSE, float* __restrict__ part,
-                                                           int splits, int parts) {
+                                                           int splits) {
   constexpr int KS = DH / 32, JD = DH / 16;
   __shared__ float s_o[4][16 * R][DH + 4];
   __shared__ float s_ml[4][16 * R][2];
@@ -480,14 +511,14 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
   const int nch = (total + 31) / 32, ncode = total / P * (P / 32), per = (nch + splits - 1) / splits;
   const int c0 = split * per + wave, c1 = min(nch, (split + 1) * per), c1c = min(c1, ncode);
   auto id_of = [&](int ch) { return ch < c1c ? page_of(c, i, 32 * ch / P) : -1; };
-  auto scores = [&](int h, const bf16x8_t (&kf)[2][KS], float f, int t0, f32x4_t (&st)[2]) {
+  auto scores = [&](int h, const bf16x8_t (&kf)[2][KS], int t0, f32x4_t (&st)[2]) {
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
       st[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) st[a] = mfma(kf[a][k], qf[h][k], st[a]);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) st[a][q] = t0 + 16 * a + 4 * g + q > lim[h] ? -INFINITY : st[a][q] * f;
+      for (int q = 0; q < 4; ++q) st[a][q] = t0 + 16 * a + 4 * g + q > lim[h] ? -INFINITY : st[a][q];
     }
   };
   auto rescale = [&](int h, float alpha) {
@@ -508,15 +539,16 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
         nx.load(c, idn, u, 32 * (ch + 4) % P, lane);
         idn = id_of(ch + 8);
       }
-      // a page that stands for NaN: rows that see it are NaN, its codes count for nothing
+      // a page that stands for NaN: rows that see it are NaN, any finite step will do
       if (!(cur.ks < INFINITY && cur.vs < INFINITY)) {
 #pragma unroll
         for (int h = 0; h < R; ++h)
           if (lim[h] >= t0) l[h] = NAN;
-        cur.ks = cur.vs = 0.0f;
+        cur.ks = cur.vs = 1.0f;
       }
       const float vr = fmaxf(vref, pow2_above(cur.vs));
-      const float vinv = pow2_inv(vr), vscale = cur.vs * vinv * WUNIT, shrink = vref * vinv;
+      const float vinv = pow2_inv(vr), shrink = vref * vinv;
+      const Step sp[1] = {step_of(cur.ks * sc, cur.vs, vinv)};
       bf16x8_t kf[2][KS];
 #pragma unroll
       for (int a = 0; a < 2; ++a)
@@ -530,12 +562,11 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
 #pragma unroll
       for (int h = 0; h < R; ++h) {
         f32x4_t st[2];
-        scores(h, kf, cur.ks * sc, t0, st);
-        rescale(h, softmax_step<2>(st, m[h], l[h]) * shrink);
+        scores(h, kf, t0, st);
+        rescale(h, softmax_step<1>(st, sp, m[h], l[h]) * shrink);
         u32x4_t w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          w[e] = pack_f16(st[e >> 1][2 * (e & 1)] * vscale, st[e >> 1][2 * (e & 1) + 1] * vscale);
+        for (int e = 0; e < 4; ++e) w[e] = pack_f16(st[e >> 1][2 * (e & 1)], st[e >> 1][2 * (e & 1) + 1]);
         pb[h] = __builtin_bit_cast(f16x8_t, w);
       }
       vref = vr;
@@ -570,17 +601,17 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
 #pragma unroll
     for (int j = 0; j < JD; ++j) vf[j] = __builtin_bit_cast(bf16x8_t, win.value(j, bad));
     bad = wave_or(bad);
-    const float wunit = pow2_inv(vref) * WUNIT;
+    const Step sp[1] = {step_of(sc, 1.0f, pow2_inv(vref))};
 #pragma unroll
     for (int h = 0; h < R; ++h) {
       if (bad && lim[h] >= t0 + __ffs(int(bad)) - 1) l[h] = NAN;
       f32x4_t st[2];
-      scores(h, kf, sc, t0, st);
-      rescale(h, softmax_step<2>(st, m[h], l[h]));
+      scores(h, kf, t0, st);
+      rescale(h, softmax_step<1>(st, sp, m[h], l[h]));
       u32x4_t wh, wl;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = st[e >> 1][2 * (e & 1)] * wunit, y = st[e >> 1][2 * (e & 1) + 1] * wunit;
+        const float x = st[e >> 1][2 * (e & 1)], y = st[e >> 1][2 * (e & 1) + 1];
         wh[e] = f2bf2(x, y);
         wl[e] = f2bf2(x - __uint_as_float(wh[e] << 16), y - __uint_as_float(wh[e] & 0xffff0000u));
       }
@@ -593,6 +624,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
   }
 #pragma unroll
   for (int h = 0; h < R; ++h) {
+    l[h] = row_sum(l[h]);
 #pragma unroll
     for (int j = 0; j < JD; ++j)
       *reinterpret_cast<f32x4_t*>(&s_o[wave][16 * h + r][16 * j + 4 * g]) = acc[h][j] * (vref / WUNIT);
@@ -602,7 +634,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
     }
   }
   __syncthreads();
-  const Out out{O, LSE, part, splits, split, H, c.T, int64_t(parts) * c.T * H * DH};
+  const Out out = out_of(O, LSE, part, splits, split, H, c.T, int64_t(c.n_seq) * c.Hkv, int64_t(i) * c.Hkv + u, 16 * R, DH);
   for (int e = tid; e < 4 * R * DH; e += 256) {          // 16 R rows of DH / 4 fours
     const int row = e / (DH / 4), c4 = 4 * (e % (DH / 4));
     if (row >= rows) break;
@@ -618,8 +650,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
     }
     if (!s.ok) ll = NAN;
     const int64_t t = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
-    put4(out, t, hd, DH, c4, o, ll);
-    if (c4 == 0) put_ml(out, t, hd, mm, ll);
+    put4(out, row, t, hd, DH, c4, o, ll);
+    if (c4 == 0) put_ml(out, row, t, hd, mm, ll);
   }
 }
 
@@ -630,7 +662,7 @@ template <int DH, int R>
 __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
                                                                 int64_t ldq, int H, uint16_t* __restrict__ O,
                                                                 float* __restrict__ LSE,
-                                                                float* __restrict__ part, int splits, int parts,
+                                                                float* __restrict__ part, int splits,
                                                                 int rows_min) {
   constexpr int KS = DH / 32, JD = DH / 16, QW = 64 * R;
   constexpr int TILE = 64 * DH / 8;                      // 16-byte pieces of one operand's tile
@@ -679,10 +711,15 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
   const int cc = wave >> 1, hw = wave & 1;
   u32x4_t rk[NL], rv[NL];
   float ks = 0.0f, vs = 0.0f;
+  // the page of this wave's chunk of tile t (a page number is a load of its own: it
+  // is fetched a tile before the codes are)
+  auto id_of = [&](int t) { return t < k1 && 64 * t + 32 * cc < closed ? page_of(c, i, (64 * t + 32 * cc) / P) : -1; };
+  int idn = id_of(k0);
   auto load = [&](int t) {                               // tile t, if its chunk is in a full page
-    const int t0 = 64 * t + 32 * cc;
+    const int t0 = 64 * t + 32 * cc, id = idn;
+    idn = id_of(t + 1);
     if (t0 < closed) {
-      const int pg = t0 / P, id = page_of(c, i, pg);
+      const int pg = t0 / P;
       const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
       ks = id < 0 ? NAN : c.ks[blk];
       vs = id < 0 ? NAN : c.vs[blk];
@@ -717,8 +754,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
       }
       if (hw == 0 && lane == 0) {
         const bool fine = ks < INFINITY && vs < INFINITY;
-        s_step[b][cc][0] = fine ? ks * sc : 0.0f;
-        s_step[b][cc][1] = fine ? vs : 0.0f;
+        s_step[b][cc][0] = fine ? ks * sc : sc;
+        s_step[b][cc][1] = fine ? vs : 1.0f;
         s_bad[b][cc][0] = fine ? 0u : 1u;
         s_bad[b][cc][1] = 0u;
       }
@@ -738,7 +775,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
       }
       bad = wave_or(bad);
       if (lane == 0) {
-        s_step[b][cc][hw] = hw ? 1.0f : in ? sc : 0.0f;
+        s_step[b][cc][hw] = hw ? 1.0f : sc;
         s_bad[b][cc][hw] = bad;
       }
     }
@@ -773,8 +810,6 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
 #pragma unroll
         for (int h = 0; h < R; ++h) st[h][a] = mfma(kf, qf[h][k], st[h][a]);
       }
-#pragma unroll
-      for (int h = 0; h < R; ++h) st[h][a] = st[h][a] * (a < 2 ? f0 : f1);
     }
     if (t0 + 63 > first_lim) {
 #pragma unroll
@@ -797,9 +832,10 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     const float vr = fmaxf(vref, fmaxf(pow2_above(vs0), pow2_above(vs1)));
     const float vinv = pow2_inv(vr), shrink = vref * vinv;
     vref = vr;
+    const Step sp[2] = {step_of(f0, vs0, vinv), step_of(f1, vs1, vinv)};
 #pragma unroll
     for (int h = 0; h < R; ++h) {
-      const float alpha = softmax_step<4>(st[h], m[h], l[h]) * shrink;
+      const float alpha = softmax_step<2>(st[h], sp, m[h], l[h]) * shrink;
       if (__any(alpha != 1.0f)) {
 #pragma unroll
         for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * alpha;
@@ -807,14 +843,13 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     }
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
-      const float vsc = (k2 ? vs1 : vs0) * vinv * WUNIT;
       u32x4_t ph[R], pl[TAIL ? R : 1];
 #pragma unroll
       for (int h = 0; h < R; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const f32x4_t p = st[h][2 * k2 + (e >> 1)];
-          const float p0 = p[2 * (e & 1)] * vsc, p1 = p[2 * (e & 1) + 1] * vsc;
+          const float p0 = p[2 * (e & 1)], p1 = p[2 * (e & 1) + 1];
           if constexpr (TAIL) {
             ph[h][e] = f2bf2(p0, p1);
             pl[h][e] = f2bf2(p0 - __uint_as_float(ph[h][e] << 16), p1 - __uint_as_float(ph[h][e] & 0xffff0000u));
@@ -840,51 +875,85 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
   int t = k0;
   for (; t < min(k1, ntc); ++t) tile(t, std::false_type{});
   for (; t < k1; ++t) tile(t, std::true_type{});
-  const Out out{O, LSE, part, splits, split, H, c.T, int64_t(parts) * c.T * H * DH};
+  const Out out = out_of(O, LSE, part, splits, split, H, c.T, int64_t(ntile) * c.n_seq * c.Hkv,
+                         (int64_t(rt) * c.n_seq + i) * c.Hkv + u, QW, DH);
+#pragma unroll
+  for (int h = 0; h < R; ++h) l[h] = row_sum(l[h]);
 #pragma unroll
   for (int h = 0; h < R; ++h) {
     const int row = row0 + 16 * (R * wave + h) + r;
     if (row >= rows) continue;
-    const float ll = s.ok ? l[h] : NAN;
+    const float ll = s.ok ? l[h] : NAN;                  // (the row's: summed above)
     const int64_t t = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
 #pragma unroll
     for (int j = 0; j < JD; ++j) {
       const f32x4_t o = acc[h][j] * (vref / WUNIT);
-      put4(out, t, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), ll);
+      put4(out, row - row0, t, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), ll);
     }
-    if (g == 0) put_ml(out, t, hd, m[h], ll);
+    if (g == 0) put_ml(out, row - row0, t, hd, m[h], ll);
   }
 }
 
-// Joins a row's splits: one thread per four output values.  Sequences of up to
-// `rows_few` rows have `few` splits, the others `many`.
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, int DH,
-                                                         const float* __restrict__ part, int parts, int few,
-                                                         int many, int rows_few, uint16_t* __restrict__ O,
+// Joins a row's splits: DH / 4 lanes of four output values each, NG groups of them
+// dealing the splits among themselves; 256 threads take 1024 / (DH NG) rows.
+struct JoinArgs {
+  const float *few, *many;           // shares of the two kernels
+  int few_splits, many_splits, row_rows, tile_rows;
+};
+template <int DH, int NG>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, JoinArgs a, uint16_t* __restrict__ O,
                                                          float* __restrict__ LSE) {
-  const Seq s = seq_of(c, blockIdx.y);
-  const int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  const int q4 = DH / 4;
-  if (e >= int64_t(s.n) * H * q4) return;
-  const int splits = s.n * (H / c.Hkv) <= rows_few ? few : many;
-  if (splits == 1) return;
-  const int64_t at = int64_t(s.b) * H + e / q4;
-  const int ch = 4 * int(e % q4);
-  const float2* ml = reinterpret_cast<const float2*>(part + int64_t(parts) * c.T * H * DH);
-  float mm = -INFINITY, ll = 0.0f;
-  for (int k = 0; k < splits; ++k) mm = fmaxf(mm, ml[k * c.T * H + at].x);
+  constexpr int Q4 = DH / 4, RW = 256 / (Q4 * NG);
+  __shared__ float4 s_o[NG][RW][Q4];
+  __shared__ float2 s_ml[NG][RW];
+  const int i = blockIdx.y, G = H / c.Hkv;
+  const Seq s = seq_of(c, i);
+  const int lane = threadIdx.x % Q4, ng = (threadIdx.x / Q4) % NG, rw = threadIdx.x / (Q4 * NG);
+  const int64_t e = int64_t(blockIdx.x) * RW + rw;       // row: token of the sequence x head
+  const bool few = s.n * G <= a.row_rows;
+  const int splits = few ? a.few_splits : a.many_splits;
+  if (splits == 1 || int64_t(blockIdx.x) * RW >= int64_t(s.n) * H) return;
+  const bool in = e < int64_t(s.n) * H;
+  const int j = in ? int(e / H) : 0, hd = in ? int(e % H) : 0, u = hd / G, row = j * G + hd % G;
+  const int rows = few ? a.row_rows : a.tile_rows, ntile = few ? 1 : (c.max_q * G + rows - 1) / rows;
+  const int64_t units = int64_t(ntile) * c.n_seq * c.Hkv;
+  const int64_t at = ((int64_t(few ? 0 : row / rows) * c.n_seq + i) * c.Hkv + u) * rows + row % rows;
+  const float* part = few ? a.few : a.many;
+  const float2* ml = reinterpret_cast<const float2*>(part + splits * units * rows * DH);
+  float m = -INFINITY, l = 0.0f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k = 0; k < splits; ++k) {
-    const float2 w = ml[k * c.T * H + at];
-    const bool none = w.x == -INFINITY;                  // no token in this split (or NaN)
-    const float f = none ? 0.0f : __builtin_amdgcn_exp2f(w.x - mm);
-    ll += none ? w.y : f * w.y;
-    const float4 x = *reinterpret_cast<const float4*>(part + (k * c.T * H + at) * DH + ch);
-    o = make_float4(o.x + f * x.x, o.y + f * x.y, o.z + f * x.z, o.w + f * x.w);
+  auto join = [&](float mk, float lk, float4 x) {
+    const float mn = fmaxf(m, mk);
+    const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+    const float fk = mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - mn);
+    // (without a token l is 0 or, for a NaN row, NaN: it stays)
+    l = (m == -INFINITY ? l : f * l) + (mk == -INFINITY ? lk : fk * lk);
+    o = make_float4(f * o.x + fk * x.x, f * o.y + fk * x.y, f * o.z + fk * x.z, f * o.w + fk * x.w);
+    m = mn;
+  };
+#pragma unroll 4
+  for (int k = ng; k < splits; k += NG) {
+    const int64_t p = k * units * rows + at;
+    const float2 w = ml[p];
+    join(w.x, w.y, *reinterpret_cast<const float4*>(part + p * DH + 4 * lane));
   }
-  const float inv = 1.0f / ll;
-  *reinterpret_cast<uint2*>(O + at * DH + ch) = make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
-  if (LSE && ch == 0) LSE[(at % H) * c.T + at / H] = mm + log2f(ll);
+  if constexpr (NG > 1) {
+    s_o[ng][rw][lane] = o;
+    if (lane == 0) s_ml[ng][rw] = make_float2(m, l);
+    __syncthreads();
+    if (ng > 0) return;
+#pragma unroll
+    for (int k = 1; k < NG; ++k) {
+      const float2 w = s_ml[k][rw];
+      join(w.x, w.y, s_o[k][rw][lane]);
+    }
+  }
+  if (!in) return;
+  const float inv = 1.0f / l;
+  const int64_t t = int64_t(s.b) + j;
+  *reinterpret_cast<uint2*>(O + (t * H + hd) * DH + 4 * lane) =
+      make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
+  if (LSE && lane == 0) LSE[hd * c.T + t] = m + log2f(l);
 }
 
 }  // namespace
@@ -920,48 +989,55 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
 
 // How a call is cut up, from its sizes alone.  Rows of a key head: up to 32 go to
 // the row kernel, more to the tile kernel; a batch of prompts and decoding
-// sequences runs both, each on its own.
-AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int max_q, int64_t max_len) {
+// sequences (tokens well below n_seq * max_q) runs both, each on its own.
+AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d) {
   const int64_t rows = int64_t(max_q) * (H / Hkv), heads = int64_t(n_seq) * Hkv;
+  const bool mixed = n_seq > 1 && 4 * tokens < 3 * int64_t(n_seq) * max_q;
   AttendPlan p;
   p.tile_rows = rows <= 32 ? 0 : rows <= 64 ? 64 : 128;
-  p.row_rows = rows <= 16 ? 16 : rows <= 32 || n_seq > 1 ? 32 : 0;
+  p.row_rows = rows <= 16 ? 16 : rows <= 32 || mixed ? 32 : 0;
   auto cut = [](int64_t want, int64_t most) { return int(std::max<int64_t>(1, std::min(want, most))); };
   p.few = p.row_rows ? cut((1024 + heads - 1) / heads, std::min<int64_t>(128, max_len / 256)) : 1;
   const int64_t tiles = p.tile_rows ? (rows + p.tile_rows - 1) / p.tile_rows * heads : 0;
   p.many = p.tile_rows ? cut(512 / std::max<int64_t>(1, tiles), std::min<int64_t>(64, max_len / 512)) : 1;
+  p.few_floats = p.few > 1 ? size_t(p.few) * size_t(heads) * size_t(p.row_rows) * size_t(d + 2) : 0;
+  p.many_floats = p.many > 1 ? size_t(p.many) * size_t(tiles) * size_t(p.tile_rows) * size_t(d + 2) : 0;
   return p;
 }
 
 hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int H, uint16_t* O, float* LSE,
                         float* ws, const AttendPlan& p, hipStream_t st) {
-  const int parts = std::max(p.few, p.many), G = H / c.Hkv;
+  const int G = H / c.Hkv;
+  float* ws_many = ws + p.few_floats;
   auto few = [&](auto dh, auto rr) {
     constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
     const dim3 grid(unsigned(p.few), unsigned(c.Hkv), unsigned(c.n_seq));
-    hipLaunchKernelGGL((cache_attend_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, p.few,
-                       parts);
+    hipLaunchKernelGGL((cache_attend_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, p.few);
   };
   auto many = [&](auto dh, auto rr) {
     constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
     const int64_t tiles = (int64_t(c.max_q) * G + 64 * R - 1) / (64 * R);
     const dim3 grid(unsigned(tiles * c.n_seq * p.many * c.Hkv));
-    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws,
-                       p.many, parts, p.row_rows + 1);
+    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws_many,
+                       p.many, p.row_rows + 1);
   };
-  auto by_rows = [&](auto dh) {
+  auto join = [&](auto dh, auto ng) {
+    constexpr int DH = decltype(dh)::value, NG = decltype(ng)::value, RW = 1024 / (DH * NG);
+    const JoinArgs a{ws, ws_many, p.few, p.many, p.row_rows, p.tile_rows};
+    const dim3 grid(unsigned((int64_t(c.max_q) * H + RW - 1) / RW), unsigned(c.n_seq));
+    hipLaunchKernelGGL((cache_join_kernel<DH, NG>), grid, dim3(256), 0, st, c, H, a, O, LSE);
+  };
+  auto run = [&](auto dh) {
     if (p.tile_rows == 64) many(dh, std::integral_constant<int, 1>{});
     else if (p.tile_rows) many(dh, std::integral_constant<int, 2>{});
     if (p.row_rows == 16) few(dh, std::integral_constant<int, 1>{});
     else if (p.row_rows) few(dh, std::integral_constant<int, 2>{});
+    const int splits = std::max(p.few, p.many);
+    if (splits > 8) join(dh, std::integral_constant<int, 8>{});
+    else if (splits > 1) join(dh, std::integral_constant<int, 1>{});
   };
-  if (c.d == 64) by_rows(std::integral_constant<int, 64>{});
-  else by_rows(std::integral_constant<int, 128>{});
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || parts == 1) return e;
-  const dim3 grid(unsigned((int64_t(c.max_q) * H * (c.d / 4) + 255) / 256), unsigned(c.n_seq));
-  hipLaunchKernelGGL(cache_join_kernel, grid, dim3(256), 0, st, c, H, c.d, ws, parts, p.few, p.many, p.row_rows,
-                     O, LSE);
+  if (c.d == 64) run(std::integral_constant<int, 64>{});
+  else run(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
 

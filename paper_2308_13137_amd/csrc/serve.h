@@ -60,9 +60,9 @@ struct AttendPlan {
   int row_rows;    // rows of a workgroup of the row kernel (16, 32; 0: not used)
   int tile_rows;   // rows of a workgroup of the tile kernel (64, 128; 0: not used)
   int few, many;   // splits of a row's tokens in the two
+  size_t few_floats, many_floats;  // their shares in the workspace
 };
-AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int max_q, int64_t max_len);
-// ws: max(few, many) * T * H * (d + 2) fp32 where that is more than one split
+AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d);
 hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int H, uint16_t* O, float* LSE,
                         float* ws, const AttendPlan& p, hipStream_t st);
 
