@@ -701,7 +701,7 @@ oq_status oq_rope_table(int64_t n_pos, int head_dim, float base, float* tab, hip
  *            32 c + 16 (e / 4) + 4 g + e % 4
  *   K window [page][d];  V window [page/32][d/16][g][r][8]: channel 16 j + r, tokens
  *            as in V codes
- * head_dim 64 or 128; page a multiple of 32, at most 128. */
+ * head_dim 64 or 128; page 32, 64 or 128. */
 typedef struct {
   int n_pages, n_slots, page, kv_heads, head_dim;
   int8_t* k_codes;                 /* [n_pages, kv_heads, page * head_dim]             */

@@ -2201,9 +2201,9 @@ namespace {
 
 oq_status check_cache(const oq_kv_cache* c, const oq_kv_batch* b) {
   OQ_REQ(c && b, "cache and batch are required");
-  if ((c->head_dim != 64 && c->head_dim != 128) || c->page <= 0 || c->page % 32 || c->page > 128)
-    return fail(OQ_ERR_UNSUPPORTED, "head_dim=%d (need 64 or 128), page=%d (need 32, 64, 96 or 128)",
-                c->head_dim, c->page);
+  if ((c->head_dim != 64 && c->head_dim != 128) || (c->page != 32 && c->page != 64 && c->page != 128))
+    return fail(OQ_ERR_UNSUPPORTED, "head_dim=%d (need 64 or 128), page=%d (need 32, 64 or 128)", c->head_dim,
+                c->page);
   OQ_REQ(c->n_pages > 0 && c->n_slots > 0 && c->kv_heads > 0 && c->kv_heads <= 65535,
          "bad cache n_pages=%d n_slots=%d kv_heads=%d", c->n_pages, c->n_slots, c->kv_heads);
   OQ_REQ(c->k_codes && c->v_codes && c->k_scale && c->v_scale && c->k_window && c->v_window,
@@ -2237,6 +2237,7 @@ CacheArgs cache_args(const oq_kv_cache* c, const oq_kv_batch* b) {
   a.n_pages = c->n_pages;
   a.n_slots = c->n_slots;
   a.P = c->page;
+  a.lgP = c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
   a.Hkv = c->kv_heads;
   a.d = c->head_dim;
   a.table = b->table;

@@ -465,7 +465,7 @@ struct Window {
   const u32x4_t* v;
   int left, lane;                                        // tokens of the chunk inside the sequence
   OQ_DEV Window(const CacheArgs& c, const Seq& s, int u, int t0, int total, int ln) : left(total - t0), lane(ln) {
-    const int pg = t0 / c.P, tin = t0 - pg * c.P;
+    const int pg = t0 >> c.lgP, tin = t0 & (c.P - 1);
     const int64_t at = ((int64_t(s.slot) * 2 + (pg & 1)) * c.Hkv + u) * c.P * DH + int64_t(tin) * DH;
     k = c.kw + at;
     v = reinterpret_cast<const u32x4_t*>(c.vw + at) + ln;
@@ -515,23 +515,27 @@ OQ_DEV float row_max(float v) { return over32(over16(v, false), false); }
 OQ_DEV float row_sum(float v) { return over32(over16(v, true), true); }
 
 // A chunk's factors: its scores' (key step x log2(e) / sqrt(d)), and its weights'
-// (value step over the unit), as an exponent and inverted.
+// (value step over the unit vref / WUNIT) as an exponent and inverted.
 struct Step {
   float f, lw, winv;
 };
-OQ_DEV Step step_of(float ks_sc, float vs, float vinv) {
-  const float w = vs * vinv * WUNIT;
-  return {ks_sc, __builtin_amdgcn_logf(w), 1.0f / w};
+// `q` = (key step x scale, value step, its log2, its inverse); vr = vref, a power of two.
+OQ_DEV float4 step_parts(float ks_sc, float vs) {
+  return make_float4(ks_sc, vs, __builtin_amdgcn_logf(vs), 1.0f / vs);
+}
+OQ_DEV Step step_of(float4 q, float vr) {
+  const float e = float(int(__float_as_uint(vr) >> 23) - 127 - 15);
+  return {q.x, q.z - e, q.w * (vr * (1.0f / WUNIT))};
 }
 
 // A row's running softmax: m, the maximum of its logits in base 2 rounded up to an
 // integer (so it seldom moves), and l, this lane's share of the sum of its
 // weights 2^(t - m).  A lane holds the row's scores of NC chunks of 32 tokens (two
-// 16-token tiles each), masked ones -inf; they become the weights times their
-// chunk's factor, which the sum takes out again.  Returns the factor that the
-// row's numerators need.
+// 16-token tiles each), masked ones -inf.  softmax_max takes the new maximum in
+// and returns the factor of the row's numerators; weight() turns a score into
+// its weight times its chunk's factor, which the sum takes out again.
 template <int NC>
-OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m, float& l) {
+OQ_DEV float softmax_max(const f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m, float& l, float& off) {
   float mt = -INFINITY;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -540,24 +544,31 @@ OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m,
     mt = fmaxf(mt, fmaxf(a, b) * sp[c].f);
   }
   const float mn = fmaxf(m, ceilf(row_max(mt)));
-  const float off = mn == -INFINITY ? 0.0f : mn;         // no token seen yet: weights 2^-inf = 0
-  float ls = 0.0f;
+  off = mn == -INFINITY ? 0.0f : mn;                     // no token seen yet: weights 2^-inf = 0
+  const float alpha = mn == m ? 1.0f : m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+  l *= alpha;
+  m = mn;
+  return alpha;
+}
+OQ_DEV float weight(float score, const Step& sp, float off) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(score, sp.f, sp.lw - off));
+}
+template <int NC>
+OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m, float& l) {
+  float off;
+  const float alpha = softmax_max<NC>(st, sp, m, l, off);
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const float e = sp[c].lw - off;
     float w = 0.0f;
 #pragma unroll
     for (int a = 2 * c; a < 2 * c + 2; ++a)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        st[a][q] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[a][q], sp[c].f, e));
+        st[a][q] = weight(st[a][q], sp[c], off);
         w += st[a][q];
       }
-    ls = __builtin_fmaf(w, sp[c].winv, ls);
+    l = __builtin_fmaf(w, sp[c].winv, l);
   }
-  const float alpha = mn == m ? 1.0f : m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
-  l = __builtin_fmaf(l, alpha, ls);
-  m = mn;
   return alpha;
 }
 
@@ -638,9 +649,9 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
 #pragma unroll
     for (int j = 0; j < JD; ++j) acc[h][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  const int nch = (total + 31) / 32, ncode = total / P * (P / 32), per = (nch + splits - 1) / splits;
+  const int nch = (total + 31) / 32, ncode = (total >> c.lgP) * (P / 32), per = (nch + splits - 1) / splits;
   const int c0 = split * per + wave, c1 = min(nch, (split + 1) * per), c1c = min(c1, ncode);
-  auto id_of = [&](int ch) { return ch < c1c ? page_of(c, i, 32 * ch / P) : -1; };
+  auto id_of = [&](int ch) { return ch < c1c ? page_of(c, i, (32 * ch) >> c.lgP) : -1; };
   auto scores = [&](int h, const bf16x8_t (&kf)[2][KS], int t0, f32x4_t (&st)[2]) {
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
@@ -660,13 +671,13 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
   int ch = c0;
   if (ch < c1c) {
     Codes<DH> nx;
-    nx.load(c, id_of(ch), u, 32 * ch % P, lane);
+    nx.load(c, id_of(ch), u, 32 * ch & (P - 1), lane);
     int idn = id_of(ch + 4);
     for (; ch < c1c; ch += 4) {
       const int t0 = 32 * ch;
       Codes<DH> cur = nx;
       if (ch + 4 < c1c) {
-        nx.load(c, idn, u, 32 * (ch + 4) % P, lane);
+        nx.load(c, idn, u, 32 * (ch + 4) & (P - 1), lane);
         idn = id_of(ch + 8);
       }
       // a page that stands for NaN: rows that see it are NaN, any finite step will do
@@ -677,8 +688,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
         cur.ks = cur.vs = 1.0f;
       }
       const float vr = fmaxf(vref, pow2_above(cur.vs));
-      const float vinv = pow2_inv(vr), shrink = vref * vinv;
-      const Step sp[1] = {step_of(cur.ks * sc, cur.vs, vinv)};
+      const float shrink = vref * pow2_inv(vr);
+      const Step sp[1] = {step_of(step_parts(cur.ks * sc, cur.vs), vr)};
       bf16x8_t kf[2][KS];
 #pragma unroll
       for (int a = 0; a < 2; ++a)
@@ -731,7 +742,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
 #pragma unroll
     for (int j = 0; j < JD; ++j) vf[j] = __builtin_bit_cast(bf16x8_t, win.value(j, bad));
     bad = wave_or(bad);
-    const Step sp[1] = {step_of(sc, 1.0f, pow2_inv(vref))};
+    const Step sp[1] = {step_of(step_parts(sc, 1.0f), vref)};
 #pragma unroll
     for (int h = 0; h < R; ++h) {
       if (bad && lim[h] >= t0 + __ffs(int(bad)) - 1) l[h] = NAN;
@@ -785,20 +796,30 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
   }
 }
 
-// Many rows (prompts): one workgroup takes 64 R rows of one key head, 16 R per wave,
-// over tiles of 64 tokens.  The waves turn a tile's codes into operands once, in
-// LDS, a tile ahead; the raw codes of the one after are in flight meanwhile.
-template <int DH, int R>
-__global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
-                                                                int64_t ldq, int H, uint16_t* __restrict__ O,
-                                                                float* __restrict__ LSE,
-                                                                float* __restrict__ part, int splits,
-                                                                int rows_min) {
-  constexpr int KS = DH / 32, JD = DH / 16, QW = 64 * R;
+// Many rows (prompts): one workgroup of NW waves takes 16 NW rows of one key head
+// over tiles of 64 tokens.  The waves turn a tile's codes into f16 operands once, in
+// LDS, a tile ahead; the raw codes of the one after are in flight meanwhile.  16
+// rows a wave keep the kernel within 128 registers, four waves to a SIMD: the
+// matrix instructions, the softmax and the conversions of different waves run
+// beside each other (32 rows a wave and two waves to a SIMD, with the same work
+// interleaved by hand, took 303 us where this takes TIME_PROMPT).
+//
+// Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
+// largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
+// 2^-39 of that entry.
+template <int DH, int NW>
+__global__ __launch_bounds__(64 * NW, 4) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
+                                                                       int64_t ldq, int H,
+                                                                       uint16_t* __restrict__ O,
+                                                                       float* __restrict__ LSE,
+                                                                       float* __restrict__ part, int splits,
+                                                                       int rows_min) {
+  constexpr int KS = DH / 32, JD = DH / 16, QW = 16 * NW;
   constexpr int TILE = 64 * DH / 8;                      // 16-byte pieces of one operand's tile
+  constexpr int CW = NW / 2, LPW = JD / CW;              // waves of a chunk, loads of a wave
   __shared__ u32x4_t s_k[2][TILE], s_v[2][TILE];
-  __shared__ float s_step[2][2][2];                      // [buffer][chunk](key step x scale, value step)
-  __shared__ unsigned s_bad[2][2][2];
+  __shared__ float4 s_step[2][2];                        // [buffer][chunk], step_parts
+  __shared__ unsigned s_bad[2][2][CW];
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // key heads fastest (an XCD keeps its heads' pages in its L2), longest rows first
@@ -813,99 +834,108 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
   const Seq s = seq_of(c, i);
   const int rows = s.n * G, row0 = rt * QW;
   if (rows < rows_min || row0 >= rows) return;
-  const int total = s.ok ? s.L + s.n : 0, closed = total / P * P;
+  const int total = s.ok ? s.L + s.n : 0, closed = total & ~(P - 1);
   const float sc = 1.4426950408889634f / sqrtf(float(DH));
 
-  bf16x8_t qf[R][KS];
-  int lim[R];
-  f32x4_t acc[R][JD];
-  float m[R], l[R], vref = VREF0;
+  const int row = min(row0 + 16 * wave + r, rows - 1), lim = s.L + row / G;   // lim: the last token the row sees
+  bf16x8_t qf[KS];                                       // f16 (times 1 / qs), bf16 for the open page
+  float qs;
+  load_q<DH>(qf, Q, ldq, s, u, G, row, g);
+  {
+    float top = 0.0f;
 #pragma unroll
-  for (int h = 0; h < R; ++h) {
-    const int row = min(row0 + 16 * (R * wave + h) + r, rows - 1);
-    lim[h] = s.L + row / G;
-    load_q<DH>(qf[h], Q, ldq, s, u, G, row, g);
-    m[h] = -INFINITY;
-    l[h] = 0.0f;
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
-    for (int j = 0; j < JD; ++j) acc[h][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(float(qf[k][e])));
+    const int e = min(max(int(__float_as_uint(row_max(top)) >> 23), 20), 253);
+    const float up = __uint_as_float(uint32_t(254 + 14 - e) << 23 & 0x7f800000u);
+    qs = __uint_as_float(uint32_t(e - 14) << 23);        // 2^(exponent - 14)
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      u32x4_t w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = pack_f16(float(qf[k][2 * q]) * up, float(qf[k][2 * q + 1]) * up);
+      qf[k] = __builtin_bit_cast(bf16x8_t, w);
+    }
   }
+  f32x4_t acc[JD];
+  float m = -INFINITY, l = 0.0f, vref = VREF0;
+#pragma unroll
+  for (int j = 0; j < JD; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const int first_lim = s.L + row0 / G;                  // what every row of the tile sees
   const int seen = s.ok ? s.L + min(row0 + QW - 1, rows - 1) / G + 1 : 0;
   const int nt = (seen + 63) / 64, per = (nt + splits - 1) / splits;
   const int k0 = split * per, k1 = min(nt, (split + 1) * per);
   const int ntc = closed / 64;                           // tiles of full pages only
-  // this wave's share of a tile: half (wave % 2) of chunk wave / 2 of the keys and
-  // of the values, DH / 64 loads each
-  constexpr int NL = DH / 64;
-  const int cc = wave >> 1, hw = wave & 1;
-  u32x4_t rk[NL], rv[NL];
+  // this wave's share of a tile: loads LPW hw .. of chunk cc, the first half of a
+  // chunk's waves of its keys, the others of its values
+  const int cc = wave / CW, hw = wave % CW;
+  const bool vals = hw >= CW / 2;
+  const int first_load = LPW * (vals ? hw - CW / 2 : hw);
+  u32x4_t raw[LPW];
   float ks = 0.0f, vs = 0.0f;
-  // the page of this wave's chunk of tile t (a page number is a load of its own: it
-  // is fetched a tile before the codes are)
-  auto id_of = [&](int t) { return t < k1 && 64 * t + 32 * cc < closed ? page_of(c, i, (64 * t + 32 * cc) / P) : -1; };
+  // The page of this wave's chunk of tile t (a page number is a load of its own: it
+  // is fetched a tile before the codes are).  Page numbers and steps come by vector
+  // loads, though the whole wave reads one word: scalar loads share a counter with
+  // the LDS reads, whose waits would then last until memory has answered.
+  int zero = 0;
+  asm("" : "+v"(zero));
+  auto id_of = [&](int t) {
+    return t < k1 && 64 * t + 32 * cc < closed ? page_of(c, i, ((64 * t + 32 * cc) >> c.lgP) + zero) : -1;
+  };
   int idn = id_of(k0);
   auto load = [&](int t) {                               // tile t, if its chunk is in a full page
-    const int t0 = 64 * t + 32 * cc, id = idn;
-    idn = id_of(t + 1);
+    const int t0 = 64 * t + 32 * cc, id = __builtin_amdgcn_readfirstlane(idn);
     if (t0 < closed) {
-      const int pg = t0 / P;
       const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
-      ks = id < 0 ? NAN : c.ks[blk];
-      vs = id < 0 ? NAN : c.vs[blk];
-      const int64_t at = blk * P * DH + (t0 - pg * P) * DH;
-      const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(c.kc + at) + 64 * NL * hw + lane;
-      const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(c.vc + at) + 64 * NL * hw + lane;
-#pragma unroll
-      for (int j = 0; j < NL; ++j) {
-        rk[j] = kp[64 * j];
-        rv[j] = vp[64 * j];
+      if (hw == 0) {
+        ks = id < 0 ? NAN : c.ks[blk + zero];
+        vs = id < 0 ? NAN : c.vs[blk + zero];
       }
+      const u32x4_t* p = reinterpret_cast<const u32x4_t*>((vals ? c.vc : c.kc) + blk * P * DH + (t0 & (P - 1)) * DH) +
+                         64 * first_load + lane;
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) raw[j] = p[64 * j];
+      idn = id_of(t + 1);
     }
   };
-  // operands of tile t into buffer b: fragment f of 64 lanes at 64 f, chunk cc's
-  // keys at tile a = 2 cc + hw, its values at 2 JD/2 fragments per half
+  auto steps = [&](int b) {
+    if (hw == 0 && lane == 0) {
+      const bool fine = ks < INFINITY && vs < INFINITY;
+      s_step[b][cc] = step_parts(fine ? ks * sc : sc, fine ? vs : 1.0f);
+      s_bad[b][cc][0] = fine ? 0u : 1u;
+    }
+    if (hw > 0 && lane == 0) s_bad[b][cc][hw] = 0u;
+  };
+  // Operands of tile t into buffer b, fragment f of a chunk (64 lanes) at 64 f: f16,
+  // or bf16 where the tile reaches into the open page (from ntc on).
   auto store = [&](int t, int b) {
     const int t0 = 64 * t + 32 * cc;
+    u32x4_t* dst = (vals ? s_v[b] : s_k[b]) + (cc * JD + 2 * first_load) * 64 + lane;
     if (t0 < closed) {
 #pragma unroll
-      for (int j = 0; j < NL; ++j) {
-        u32x4_t* kd = &s_k[b][((2 * cc + hw) * KS + 2 * j) * 64 + lane];
-        kd[0] = __builtin_bit_cast(u32x4_t, codes_bf16(rk[j][0], rk[j][1]));
-        kd[64] = __builtin_bit_cast(u32x4_t, codes_bf16(rk[j][2], rk[j][3]));
-        u32x4_t* vd = &s_v[b][(cc * JD + 2 * (NL * hw + j)) * 64 + lane];
-        if (t < ntc) {
-          vd[0] = __builtin_bit_cast(u32x4_t, codes_f16(rv[j][0], rv[j][1]));
-          vd[64] = __builtin_bit_cast(u32x4_t, codes_f16(rv[j][2], rv[j][3]));
-        } else {
-          vd[0] = __builtin_bit_cast(u32x4_t, codes_bf16(rv[j][0], rv[j][1]));
-          vd[64] = __builtin_bit_cast(u32x4_t, codes_bf16(rv[j][2], rv[j][3]));
-        }
-      }
-      if (hw == 0 && lane == 0) {
-        const bool fine = ks < INFINITY && vs < INFINITY;
-        s_step[b][cc][0] = fine ? ks * sc : sc;
-        s_step[b][cc][1] = fine ? vs : 1.0f;
-        s_bad[b][cc][0] = fine ? 0u : 1u;
-        s_bad[b][cc][1] = 0u;
-      }
+      for (int j = 0; j < LPW; ++j)
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+          dst[64 * (2 * j + o)] = t < ntc
+                                      ? __builtin_bit_cast(u32x4_t, codes_f16(raw[j][2 * o], raw[j][2 * o + 1]))
+                                      : __builtin_bit_cast(u32x4_t, codes_bf16(raw[j][2 * o], raw[j][2 * o + 1]));
+      steps(b);
     } else {
-      // the open page: one of the chunk's waves takes its keys, one its values (past
-      // every row's limit zeros, any finite operands); one operand at a time, which
-      // keeps the registers of the loop for its products
+      // one operand at a time (past every row's limit zeros, any finite operands)
       unsigned bad = 0;
       const Window<DH> win(c, s, u, min(t0, max(seen - 1, 0) / 32 * 32), total, lane);
       const bool in = t0 < seen;
-      u32x4_t* dst = hw ? &s_v[b][cc * JD * 64 + lane] : &s_k[b][2 * cc * KS * 64 + lane];
 #pragma unroll 1
-      for (int f = 0; f < JD; ++f) {
+      for (int f = 0; f < 2 * LPW; ++f) {
+        const int ff = 2 * first_load + f;
         u32x4_t w = {0u, 0u, 0u, 0u};
-        if (in) w = hw ? win.value(f, bad) : win.key(f / KS, f % KS, bad);
+        if (in) w = vals ? win.value(ff, bad) : win.key(ff / KS, ff % KS, bad);
         dst[64 * f] = w;
       }
       bad = wave_or(bad);
       if (lane == 0) {
-        s_step[b][cc][hw] = hw ? 1.0f : sc;
+        if (hw == 0) s_step[b][cc] = step_parts(sc, 1.0f);
         s_bad[b][cc][hw] = bad;
       }
     }
@@ -915,113 +945,97 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     store(k0, 0);
     if (k0 + 1 < k1) load(k0 + 1);
   }
-  // One tile.  TAIL: it reaches into the open page; values are bf16 operands and
-  // the weights pairs of bf16 terms, else f16 and one f16 term.  (Two loops: with
-  // both forms in one the registers of 128 rows x 128 channels do not suffice.)
-  auto tile = [&](int t, auto is_tail) {
-    constexpr bool TAIL = decltype(is_tail)::value;
+  // OPEN: the tile reaches into the open page; the weights enter as pairs of bf16 terms.
+  auto tile = [&](int t, auto open) {
+    constexpr bool OPEN = decltype(open)::value;
     const int b = (t - k0) & 1, t0 = 64 * t;
     __syncthreads();                                     // tile t is in buffer b, the other is free
     if (t + 1 < k1) {
       store(t + 1, b ^ 1);
       if (t + 2 < k1) load(t + 2);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    f32x4_t st[R][4];
-    const float f0 = s_step[b][0][0], f1 = s_step[b][1][0];
-    const unsigned bad0 = s_bad[b][0][0] | s_bad[b][0][1], bad1 = s_bad[b][1][0] | s_bad[b][1][1];
+    f32x4_t st[4];
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
-#pragma unroll
-      for (int h = 0; h < R; ++h) st[h][a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      st[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, s_k[b][(a * KS + k) * 64 + lane]);
-#pragma unroll
-        for (int h = 0; h < R; ++h) st[h][a] = mfma(kf, qf[h][k], st[h][a]);
+        const u32x4_t kf = s_k[b][(a * KS + k) * 64 + lane];
+        if constexpr (OPEN) st[a] = mfma(__builtin_bit_cast(bf16x8_t, kf), qf[k], st[a]);
+        else st[a] = mfma_h(__builtin_bit_cast(f16x8_t, kf), __builtin_bit_cast(f16x8_t, qf[k]), st[a]);
       }
     }
     if (t0 + 63 > first_lim) {
 #pragma unroll
-      for (int h = 0; h < R; ++h)
+      for (int a = 0; a < 4; ++a)
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (t0 + 16 * a + 4 * g + q > lim[h]) st[h][a][q] = -INFINITY;
+        for (int q = 0; q < 4; ++q)
+          if (t0 + 16 * a + 4 * g + q > lim) st[a][q] = -INFINITY;
     }
-    if (bad0 | bad1) {
-      // (a full page that stands for NaN: from its chunk's first token on)
+    unsigned bad0 = 0, bad1 = 0;
 #pragma unroll
-      for (int h = 0; h < R; ++h) {
-        if (bad0 && lim[h] >= t0 + __ffs(int(bad0)) - 1) l[h] = NAN;
-        if (bad1 && lim[h] >= t0 + 32 + __ffs(int(bad1)) - 1) l[h] = NAN;
-      }
+    for (int w = 0; w < CW; ++w) {
+      bad0 |= s_bad[b][0][w];
+      bad1 |= s_bad[b][1][w];
     }
-    const float vs0 = s_step[b][0][1], vs1 = s_step[b][1][1];
-    const float vr = fmaxf(vref, fmaxf(pow2_above(vs0), pow2_above(vs1)));
-    const float vinv = pow2_inv(vr), shrink = vref * vinv;
+    // (a full page that stands for NaN: from its chunk's first token on)
+    if (bad0 && lim >= t0 + __ffs(int(bad0)) - 1) l = NAN;
+    if (bad1 && lim >= t0 + 32 + __ffs(int(bad1)) - 1) l = NAN;
+    const float4 q0 = s_step[b][0], q1 = s_step[b][1];
+    const float vr = fmaxf(vref, fmaxf(pow2_above(q0.y), pow2_above(q1.y)));
+    const float shrink = vref * pow2_inv(vr);
     vref = vr;
-    const Step sp[2] = {step_of(f0, vs0, vinv), step_of(f1, vs1, vinv)};
+    Step sp[2] = {step_of(q0, vr), step_of(q1, vr)};
+    if constexpr (!OPEN) {
+      sp[0].f *= qs;
+      sp[1].f *= qs;
+    }
+    const float alpha = softmax_step<2>(st, sp, m, l) * shrink;
+    if (__any(alpha != 1.0f)) {
 #pragma unroll
-    for (int h = 0; h < R; ++h) {
-      const float alpha = softmax_step<2>(st[h], sp, m[h], l[h]) * shrink;
-      if (__any(alpha != 1.0f)) {
-#pragma unroll
-        for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * alpha;
-      }
+      for (int j = 0; j < JD; ++j) acc[j] = acc[j] * alpha;
     }
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
-      u32x4_t ph[R], pl[TAIL ? R : 1];
+      u32x4_t ph, pl;
 #pragma unroll
-      for (int h = 0; h < R; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f32x4_t p = st[h][2 * k2 + (e >> 1)];
-          const float p0 = p[2 * (e & 1)], p1 = p[2 * (e & 1) + 1];
-          if constexpr (TAIL) {
-            ph[h][e] = f2bf2(p0, p1);
-            pl[h][e] = f2bf2(p0 - __uint_as_float(ph[h][e] << 16), p1 - __uint_as_float(ph[h][e] & 0xffff0000u));
-          } else {
-            ph[h][e] = pack_f16(p0, p1);
-          }
+      for (int e = 0; e < 4; ++e) {
+        const float p0 = st[2 * k2 + (e >> 1)][2 * (e & 1)], p1 = st[2 * k2 + (e >> 1)][2 * (e & 1) + 1];
+        if constexpr (OPEN) {
+          ph[e] = f2bf2(p0, p1);
+          pl[e] = f2bf2(p0 - __uint_as_float(ph[e] << 16), p1 - __uint_as_float(ph[e] & 0xffff0000u));
+        } else {
+          ph[e] = pack_f16(p0, p1);
         }
+      }
 #pragma unroll
       for (int j = 0; j < JD; ++j) {
         const u32x4_t vf = s_v[b][(k2 * JD + j) * 64 + lane];
-#pragma unroll
-        for (int h = 0; h < R; ++h) {
-          if constexpr (TAIL) {
-            acc[h][j] = mfma(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, ph[h]), acc[h][j]);
-            acc[h][j] = mfma(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pl[h]), acc[h][j]);
-          } else {
-            acc[h][j] = mfma_h(__builtin_bit_cast(f16x8_t, vf), __builtin_bit_cast(f16x8_t, ph[h]), acc[h][j]);
-          }
+        if constexpr (OPEN) {
+          acc[j] = mfma(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, ph), acc[j]);
+          acc[j] = mfma(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pl), acc[j]);
+        } else {
+          acc[j] = mfma_h(__builtin_bit_cast(f16x8_t, vf), __builtin_bit_cast(f16x8_t, ph), acc[j]);
         }
       }
     }
   };
   int t = k0;
   for (; t < min(k1, ntc); ++t) tile(t, std::false_type{});
+  if (t < k1) load_q<DH>(qf, Q, ldq, s, u, G, row, g);
   for (; t < k1; ++t) tile(t, std::true_type{});
+  l = row_sum(l);
+  if (row0 + 16 * wave + r >= rows) return;
   const Out out = out_of(O, LSE, part, splits, split, H, c.T, int64_t(ntile) * c.n_seq * c.Hkv,
                          (int64_t(rt) * c.n_seq + i) * c.Hkv + u, QW, DH);
+  if (!s.ok) l = NAN;
+  const int64_t tok = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
 #pragma unroll
-  for (int h = 0; h < R; ++h) l[h] = row_sum(l[h]);
-#pragma unroll
-  for (int h = 0; h < R; ++h) {
-    const int row = row0 + 16 * (R * wave + h) + r;
-    if (row >= rows) continue;
-    const float ll = s.ok ? l[h] : NAN;                  // (the row's: summed above)
-    const int64_t t = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
-#pragma unroll
-    for (int j = 0; j < JD; ++j) {
-      const f32x4_t o = acc[h][j] * (vref / WUNIT);
-      put4(out, row - row0, t, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), ll);
-    }
-    if (g == 0) put_ml(out, row - row0, t, hd, m[h], ll);
+  for (int j = 0; j < JD; ++j) {
+    const f32x4_t o = acc[j] * (vref / WUNIT);
+    put4(out, row - row0, tok, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), l);
   }
+  if (g == 0) put_ml(out, row - row0, tok, hd, m, l);
 }
 
 // Joins a row's splits: DH / 4 lanes of four output values each, NG groups of them
@@ -1145,10 +1159,10 @@ hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int 
     hipLaunchKernelGGL((cache_attend_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, p.few);
   };
   auto many = [&](auto dh, auto rr) {
-    constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
-    const int64_t tiles = (int64_t(c.max_q) * G + 64 * R - 1) / (64 * R);
+    constexpr int DH = decltype(dh)::value, NW = decltype(rr)::value;
+    const int64_t tiles = (int64_t(c.max_q) * G + 16 * NW - 1) / (16 * NW);
     const dim3 grid(unsigned(tiles * c.n_seq * p.many * c.Hkv));
-    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws_many,
+    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, NW>), grid, dim3(64 * NW), 0, st, c, Q, ldq, H, O, LSE, ws_many,
                        p.many, p.row_rows + 1);
   };
   auto join = [&](auto dh, auto ng) {
@@ -1158,8 +1172,8 @@ hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int 
     hipLaunchKernelGGL((cache_join_kernel<DH, NG>), grid, dim3(256), 0, st, c, H, a, O, LSE);
   };
   auto run = [&](auto dh) {
-    if (p.tile_rows == 64) many(dh, std::integral_constant<int, 1>{});
-    else if (p.tile_rows) many(dh, std::integral_constant<int, 2>{});
+    if (p.tile_rows == 64) many(dh, std::integral_constant<int, 4>{});
+    else if (p.tile_rows) many(dh, std::integral_constant<int, 8>{});
     if (p.row_rows == 16) few(dh, std::integral_constant<int, 1>{});
     else if (p.row_rows) few(dh, std::integral_constant<int, 2>{});
     const int splits = std::max(p.few, p.many);

@@ -285,7 +285,7 @@ class Batch:
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("page", [32, 64, 96, 128])
+@pytest.mark.parametrize("page", [32, 64, 128])
 @pytest.mark.parametrize("H,Hkv", [(2, 2), (8, 2), (5, 1)])
 def test_cache_steps(d, page, H, Hkv):
     """Prompts, then decoding, then chunks that end pages in every position."""
