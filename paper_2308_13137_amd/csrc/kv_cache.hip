@@ -57,10 +57,8 @@ OQ_DEV Seq seq_of(const CacheArgs& c, int i) {
   if (int64_t(s.L) + s.n > int64_t(c.max_pages) * c.P) s.ok = false;
   return s;
 }
-OQ_DEV int page_of(const CacheArgs& c, int i, int pg) {
-  const int p = c.table[int64_t(i) * c.max_pages + pg];
-  return p >= 0 && p < c.n_pages ? p : -1;
-}
+OQ_DEV int page_in(const CacheArgs& c, int p) { return p >= 0 && p < c.n_pages ? p : -1; }
+OQ_DEV int page_of(const CacheArgs& c, int i, int pg) { return page_in(c, c.table[int64_t(i) * c.max_pages + pg]); }
 
 // ------------------------------------------------------------------ append
 constexpr int AT = 256;
@@ -439,7 +437,9 @@ template <int DH>
 struct Codes {
   u32x4_t k[DH / 32], v[DH / 32];
   float ks, vs;
-  OQ_DEV void load(const CacheArgs& c, int id, int u, int tin, int lane) {
+  // (entry: the table's, checked here: at its load the check would wait for memory)
+  OQ_DEV void load(const CacheArgs& c, int entry, int u, int tin, int lane) {
+    const int id = page_in(c, entry);
     const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
     ks = id < 0 ? NAN : c.ks[blk];
     vs = id < 0 ? NAN : c.vs[blk];
@@ -531,40 +531,37 @@ OQ_DEV Step step_of(float4 q, float vr) {
 // A row's running softmax: m, the maximum of its logits in base 2 rounded up to an
 // integer (so it seldom moves), and l, this lane's share of the sum of its
 // weights 2^(t - m).  A lane holds the row's scores of NC chunks of 32 tokens (two
-// 16-token tiles each), masked ones -inf.  softmax_max takes the new maximum in
-// and returns the factor of the row's numerators; weight() turns a score into
-// its weight times its chunk's factor, which the sum takes out again.
+// 16-token tiles each), masked ones -inf; they become the weights times their
+// chunk's factor, which the sum takes out again.  Returns the factor that the
+// row's numerators need.
 template <int NC>
-OQ_DEV float softmax_max(const f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m, float& l, float& off) {
+OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m, float& l) {
+  // (scaled first: a maximum of values straight from the matrix unit costs two
+  // instructions for each, to quiet a NaN)
   float mt = -INFINITY;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
+#pragma unroll
+    for (int a = 2 * c; a < 2 * c + 2; ++a)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) st[a][q] = st[a][q] * sp[c].f;
     const f32x4_t x = st[2 * c], y = st[2 * c + 1];
-    const float a = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), b = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
-    mt = fmaxf(mt, fmaxf(a, b) * sp[c].f);
+    mt = fmaxf(mt, fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))));
   }
   const float mn = fmaxf(m, ceilf(row_max(mt)));
-  off = mn == -INFINITY ? 0.0f : mn;                     // no token seen yet: weights 2^-inf = 0
+  const float off = mn == -INFINITY ? 0.0f : mn;         // no token seen yet: weights 2^-inf = 0
   const float alpha = mn == m ? 1.0f : m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
   l *= alpha;
   m = mn;
-  return alpha;
-}
-OQ_DEV float weight(float score, const Step& sp, float off) {
-  return __builtin_amdgcn_exp2f(__builtin_fmaf(score, sp.f, sp.lw - off));
-}
-template <int NC>
-OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m, float& l) {
-  float off;
-  const float alpha = softmax_max<NC>(st, sp, m, l, off);
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
+    const float e = sp[c].lw - off;
     float w = 0.0f;
 #pragma unroll
     for (int a = 2 * c; a < 2 * c + 2; ++a)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        st[a][q] = weight(st[a][q], sp[c], off);
+        st[a][q] = __builtin_amdgcn_exp2f(st[a][q] + e);
         w += st[a][q];
       }
     l = __builtin_fmaf(w, sp[c].winv, l);
@@ -651,7 +648,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
   }
   const int nch = (total + 31) / 32, ncode = (total >> c.lgP) * (P / 32), per = (nch + splits - 1) / splits;
   const int c0 = split * per + wave, c1 = min(nch, (split + 1) * per), c1c = min(c1, ncode);
-  auto id_of = [&](int ch) { return ch < c1c ? page_of(c, i, (32 * ch) >> c.lgP) : -1; };
+  auto id_of = [&](int ch) { return ch < c1c ? c.table[int64_t(i) * c.max_pages + ((32 * ch) >> c.lgP)] : -1; };
   auto scores = [&](int h, const bf16x8_t (&kf)[2][KS], int t0, f32x4_t (&st)[2]) {
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
@@ -796,27 +793,25 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs c, const
   }
 }
 
-// Many rows (prompts): one workgroup of NW waves takes 16 NW rows of one key head
-// over tiles of 64 tokens.  The waves turn a tile's codes into f16 operands once, in
-// LDS, a tile ahead; the raw codes of the one after are in flight meanwhile.  16
-// rows a wave keep the kernel within 128 registers, four waves to a SIMD: the
-// matrix instructions, the softmax and the conversions of different waves run
-// beside each other (32 rows a wave and two waves to a SIMD, with the same work
-// interleaved by hand, took 303 us where this takes TIME_PROMPT).
+// Many rows (prompts): one workgroup of four waves takes 64 R rows of one key head,
+// 16 R per wave, over tiles of 64 tokens.  The waves turn a tile's codes into f16
+// operands once, in LDS, a tile ahead; the raw codes of the one after are in
+// flight meanwhile.  Bound by the vector units (softmax, conversion) beside the
+// matrix instructions, two workgroups to a compute unit.
 //
 // Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
 // 2^-39 of that entry.
-template <int DH, int NW>
-__global__ __launch_bounds__(64 * NW, 4) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
+template <int DH, int R>
+__global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
                                                                        int64_t ldq, int H,
                                                                        uint16_t* __restrict__ O,
                                                                        float* __restrict__ LSE,
                                                                        float* __restrict__ part, int splits,
                                                                        int rows_min) {
-  constexpr int KS = DH / 32, JD = DH / 16, QW = 16 * NW;
+  constexpr int KS = DH / 32, JD = DH / 16, QW = 64 * R;
   constexpr int TILE = 64 * DH / 8;                      // 16-byte pieces of one operand's tile
-  constexpr int CW = NW / 2, LPW = JD / CW;              // waves of a chunk, loads of a wave
+  constexpr int CW = 2, LPW = JD / CW;                   // waves of a chunk, loads of a wave
   __shared__ u32x4_t s_k[2][TILE], s_v[2][TILE];
   __shared__ float4 s_step[2][2];                        // [buffer][chunk], step_parts
   __shared__ unsigned s_bad[2][2][CW];
@@ -837,41 +832,44 @@ __global__ __launch_bounds__(64 * NW, 4) void cache_attend_tile_kernel(CacheArgs
   const int total = s.ok ? s.L + s.n : 0, closed = total & ~(P - 1);
   const float sc = 1.4426950408889634f / sqrtf(float(DH));
 
-  const int row = min(row0 + 16 * wave + r, rows - 1), lim = s.L + row / G;   // lim: the last token the row sees
-  bf16x8_t qf[KS];                                       // f16 (times 1 / qs), bf16 for the open page
-  float qs;
-  load_q<DH>(qf, Q, ldq, s, u, G, row, g);
-  {
+  bf16x8_t qf[R][KS];                                    // f16 (times 1 / qs), bf16 for the open page
+  float qs[R];
+  int lim[R];                                            // the last token this lane's row sees
+  f32x4_t acc[R][JD];
+  float m[R], l[R], vref = VREF0;
+  auto row_of = [&](int h) { return min(row0 + 16 * (R * wave + h) + r, rows - 1); };
+#pragma unroll
+  for (int h = 0; h < R; ++h) {
+    lim[h] = s.L + row_of(h) / G;
+    load_q<DH>(qf[h], Q, ldq, s, u, G, row_of(h), g);
     float top = 0.0f;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(float(qf[k][e])));
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(float(qf[h][k][e])));
     const int e = min(max(int(__float_as_uint(row_max(top)) >> 23), 20), 253);
-    const float up = __uint_as_float(uint32_t(254 + 14 - e) << 23 & 0x7f800000u);
-    qs = __uint_as_float(uint32_t(e - 14) << 23);        // 2^(exponent - 14)
+    const float up = __uint_as_float(uint32_t(268 - e) << 23);   // 2^(14 - exponent)
+    qs[h] = __uint_as_float(uint32_t(e - 14) << 23);
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       u32x4_t w;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) w[q] = pack_f16(float(qf[k][2 * q]) * up, float(qf[k][2 * q + 1]) * up);
-      qf[k] = __builtin_bit_cast(bf16x8_t, w);
+      for (int q = 0; q < 4; ++q) w[q] = pack_f16(float(qf[h][k][2 * q]) * up, float(qf[h][k][2 * q + 1]) * up);
+      qf[h][k] = __builtin_bit_cast(bf16x8_t, w);
     }
-  }
-  f32x4_t acc[JD];
-  float m = -INFINITY, l = 0.0f, vref = VREF0;
+    m[h] = -INFINITY;
+    l[h] = 0.0f;
 #pragma unroll
-  for (int j = 0; j < JD; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < JD; ++j) acc[h][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
   const int first_lim = s.L + row0 / G;                  // what every row of the tile sees
   const int seen = s.ok ? s.L + min(row0 + QW - 1, rows - 1) / G + 1 : 0;
   const int nt = (seen + 63) / 64, per = (nt + splits - 1) / splits;
   const int k0 = split * per, k1 = min(nt, (split + 1) * per);
   const int ntc = closed / 64;                           // tiles of full pages only
-  // this wave's share of a tile: loads LPW hw .. of chunk cc, the first half of a
-  // chunk's waves of its keys, the others of its values
-  const int cc = wave / CW, hw = wave % CW;
-  const bool vals = hw >= CW / 2;
-  const int first_load = LPW * (vals ? hw - CW / 2 : hw);
+  // this wave's share of a tile: the keys or the values of chunk cc
+  const int cc = wave >> 1, hw = wave & 1;
+  const bool vals = hw != 0;
   u32x4_t raw[LPW];
   float ks = 0.0f, vs = 0.0f;
   // The page of this wave's chunk of tile t (a page number is a load of its own: it
@@ -881,19 +879,20 @@ __global__ __launch_bounds__(64 * NW, 4) void cache_attend_tile_kernel(CacheArgs
   int zero = 0;
   asm("" : "+v"(zero));
   auto id_of = [&](int t) {
-    return t < k1 && 64 * t + 32 * cc < closed ? page_of(c, i, ((64 * t + 32 * cc) >> c.lgP) + zero) : -1;
+    return t < k1 && 64 * t + 32 * cc < closed
+               ? c.table[int64_t(i) * c.max_pages + ((64 * t + 32 * cc) >> c.lgP) + zero]
+               : -1;
   };
   int idn = id_of(k0);
   auto load = [&](int t) {                               // tile t, if its chunk is in a full page
-    const int t0 = 64 * t + 32 * cc, id = __builtin_amdgcn_readfirstlane(idn);
+    const int t0 = 64 * t + 32 * cc, id = page_in(c, __builtin_amdgcn_readfirstlane(idn));
     if (t0 < closed) {
       const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
       if (hw == 0) {
         ks = id < 0 ? NAN : c.ks[blk + zero];
         vs = id < 0 ? NAN : c.vs[blk + zero];
       }
-      const u32x4_t* p = reinterpret_cast<const u32x4_t*>((vals ? c.vc : c.kc) + blk * P * DH + (t0 & (P - 1)) * DH) +
-                         64 * first_load + lane;
+      const u32x4_t* p = reinterpret_cast<const u32x4_t*>((vals ? c.vc : c.kc) + blk * P * DH + (t0 & (P - 1)) * DH) + lane;
 #pragma unroll
       for (int j = 0; j < LPW; ++j) raw[j] = p[64 * j];
       idn = id_of(t + 1);
@@ -911,15 +910,17 @@ __global__ __launch_bounds__(64 * NW, 4) void cache_attend_tile_kernel(CacheArgs
   // or bf16 where the tile reaches into the open page (from ntc on).
   auto store = [&](int t, int b) {
     const int t0 = 64 * t + 32 * cc;
-    u32x4_t* dst = (vals ? s_v[b] : s_k[b]) + (cc * JD + 2 * first_load) * 64 + lane;
+    u32x4_t* dst = (vals ? s_v[b] : s_k[b]) + cc * JD * 64 + lane;
     if (t0 < closed) {
+      if (t < ntc) {
 #pragma unroll
-      for (int j = 0; j < LPW; ++j)
+        for (int j = 0; j < 2 * LPW; ++j)
+          dst[64 * j] = __builtin_bit_cast(u32x4_t, codes_f16(raw[j / 2][2 * (j & 1)], raw[j / 2][2 * (j & 1) + 1]));
+      } else {
 #pragma unroll
-        for (int o = 0; o < 2; ++o)
-          dst[64 * (2 * j + o)] = t < ntc
-                                      ? __builtin_bit_cast(u32x4_t, codes_f16(raw[j][2 * o], raw[j][2 * o + 1]))
-                                      : __builtin_bit_cast(u32x4_t, codes_bf16(raw[j][2 * o], raw[j][2 * o + 1]));
+        for (int j = 0; j < 2 * LPW; ++j)
+          dst[64 * j] = __builtin_bit_cast(u32x4_t, codes_bf16(raw[j / 2][2 * (j & 1)], raw[j / 2][2 * (j & 1) + 1]));
+      }
       steps(b);
     } else {
       // one operand at a time (past every row's limit zeros, any finite operands)
@@ -928,9 +929,8 @@ __global__ __launch_bounds__(64 * NW, 4) void cache_attend_tile_kernel(CacheArgs
       const bool in = t0 < seen;
 #pragma unroll 1
       for (int f = 0; f < 2 * LPW; ++f) {
-        const int ff = 2 * first_load + f;
         u32x4_t w = {0u, 0u, 0u, 0u};
-        if (in) w = vals ? win.value(ff, bad) : win.key(ff / KS, ff % KS, bad);
+        if (in) w = vals ? win.value(f, bad) : win.key(f / KS, f % KS, bad);
         dst[64 * f] = w;
       }
       bad = wave_or(bad);
@@ -950,27 +950,38 @@ __global__ __launch_bounds__(64 * NW, 4) void cache_attend_tile_kernel(CacheArgs
     constexpr bool OPEN = decltype(open)::value;
     const int b = (t - k0) & 1, t0 = 64 * t;
     __syncthreads();                                     // tile t is in buffer b, the other is free
+    // operands are read from LDS AH ahead of their products
+    constexpr int AH = 4;
+    const u32x4_t *sk = &s_k[b][lane], *sv = &s_v[b][lane];
+    u32x4_t kf[AH];
+#pragma unroll
+    for (int x = 0; x < AH; ++x) kf[x] = sk[64 * x];
     if (t + 1 < k1) {
       store(t + 1, b ^ 1);
       if (t + 2 < k1) load(t + 2);
     }
-    f32x4_t st[4];
+    f32x4_t st[R][4];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
-      st[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < 4 * KS; ++x) {
+      const int a = x / KS, k = x % KS;
+      const u32x4_t f = kf[x % AH];
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const u32x4_t kf = s_k[b][(a * KS + k) * 64 + lane];
-        if constexpr (OPEN) st[a] = mfma(__builtin_bit_cast(bf16x8_t, kf), qf[k], st[a]);
-        else st[a] = mfma_h(__builtin_bit_cast(f16x8_t, kf), __builtin_bit_cast(f16x8_t, qf[k]), st[a]);
+      for (int h = 0; h < R; ++h) {
+        if (k == 0) st[h][a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if constexpr (OPEN) st[h][a] = mfma(__builtin_bit_cast(bf16x8_t, f), qf[h][k], st[h][a]);
+        else st[h][a] = mfma_h(__builtin_bit_cast(f16x8_t, f), __builtin_bit_cast(f16x8_t, qf[h][k]), st[h][a]);
       }
+      if (x + AH < 4 * KS) kf[x % AH] = sk[64 * (x + AH)];
+      __builtin_amdgcn_sched_barrier(0);
     }
     if (t0 + 63 > first_lim) {
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
+      for (int h = 0; h < R; ++h)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (t0 + 16 * a + 4 * g + q > lim) st[a][q] = -INFINITY;
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (t0 + 16 * a + 4 * g + q > lim[h]) st[h][a][q] = -INFINITY;
     }
     unsigned bad0 = 0, bad1 = 0;
 #pragma unroll
@@ -978,64 +989,91 @@ __global__ __launch_bounds__(64 * NW, 4) void cache_attend_tile_kernel(CacheArgs
       bad0 |= s_bad[b][0][w];
       bad1 |= s_bad[b][1][w];
     }
-    // (a full page that stands for NaN: from its chunk's first token on)
-    if (bad0 && lim >= t0 + __ffs(int(bad0)) - 1) l = NAN;
-    if (bad1 && lim >= t0 + 32 + __ffs(int(bad1)) - 1) l = NAN;
+    if (bad0 | bad1) {
+      // (a full page that stands for NaN: from its chunk's first token on)
+#pragma unroll
+      for (int h = 0; h < R; ++h) {
+        if (bad0 && lim[h] >= t0 + __ffs(int(bad0)) - 1) l[h] = NAN;
+        if (bad1 && lim[h] >= t0 + 32 + __ffs(int(bad1)) - 1) l[h] = NAN;
+      }
+    }
     const float4 q0 = s_step[b][0], q1 = s_step[b][1];
     const float vr = fmaxf(vref, fmaxf(pow2_above(q0.y), pow2_above(q1.y)));
     const float shrink = vref * pow2_inv(vr);
     vref = vr;
-    Step sp[2] = {step_of(q0, vr), step_of(q1, vr)};
-    if constexpr (!OPEN) {
-      sp[0].f *= qs;
-      sp[1].f *= qs;
-    }
-    const float alpha = softmax_step<2>(st, sp, m, l) * shrink;
-    if (__any(alpha != 1.0f)) {
+    const Step s0 = step_of(q0, vr), s1 = step_of(q1, vr);
+    u32x4_t vf[AH];
 #pragma unroll
-      for (int j = 0; j < JD; ++j) acc[j] = acc[j] * alpha;
+    for (int x = 0; x < AH; ++x) vf[x] = sv[64 * x];
+#pragma unroll
+    for (int h = 0; h < R; ++h) {
+      Step sp[2] = {s0, s1};
+      if constexpr (!OPEN) {
+        sp[0].f *= qs[h];
+        sp[1].f *= qs[h];
+      }
+      const float alpha = softmax_step<2>(st[h], sp, m[h], l[h]) * shrink;
+      if (__any(alpha != 1.0f)) {
+#pragma unroll
+        for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * alpha;
+      }
     }
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
-      u32x4_t ph, pl;
+      u32x4_t ph[R], pl[OPEN ? R : 1];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p0 = st[2 * k2 + (e >> 1)][2 * (e & 1)], p1 = st[2 * k2 + (e >> 1)][2 * (e & 1) + 1];
-        if constexpr (OPEN) {
-          ph[e] = f2bf2(p0, p1);
-          pl[e] = f2bf2(p0 - __uint_as_float(ph[e] << 16), p1 - __uint_as_float(ph[e] & 0xffff0000u));
-        } else {
-          ph[e] = pack_f16(p0, p1);
+      for (int h = 0; h < R; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = st[h][2 * k2 + (e >> 1)][2 * (e & 1)], p1 = st[h][2 * k2 + (e >> 1)][2 * (e & 1) + 1];
+          if constexpr (OPEN) {
+            ph[h][e] = f2bf2(p0, p1);
+            pl[h][e] = f2bf2(p0 - __uint_as_float(ph[h][e] << 16), p1 - __uint_as_float(ph[h][e] & 0xffff0000u));
+          } else {
+            ph[h][e] = pack_f16(p0, p1);
+          }
         }
-      }
 #pragma unroll
       for (int j = 0; j < JD; ++j) {
-        const u32x4_t vf = s_v[b][(k2 * JD + j) * 64 + lane];
-        if constexpr (OPEN) {
-          acc[j] = mfma(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, ph), acc[j]);
-          acc[j] = mfma(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pl), acc[j]);
-        } else {
-          acc[j] = mfma_h(__builtin_bit_cast(f16x8_t, vf), __builtin_bit_cast(f16x8_t, ph), acc[j]);
+        const int x = k2 * JD + j;
+        const u32x4_t v = vf[x % AH];
+#pragma unroll
+        for (int h = 0; h < R; ++h) {
+          if constexpr (OPEN) {
+            acc[h][j] = mfma(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, ph[h]), acc[h][j]);
+            acc[h][j] = mfma(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, pl[h]), acc[h][j]);
+          } else {
+            acc[h][j] = mfma_h(__builtin_bit_cast(f16x8_t, v), __builtin_bit_cast(f16x8_t, ph[h]), acc[h][j]);
+          }
         }
+        if (x + AH < 2 * JD) vf[x % AH] = sv[64 * (x + AH)];
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
   int t = k0;
   for (; t < min(k1, ntc); ++t) tile(t, std::false_type{});
-  if (t < k1) load_q<DH>(qf, Q, ldq, s, u, G, row, g);
+  if (t < k1) {
+#pragma unroll
+    for (int h = 0; h < R; ++h) load_q<DH>(qf[h], Q, ldq, s, u, G, row_of(h), g);
+  }
   for (; t < k1; ++t) tile(t, std::true_type{});
-  l = row_sum(l);
-  if (row0 + 16 * wave + r >= rows) return;
   const Out out = out_of(O, LSE, part, splits, split, H, c.T, int64_t(ntile) * c.n_seq * c.Hkv,
                          (int64_t(rt) * c.n_seq + i) * c.Hkv + u, QW, DH);
-  if (!s.ok) l = NAN;
-  const int64_t tok = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
 #pragma unroll
-  for (int j = 0; j < JD; ++j) {
-    const f32x4_t o = acc[j] * (vref / WUNIT);
-    put4(out, row - row0, tok, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), l);
+  for (int h = 0; h < R; ++h) {
+    l[h] = row_sum(l[h]);
+    const int row = row0 + 16 * (R * wave + h) + r;
+    if (row >= rows) continue;
+    if (!s.ok) l[h] = NAN;
+    const int64_t tok = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
+#pragma unroll
+    for (int j = 0; j < JD; ++j) {
+      const f32x4_t o = acc[h][j] * (vref / WUNIT);
+      put4(out, row - row0, tok, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), l[h]);
+    }
+    if (g == 0) put_ml(out, row - row0, tok, hd, m[h], l[h]);
   }
-  if (g == 0) put_ml(out, row - row0, tok, hd, m, l);
 }
 
 // Joins a row's splits: DH / 4 lanes of four output values each, NG groups of them
@@ -1159,10 +1197,10 @@ hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int 
     hipLaunchKernelGGL((cache_attend_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, p.few);
   };
   auto many = [&](auto dh, auto rr) {
-    constexpr int DH = decltype(dh)::value, NW = decltype(rr)::value;
-    const int64_t tiles = (int64_t(c.max_q) * G + 16 * NW - 1) / (16 * NW);
+    constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
+    const int64_t tiles = (int64_t(c.max_q) * G + 64 * R - 1) / (64 * R);
     const dim3 grid(unsigned(tiles * c.n_seq * p.many * c.Hkv));
-    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, NW>), grid, dim3(64 * NW), 0, st, c, Q, ldq, H, O, LSE, ws_many,
+    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws_many,
                        p.many, p.row_rows + 1);
   };
   auto join = [&](auto dh, auto ng) {
@@ -1172,8 +1210,10 @@ hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int 
     hipLaunchKernelGGL((cache_join_kernel<DH, NG>), grid, dim3(256), 0, st, c, H, a, O, LSE);
   };
   auto run = [&](auto dh) {
-    if (p.tile_rows == 64) many(dh, std::integral_constant<int, 4>{});
-    else if (p.tile_rows) many(dh, std::integral_constant<int, 8>{});
+    const std::integral_constant<int, 1> i1{};
+    const std::integral_constant<int, 2> i2{};
+    if (p.tile_rows == 64) many(dh, i1);
+    else if (p.tile_rows) many(dh, i2);
     if (p.row_rows == 16) few(dh, std::integral_constant<int, 1>{});
     else if (p.row_rows) few(dh, std::integral_constant<int, 2>{});
     const int splits = std::max(p.few, p.many);
