@@ -2204,7 +2204,7 @@ oq_status check_cache(const oq_kv_cache* c, const oq_kv_batch* b) {
   if ((c->head_dim != 64 && c->head_dim != 128) || (c->page != 32 && c->page != 64 && c->page != 128))
     return fail(OQ_ERR_UNSUPPORTED, "head_dim=%d (need 64 or 128), page=%d (need 32, 64 or 128)", c->head_dim,
                 c->page);
-  OQ_REQ(c->n_pages > 0 && c->n_slots > 0 && c->kv_heads > 0 && c->kv_heads <= 65535,
+  OQ_REQ(c->n_pages > 0 && c->n_slots > 0 && c->kv_heads > 0 && c->kv_heads <= 32768,
          "bad cache n_pages=%d n_slots=%d kv_heads=%d", c->n_pages, c->n_slots, c->kv_heads);
   OQ_REQ(c->k_codes && c->v_codes && c->k_scale && c->v_scale && c->k_window && c->v_window,
          "every tensor of the cache is required");

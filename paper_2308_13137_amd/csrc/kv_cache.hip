@@ -61,8 +61,6 @@ OQ_DEV int page_in(const CacheArgs& c, int p) { return p >= 0 && p < c.n_pages ?
 OQ_DEV int page_of(const CacheArgs& c, int i, int pg) { return page_in(c, c.table[int64_t(i) * c.max_pages + pg]); }
 
 // ------------------------------------------------------------------ append
-constexpr int AT = 256;
-
 template <typename TI>
 struct RowIn {
   const TI *q, *k, *v;
@@ -106,31 +104,78 @@ OQ_DEV void turned4(const TI* row, const float* rope, int64_t n_rope, int pos, i
   }
 }
 
-// One workgroup: one page's worth of one sequence's new tokens, for one key head
-// and its group's query heads; a thread takes channels p .. p + 3 and p + d/2 .. of
-// a head's row at a time.  HBM-bound for prompts (each row read once, written
-// once); for decoding a few loads deep.  A page that fills up is gathered in LDS,
-// the keys as rows, the values in the window's operand order, so that its codes
-// are written in whole 16-byte pieces.
+// Channels p .. p + 3 and p + d/2 .. of one query head's row, U rows (or heads) at
+// a time so that their loads are in flight together.
 template <typename TI>
-__global__ __launch_bounds__(AT) void cache_append_kernel(CacheArgs c, RowIn<TI> in, int H,
+OQ_DEV void append_queries(const CacheArgs& c, const Seq& s, const RowIn<TI>& in, int H, const float* rope,
+                           int64_t n_rope, const float* sa, uint16_t* Qout, int lo, int hi, int slice, int slices) {
+  constexpr int U = 4;
+  const int d = c.d, half = d / 2, q4 = half / 4, G = H / c.Hkv, per = H * q4;
+  const int64_t items = int64_t(hi - lo) * per, step = int64_t(slices) * blockDim.x;
+  for (int64_t e0 = int64_t(slice) * blockDim.x + threadIdx.x; e0 < items; e0 += U * step) {
+    float x[U][4], y[U][4];
+    int64_t at[U];
+    int sc[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int64_t e = min(e0 + k * step, items - 1);     // (past the end: the last one, not stored)
+      const int row = int(e / per), hh = int(e % per) / q4, p = 4 * int(e % q4), pos = lo + row;
+      const int64_t t = int64_t(s.b) + (pos - s.L);
+      turned4(in.q + t * in.ldq + int64_t(hh) * d, rope, n_rope, pos, p, half, x[k], y[k]);
+      at[k] = (t * H + hh) * d + p;
+      sc[k] = (hh / G) * d + p;
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (e0 + k * step >= items) break;
+      if (sa) {
+        float s0[4], s1[4];
+        load4(sa + sc[k], s0);
+        load4(sa + sc[k] + half, s1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[k][i] = x[k][i] / s0[i];
+          y[k][i] = y[k][i] / s1[i];
+        }
+      }
+      *reinterpret_cast<uint2*>(Qout + at[k]) = pack4(x[k]);
+      *reinterpret_cast<uint2*>(Qout + at[k] + half) = pack4(y[k]);
+    }
+  }
+}
+
+// One workgroup takes one page's worth of one sequence's new tokens: the keys and
+// values of one head (blockIdx.y < kv heads), or a slice of the queries.  A thread
+// takes channels p .. p + 3 and p + d/2 .. of a head's row at a time.  HBM-bound for
+// prompts (each row read once, written once); for decoding a few loads deep.  A
+// page that fills up is gathered in LDS, the keys as rows, the values in the
+// window's operand order, so that its codes are written in whole 16-byte pieces.
+template <typename TI>
+__global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI> in, int H,
                                                           const float* __restrict__ rope, int64_t n_rope,
                                                           const float* __restrict__ sa,
                                                           uint16_t* __restrict__ Qout) {
   extern __shared__ uint4 s_page[];                        // K [P][d], then V in operand order, bf16
-  __shared__ int s_max[2][AT / 64];
-  const int u = blockIdx.y, i = blockIdx.z, tid = threadIdx.x;
-  const int d = c.d, half = d / 2, P = c.P, G = H / c.Hkv;
+  __shared__ int s_max[2][8];
+  const int u = blockIdx.y, i = blockIdx.z, tid = threadIdx.x, AT = blockDim.x;
+  const int d = c.d, half = d / 2, P = c.P;
   const Seq s = seq_of(c, i);
   if (s.n == 0) return;
+  const int slice = u - c.Hkv, slices = int(gridDim.y) - c.Hkv;
   if (!s.ok) {                                             // nothing is cached; the queries are NaN
-    for (int64_t e = tid + int64_t(AT) * blockIdx.x; e < int64_t(s.n) * G * d; e += int64_t(AT) * gridDim.x)
-      Qout[(int64_t(s.b) + e / (G * d)) * H * d + int64_t(u) * G * d + e % (G * d)] = 0x7fc0;
+    if (slice < 0) return;
+    const int64_t n = int64_t(s.n) * H * d, step = int64_t(AT) * gridDim.x * slices;
+    for (int64_t e = tid + int64_t(AT) * (blockIdx.x + int64_t(gridDim.x) * slice); e < n; e += step)
+      Qout[int64_t(s.b) * H * d + e] = 0x7fc0;
     return;
   }
   const int pg0 = s.L / P, pg = pg0 + int(blockIdx.x), end = s.L + s.n;
   const int lo = max(s.L, pg * P), hi = min(end, (pg + 1) * P);
   if (lo >= hi) return;
+  if (slice >= 0) {
+    append_queries(c, s, in, H, rope, n_rope, sa, Qout, lo, hi, slice, slices);
+    return;
+  }
   const int last = (end - 1) / P;
   const int64_t win = int64_t(P) * d;
   auto window = [&](uint16_t* w, int page) { return w + ((int64_t(s.slot) * 2 + (page & 1)) * c.Hkv + u) * win; };
@@ -189,36 +234,15 @@ __global__ __launch_bounds__(AT) void cache_append_kernel(CacheArgs c, RowIn<TI>
     load4(row + p + half, x);
     b = pack4(x);
   };
-  // this page's new rows: queries out; keys and values to LDS where the page fills
-  // up, to the window where it is one of the last two.  A later page of the same
-  // half as the first must wait until the first one's old rows are read: workgroup
-  // 0 writes it.
+  // this page's new rows: to LDS where the page fills up, to the window where it is
+  // one of the last two.  A later page of the same half as the first must wait until
+  // the first one's old rows are read: workgroup 0 writes it.
   const bool keep = pg >= last - 1 && !(blockIdx.x > 0 && old_rows && ((pg - pg0) & 1) == 0);
-  const int q4 = half / 4, per = (G + 2) * q4;
-  for (int e = tid; e < (hi - lo) * per; e += AT) {
-    const int pos = lo + e / per, hh = (e % per) / q4, p = 4 * (e % q4);
+  const int q4 = half / 4;
+  for (int e = tid; e < (hi - lo) * 2 * q4; e += AT) {
+    const int pos = lo + e / (2 * q4), p = 4 * (e % q4);
     uint2 a, b;
-    if (hh < G) {
-      const int64_t t = int64_t(s.b) + (pos - s.L);
-      const int64_t col = int64_t(u * G + hh) * d;
-      float x[4], y[4];
-      turned4(in.q + t * in.ldq + col, rope, n_rope, pos, p, half, x, y);
-      if (sa) {
-        float s0[4], s1[4];
-        load4(sa + u * d + p, s0);
-        load4(sa + u * d + p + half, s1);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          x[k] = x[k] / s0[k];
-          y[k] = y[k] / s1[k];
-        }
-      }
-      uint16_t* q = Qout + t * H * d + col + p;
-      *reinterpret_cast<uint2*>(q) = pack4(x);
-      *reinterpret_cast<uint2*>(q + half) = pack4(y);
-      continue;
-    }
-    const bool key = hh == G;
+    const bool key = (e / q4) & 1;
     const int r = pos - pg * P;
     if (key) key_row(pos, p, a, b);
     else value_row(pos, p, a, b);
@@ -1147,17 +1171,22 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, Joi
 hipError_t cache_append(const CacheArgs& c, const void* Q, int64_t ldq, const void* K, int64_t ldk,
                         const void* V, int64_t ldv, bool in_bf16, int H, const float* rope, int64_t n_rope,
                         const float* s_a, uint16_t* Qout, hipStream_t st) {
-  const dim3 grid(unsigned((c.max_q + c.P - 2) / c.P + 1), unsigned(c.Hkv), unsigned(c.n_seq));
+  // 512 threads where the pages' workgroups are few (a page that fills up is then a
+  // long walk: 26 us against 35 for 11 sequences of 142 tokens at one key head),
+  // 256 where they fill the card (91 us against 100 for twelve chunks of up to 4096
+  // float32 tokens at 64 heads).  Query slices: eight items of a thread each.
+  const int64_t pages = (int64_t(c.max_q) + c.P - 2) / c.P + 1, items = std::min<int64_t>(c.max_q, c.P) * H * (c.d / 8);
+  const unsigned threads = pages * c.Hkv * c.n_seq <= 1024 ? 512 : 256;
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(items / (8 * threads), 65535 - c.Hkv));
+  const dim3 grid(unsigned(pages), unsigned(c.Hkv + slices), unsigned(c.n_seq));
   const unsigned lds = unsigned(c.P) * c.d * 4;
-  if (in_bf16) {
-    RowIn<uint16_t> in{static_cast<const uint16_t*>(Q), static_cast<const uint16_t*>(K),
-                       static_cast<const uint16_t*>(V), ldq, ldk, ldv};
-    hipLaunchKernelGGL(cache_append_kernel<uint16_t>, grid, dim3(AT), lds, st, c, in, H, rope, n_rope, s_a, Qout);
-  } else {
-    RowIn<float> in{static_cast<const float*>(Q), static_cast<const float*>(K), static_cast<const float*>(V),
-                    ldq, ldk, ldv};
-    hipLaunchKernelGGL(cache_append_kernel<float>, grid, dim3(AT), lds, st, c, in, H, rope, n_rope, s_a, Qout);
-  }
+  auto go = [&](auto ti) {
+    using TI = decltype(ti);
+    const RowIn<TI> in{static_cast<const TI*>(Q), static_cast<const TI*>(K), static_cast<const TI*>(V), ldq, ldk, ldv};
+    hipLaunchKernelGGL(cache_append_kernel<TI>, grid, dim3(threads), lds, st, c, in, H, rope, n_rope, s_a, Qout);
+  };
+  if (in_bf16) go(uint16_t{});
+  else go(float{});
   return hipGetLastError();
 }
 
@@ -1176,6 +1205,12 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
 // How a call is cut up, from its sizes alone.  Rows of a key head: up to 32 go to
 // the row kernel, more to the tile kernel; a batch of prompts and decoding
 // sequences (tokens well below n_seq * max_q) runs both, each on its own.
+// Splits of the tokens: as many as give 1024 workgroups of the row kernel, which
+// streams the codes.  Tiles of 128 rows are bound by arithmetic, and 512 workgroups
+// are all that run at once (4 times as many: 119 -> 145 us for 512 rows a head over
+// 32768 tokens, the join's traffic); tiles of 64 rows wait for memory like the row
+// kernel and lengths are ragged, so 1536 (200 -> 126 us for 35 sequences of up to 27
+// tokens at 4 key heads of 8, up to 16741 long; 252 -> 136 us for 8 of 48, up to 16384).
 AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d) {
   const int64_t rows = int64_t(max_q) * (H / Hkv), heads = int64_t(n_seq) * Hkv;
   const bool mixed = n_seq > 1 && 4 * tokens < 3 * int64_t(n_seq) * max_q;
@@ -1185,7 +1220,9 @@ AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_
   auto cut = [](int64_t want, int64_t most) { return int(std::max<int64_t>(1, std::min(want, most))); };
   p.few = p.row_rows ? cut((1024 + heads - 1) / heads, std::min<int64_t>(128, max_len / 256)) : 1;
   const int64_t tiles = p.tile_rows ? (rows + p.tile_rows - 1) / p.tile_rows * heads : 0;
-  p.many = p.tile_rows ? cut(512 / std::max<int64_t>(1, tiles), std::min<int64_t>(64, max_len / 512)) : 1;
+  p.many = p.tile_rows ? cut((p.tile_rows == 64 ? 1536 : 512) / std::max<int64_t>(1, tiles),
+                             std::min<int64_t>(64, max_len / 512))
+                       : 1;
   p.few_floats = p.few > 1 ? size_t(p.few) * size_t(heads) * size_t(p.row_rows) * size_t(d + 2) : 0;
   p.many_floats = p.many > 1 ? size_t(p.many) * size_t(tiles) * size_t(p.tile_rows) * size_t(d + 2) : 0;
   return p;
