@@ -559,19 +559,16 @@ OQ_DEV Step step_of(float4 q, float vr) {
 // 16-token tiles each), masked ones -inf; they become the weights times their
 // chunk's factor, which the sum takes out again.  Returns the factor that the
 // row's numerators need.
+// (The maximum that passes NaN on takes two values an instruction straight from the
+// matrix unit; fmaxf would first quiet each.  A NaN score makes its weight NaN.)
 template <int NC>
 OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m, float& l) {
-  // (scaled first: a maximum of values straight from the matrix unit costs two
-  // instructions for each, to quiet a NaN)
+  auto top = [](float a, float b) { return __builtin_elementwise_maximum(a, b); };
   float mt = -INFINITY;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-#pragma unroll
-    for (int a = 2 * c; a < 2 * c + 2; ++a)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) st[a][q] = st[a][q] * sp[c].f;
     const f32x4_t x = st[2 * c], y = st[2 * c + 1];
-    mt = fmaxf(mt, fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))));
+    mt = fmaxf(mt, sp[c].f * top(top(top(top(x[0], x[1]), x[2]), top(x[3], y[0])), top(top(y[1], y[2]), y[3])));
   }
   const float mn = fmaxf(m, ceilf(row_max(mt)));
   const float off = mn == -INFINITY ? 0.0f : mn;         // no token seen yet: weights 2^-inf = 0
@@ -586,14 +583,13 @@ OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m,
     for (int a = 2 * c; a < 2 * c + 2; ++a)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        st[a][q] = __builtin_amdgcn_exp2f(st[a][q] + e);
+        st[a][q] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[a][q], sp[c].f, e));
         w += st[a][q];
       }
     l = __builtin_fmaf(w, sp[c].winv, l);
   }
   return alpha;
 }
-
 // The query rows of one key head (query x head of the group) in matrix operands.
 template <int DH>
 OQ_DEV void load_q(bf16x8_t (&qf)[DH / 32], const uint16_t* Q, int64_t ldq, const Seq& s, int u, int G, int row,
