@@ -2258,7 +2258,7 @@ oq_status check_heads(const oq_kv_cache* c, int heads) {
 }
 
 AttendPlan attend_plan(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
-  if (b->n_seq == 0 || b->max_q == 0) return AttendPlan{16, 0, 1, 1, 0, 0};
+  if (b->n_seq == 0 || b->max_q == 0) return AttendPlan{16, 0, 1, 1, 0, true, 0, 0};
   return cache_attend_plan(b->n_seq, c->kv_heads, heads, b->tokens, b->max_q, int64_t(b->max_pages) * c->page,
                            c->head_dim);
 }
@@ -2394,9 +2394,10 @@ oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const
   OQ_REQ(Q && O, "Q and O are required");
   OQ_REQ(aligned16(Q) && aligned16(O) && aligned16(LSE) && aligned16(ws), "pointers must be 16-byte aligned");
   const AttendPlan plan = attend_plan(cache, batch, heads);
-  const double groups = double(batch->max_q) * heads * batch->n_seq;
-  if (plan.tile_rows && groups * plan.many >= double(INT32_MAX))
-    return fail(OQ_ERR_UNSUPPORTED, "n_seq * max_q * heads = %.0f: too many rows for one call", groups);
+  const int64_t rows = int64_t(batch->max_q) * (heads / cache->kv_heads);
+  if (plan.tile_rows && (rows > (1 << 30) || plan.units * cache->kv_heads * plan.many >= (1 << 24)))
+    return fail(OQ_ERR_UNSUPPORTED, "%lld tokens of up to %lld query rows a key head: too many for one call",
+                (long long)batch->tokens, (long long)rows);
   const size_t need = (plan.few_floats + plan.many_floats) * 4;
   if (need && (!ws || ws_bytes < need))
     return fail(OQ_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws ? ws_bytes : size_t(0), need);

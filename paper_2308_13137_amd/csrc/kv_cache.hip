@@ -57,6 +57,39 @@ OQ_DEV Seq seq_of(const CacheArgs& c, int i) {
   if (int64_t(s.L) + s.n > int64_t(c.max_pages) * c.P) s.ok = false;
   return s;
 }
+// Ragged batches: unit w of all sequences' units (pages, row tiles), in the order of
+// the sequences, as (sequence, its unit); (-1, 0) past the last.  By every wave for
+// itself.  Batches whose grid of n_seq times the longest sequence's units is no
+// larger than the units' bound, or small, are numbered directly instead (a search
+// costs some 4 us: 15 chunks of up to 152 tokens 27 us, searched 32).  With 63
+// decoding sequences beside a prompt of 4,096 tokens at 64 heads the empty
+// workgroups of the direct grid took most of the time: attention 2,340 us, searched
+// 390; the append 154 and 49.
+struct Unit {
+  int i, k;
+};
+template <typename F>
+OQ_DEV Unit unit_of(int n_seq, int w, bool direct, F units) {
+  if (direct) return {w % n_seq, w / n_seq};
+  const int lane = threadIdx.x & 63;
+  for (int i0 = 0; i0 < n_seq; i0 += 64) {
+    const int n = i0 + lane < n_seq ? units(i0 + lane) : 0;
+    int sum = min(n, 0x3fffffff);                          // (row ranges may overlap: no sum overflows)
+    for (int off = 1; off < 64; off <<= 1) {
+      const int o = __shfl_up(sum, off);
+      if (lane >= off) sum = min(sum + o, 0x3fffffff);
+    }
+    const uint64_t past = __ballot(sum > w);
+    if (past) {
+      const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      const int before = l > 0 ? __shfl(sum, l - 1) : 0;
+      return {__builtin_amdgcn_readfirstlane(i0 + l), __builtin_amdgcn_readfirstlane(w - before)};
+    }
+    w -= __shfl(sum, 63);
+  }
+  return {-1, 0};
+}
+
 OQ_DEV int page_in(const CacheArgs& c, int p) { return p >= 0 && p < c.n_pages ? p : -1; }
 OQ_DEV int page_of(const CacheArgs& c, int i, int pg) { return page_in(c, c.table[int64_t(i) * c.max_pages + pg]); }
 
@@ -154,22 +187,28 @@ template <typename TI>
 __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI> in, int H,
                                                           const float* __restrict__ rope, int64_t n_rope,
                                                           const float* __restrict__ sa,
-                                                          uint16_t* __restrict__ Qout) {
+                                                          uint16_t* __restrict__ Qout, bool direct) {
   extern __shared__ uint4 s_page[];                        // K [P][d], then V in operand order, bf16
   __shared__ int s_max[2][8];
-  const int u = blockIdx.y, i = blockIdx.z, tid = threadIdx.x, AT = blockDim.x;
+  const int u = blockIdx.y, tid = threadIdx.x, AT = blockDim.x;
   const int d = c.d, half = d / 2, P = c.P;
+  const Unit un = unit_of(c.n_seq, int(blockIdx.x), direct, [&](int j) {
+    const Seq s = seq_of(c, j);
+    return s.n == 0 ? 0 : s.ok ? ((s.L + s.n - 1) >> c.lgP) - (s.L >> c.lgP) + 1 : (s.n + P - 1) >> c.lgP;
+  });
+  if (un.i < 0) return;
+  const int i = un.i;
   const Seq s = seq_of(c, i);
   if (s.n == 0) return;
   const int slice = u - c.Hkv, slices = int(gridDim.y) - c.Hkv;
   if (!s.ok) {                                             // nothing is cached; the queries are NaN
     if (slice < 0) return;
-    const int64_t n = int64_t(s.n) * H * d, step = int64_t(AT) * gridDim.x * slices;
-    for (int64_t e = tid + int64_t(AT) * (blockIdx.x + int64_t(gridDim.x) * slice); e < n; e += step)
-      Qout[int64_t(s.b) * H * d + e] = 0x7fc0;
+    const int64_t wide = int64_t(H) * d, at = int64_t(un.k) * P, n = min(int64_t(s.n), at + P) * wide;
+    for (int64_t e = at * wide + tid + int64_t(AT) * slice; e < n; e += int64_t(AT) * slices)
+      Qout[int64_t(s.b) * wide + e] = 0x7fc0;
     return;
   }
-  const int pg0 = s.L / P, pg = pg0 + int(blockIdx.x), end = s.L + s.n;
+  const int pg0 = s.L / P, pg = pg0 + un.k, end = s.L + s.n;
   const int lo = max(s.L, pg * P), hi = min(end, (pg + 1) * P);
   if (lo >= hi) return;
   if (slice >= 0) {
@@ -183,7 +222,7 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
   uint16_t* sk = reinterpret_cast<uint16_t*>(s_page);
   uint16_t* sv = sk + P * d;
   const bool old_rows = s.L % P != 0;
-  if (full && blockIdx.x == 0 && old_rows) {
+  if (full && un.k == 0 && old_rows) {
     // the page's rows from before the call (with whatever lies behind them: the new
     // rows overwrite that)
     const uint4* kw = reinterpret_cast<const uint4*>(window(c.kw, pg));
@@ -236,8 +275,8 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
   };
   // this page's new rows: to LDS where the page fills up, to the window where it is
   // one of the last two.  A later page of the same half as the first must wait until
-  // the first one's old rows are read: workgroup 0 writes it.
-  const bool keep = pg >= last - 1 && !(blockIdx.x > 0 && old_rows && ((pg - pg0) & 1) == 0);
+  // the first one's old rows are read: the first page's workgroup writes it.
+  const bool keep = pg >= last - 1 && !(un.k > 0 && old_rows && ((pg - pg0) & 1) == 0);
   const int q4 = half / 4;
   for (int e = tid; e < (hi - lo) * 2 * q4; e += AT) {
     const int pos = lo + e / (2 * q4), p = 4 * (e % q4);
@@ -263,7 +302,7 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
   }
   if (!full) return;
   __syncthreads();
-  if (blockIdx.x == 0 && old_rows) {
+  if (un.k == 0 && old_rows) {
     for (int page = max(last - 1, pg0 + 1); page <= last; ++page) {
       if ((page - pg0) & 1) continue;
       const int a0 = page * P, b0 = min(end, a0 + P);
@@ -348,13 +387,27 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
 template <typename TO>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int32_t* __restrict__ begin,
                                                          const int32_t* __restrict__ row_start, int64_t rows,
-                                                         TO* __restrict__ K, TO* __restrict__ V) {
+                                                         int max_rows, TO* __restrict__ K, TO* __restrict__ V,
+                                                         bool direct) {
   __shared__ float s_x[32][132];
-  const int u = blockIdx.y, i = blockIdx.z, d = c.d, tid = threadIdx.x;
+  const int u = blockIdx.y, d = c.d, tid = threadIdx.x;
+  // rows b .. e - 1 of sequence j, from its position `first` on
+  int64_t first, b, e;
+  auto range = [&](int j) {
+    first = max(begin[j], 0);
+    b = max(row_start[j], 0);
+    e = min(min(int64_t(row_start[j + 1]), rows), b + max_rows);
+  };
+  const Unit un = unit_of(c.n_seq, int(blockIdx.x), direct, [&](int j) {
+    range(j);
+    return b < e ? int((first % 32 + (e - b) + 31) / 32) : 0;
+  });
+  if (un.i < 0) return;
+  const int i = un.i;
   const Seq s = seq_of(c, i);
-  const int64_t first = max(begin[i], 0), b = max(row_start[i], 0), e = min(int64_t(row_start[i + 1]), rows);
+  range(i);
   // chunks of 32 from the one that holds the first position
-  const int64_t t0 = (first / 32 + blockIdx.x) * 32;
+  const int64_t t0 = (first / 32 + un.k) * 32;
   const int64_t at0 = b + (t0 - first);                   // the chunk's first row of the output
   if (b >= e || at0 >= e) return;
   const int64_t total = int64_t(s.L) + s.n, win = int64_t(c.P) * d;
@@ -817,6 +870,13 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void cache_attend_kernel(Cache
   }
 }
 
+// Tiles of `qw` rows of a sequence's rows of one key head, and the one of a unit (the
+// last one first).
+OQ_DEV int row_tiles(int rows, int qw, int rows_min) { return rows < rows_min ? 0 : (rows + qw - 1) / qw; }
+OQ_DEV int tile_of(Unit un, int max_rows, int rows, int qw, bool direct) {
+  return ((direct ? max_rows : rows) + qw - 1) / qw - 1 - un.k;
+}
+
 // Many rows (prompts): one workgroup of four waves takes 64 R rows of one key head,
 // 16 R per wave, over tiles of 64 tokens.  The waves turn a tile's codes into f16
 // operands once, in LDS, a tile ahead; the raw codes of the one after are in
@@ -832,7 +892,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
                                                                        uint16_t* __restrict__ O,
                                                                        float* __restrict__ LSE,
                                                                        float* __restrict__ part, int splits,
-                                                                       int rows_min) {
+                                                                       int rows_min, int units, bool direct) {
   constexpr int KS = DH / 32, JD = DH / 16, QW = 64 * R;
   constexpr int TILE = 64 * DH / 8;                      // 16-byte pieces of one operand's tile
   constexpr int CW = 2, LPW = JD / CW;                   // waves of a chunk, loads of a wave
@@ -841,17 +901,17 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
   __shared__ unsigned s_bad[2][2][CW];
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // key heads fastest (an XCD keeps its heads' pages in its L2), longest rows first
+  // key heads fastest (an XCD keeps its heads' pages in its L2), a sequence's longest rows first
   const int G = H / c.Hkv, P = c.P;
-  const int ntile = (c.max_q * G + QW - 1) / QW;
   int x = int(blockIdx.x);
   const int u = x % c.Hkv;
   x /= c.Hkv;
-  const int split = x % splits;
-  x /= splits;
-  const int i = x % c.n_seq, rt = ntile - 1 - x / c.n_seq;
+  const int split = x % splits, w = x / splits;
+  const Unit un = unit_of(c.n_seq, w, direct, [&](int j) { return row_tiles(seq_of(c, j).n * G, QW, rows_min); });
+  if (un.i < 0) return;
+  const int i = un.i;
   const Seq s = seq_of(c, i);
-  const int rows = s.n * G, row0 = rt * QW;
+  const int rows = s.n * G, rt = tile_of(un, c.max_q * G, rows, QW, direct), row0 = rt * QW;
   if (rows < rows_min || row0 >= rows) return;
   const int total = s.ok ? s.L + s.n : 0, closed = total & ~(P - 1);
   const float sc = 1.4426950408889634f / sqrtf(float(DH));
@@ -1082,8 +1142,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     for (int h = 0; h < R; ++h) load_q<DH>(qf[h], Q, ldq, s, u, G, row_of(h), g);
   }
   for (; t < k1; ++t) tile(t, std::true_type{});
-  const Out out = out_of(O, LSE, part, splits, split, H, c.T, int64_t(ntile) * c.n_seq * c.Hkv,
-                         (int64_t(rt) * c.n_seq + i) * c.Hkv + u, QW, DH);
+  const Out out = out_of(O, LSE, part, splits, split, H, c.T, int64_t(units) * c.Hkv, int64_t(w) * c.Hkv + u, QW, DH);
 #pragma unroll
   for (int h = 0; h < R; ++h) {
     l[h] = row_sum(l[h]);
@@ -1101,10 +1160,14 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
 }
 
 // Joins a row's splits: DH / 4 lanes of four output values each, NG groups of them
-// dealing the splits among themselves; 256 threads take 1024 / (DH NG) rows.
+// dealing the splits among themselves; 256 threads take RW rows of a unit, of the
+// row kernel's first.
 struct JoinArgs {
   const float *few, *many;           // shares of the two kernels
-  int few_splits, many_splits, row_rows, tile_rows;
+  int few_splits, many_splits, row_rows, tile_rows, units;
+  int few_rows;                      // rows of a unit of the row kernel that can be in use
+  int few_blocks;
+  bool direct;
 };
 template <int DH, int NG>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, JoinArgs a, uint16_t* __restrict__ O,
@@ -1112,20 +1175,26 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, Joi
   constexpr int Q4 = DH / 4, RW = 256 / (Q4 * NG);
   __shared__ float4 s_o[NG][RW][Q4];
   __shared__ float2 s_ml[NG][RW];
-  const int i = blockIdx.y, G = H / c.Hkv;
-  const Seq s = seq_of(c, i);
+  const int G = H / c.Hkv;
+  const bool few = int(blockIdx.x) < a.few_blocks;
+  const int unit_rows = few ? a.row_rows : a.tile_rows, blocks = ((few ? a.few_rows : a.tile_rows) + RW - 1) / RW;
+  const int bid = int(blockIdx.x) - (few ? 0 : a.few_blocks), unit = bid / blocks, u = unit % c.Hkv;
+  const Unit un = few ? Unit{unit / c.Hkv, 0}
+                      : unit_of(c.n_seq, unit / c.Hkv, a.direct, [&](int j) {
+                          return row_tiles(seq_of(c, j).n * G, a.tile_rows, a.row_rows + 1);
+                        });
+  if (un.i < 0) return;
+  const Seq s = seq_of(c, un.i);
+  const int rows = s.n * G, row0 = few ? 0 : tile_of(un, c.max_q * G, rows, a.tile_rows, a.direct) * a.tile_rows;
   const int lane = threadIdx.x % Q4, ng = (threadIdx.x / Q4) % NG, rw = threadIdx.x / (Q4 * NG);
-  const int64_t e = int64_t(blockIdx.x) * RW + rw;       // row: token of the sequence x head
-  const bool few = s.n * G <= a.row_rows;
+  const int at0 = (bid % blocks) * RW;                     // the block's first row of the unit
+  if (few != (rows <= a.row_rows) || row0 + at0 >= rows) return;
+  const bool in = at0 + rw < unit_rows && row0 + at0 + rw < rows;
+  const int row = in ? row0 + at0 + rw : row0 + at0, j = row / G, hd = u * G + row % G;
   const int splits = few ? a.few_splits : a.many_splits;
-  if (splits == 1 || int64_t(blockIdx.x) * RW >= int64_t(s.n) * H) return;
-  const bool in = e < int64_t(s.n) * H;
-  const int j = in ? int(e / H) : 0, hd = in ? int(e % H) : 0, u = hd / G, row = j * G + hd % G;
-  const int rows = few ? a.row_rows : a.tile_rows, ntile = few ? 1 : (c.max_q * G + rows - 1) / rows;
-  const int64_t units = int64_t(ntile) * c.n_seq * c.Hkv;
-  const int64_t at = ((int64_t(few ? 0 : row / rows) * c.n_seq + i) * c.Hkv + u) * rows + row % rows;
+  const int64_t units = int64_t(few ? c.n_seq : a.units) * c.Hkv, at = int64_t(unit) * unit_rows + (row - row0);
   const float* part = few ? a.few : a.many;
-  const float2* ml = reinterpret_cast<const float2*>(part + splits * units * rows * DH);
+  const float2* ml = reinterpret_cast<const float2*>(part + splits * units * unit_rows * DH);
   float m = -INFINITY, l = 0.0f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   auto join = [&](float mk, float lk, float4 x) {
@@ -1139,7 +1208,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, Joi
   };
 #pragma unroll 4
   for (int k = ng; k < splits; k += NG) {
-    const int64_t p = k * units * rows + at;
+    const int64_t p = k * units * unit_rows + at;
     const float2 w = ml[p];
     join(w.x, w.y, *reinterpret_cast<const float4*>(part + p * DH + 4 * lane));
   }
@@ -1171,15 +1240,21 @@ hipError_t cache_append(const CacheArgs& c, const void* Q, int64_t ldq, const vo
   // long walk: 26 us against 35 for 11 sequences of 142 tokens at one key head),
   // 256 where they fill the card (91 us against 100 for twelve chunks of up to 4096
   // float32 tokens at 64 heads).  Query slices: eight items of a thread each.
-  const int64_t pages = (int64_t(c.max_q) + c.P - 2) / c.P + 1, items = std::min<int64_t>(c.max_q, c.P) * H * (c.d / 8);
-  const unsigned threads = pages * c.Hkv * c.n_seq <= 1024 ? 512 : 256;
+  // Pages: of the longest sequence times n_seq, or, where that is less, what T tokens
+  // in at most min(n_seq, T) sequences can touch.
+  const int64_t grid_pages = ((int64_t(c.max_q) + c.P - 2) / c.P + 1) * c.n_seq;
+  const int64_t most = c.T / c.P + 2 * std::min<int64_t>(c.n_seq, c.T);
+  const bool direct = grid_pages <= most || grid_pages * c.Hkv <= 1024;
+  const int64_t units = direct ? grid_pages : most, items = std::min<int64_t>(c.max_q, c.P) * H * (c.d / 8);
+  const unsigned threads = units * c.Hkv <= 1024 ? 512 : 256;
   const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(items / (8 * threads), 65535 - c.Hkv));
-  const dim3 grid(unsigned(pages), unsigned(c.Hkv + slices), unsigned(c.n_seq));
+  const dim3 grid(unsigned(units), unsigned(c.Hkv + slices));
   const unsigned lds = unsigned(c.P) * c.d * 4;
   auto go = [&](auto ti) {
     using TI = decltype(ti);
     const RowIn<TI> in{static_cast<const TI*>(Q), static_cast<const TI*>(K), static_cast<const TI*>(V), ldq, ldk, ldv};
-    hipLaunchKernelGGL(cache_append_kernel<TI>, grid, dim3(threads), lds, st, c, in, H, rope, n_rope, s_a, Qout);
+    hipLaunchKernelGGL(cache_append_kernel<TI>, grid, dim3(threads), lds, st, c, in, H, rope, n_rope, s_a, Qout,
+                       direct);
   };
   if (in_bf16) go(uint16_t{});
   else go(float{});
@@ -1188,13 +1263,16 @@ hipError_t cache_append(const CacheArgs& c, const void* Q, int64_t ldq, const vo
 
 hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* row_start, int64_t rows,
                       int max_rows, void* K, void* V, bool bf16, hipStream_t st) {
-  const dim3 grid(unsigned((int64_t(max_rows) + 30) / 32 + 1), unsigned(c.Hkv), unsigned(c.n_seq));
+  const int64_t grid_chunks = ((int64_t(max_rows) + 30) / 32 + 1) * c.n_seq;
+  const int64_t most = rows / 32 + 2 * std::min<int64_t>(c.n_seq, rows);
+  const bool direct = grid_chunks <= most || grid_chunks * c.Hkv <= 1024;
+  const dim3 grid(unsigned(direct ? grid_chunks : most), unsigned(c.Hkv));
   if (bf16)
-    hipLaunchKernelGGL(cache_read_kernel<uint16_t>, grid, dim3(256), 0, st, c, begin, row_start, rows,
-                       static_cast<uint16_t*>(K), static_cast<uint16_t*>(V));
+    hipLaunchKernelGGL(cache_read_kernel<uint16_t>, grid, dim3(256), 0, st, c, begin, row_start, rows, max_rows,
+                       static_cast<uint16_t*>(K), static_cast<uint16_t*>(V), direct);
   else
-    hipLaunchKernelGGL(cache_read_kernel<float>, grid, dim3(256), 0, st, c, begin, row_start, rows,
-                       static_cast<float*>(K), static_cast<float*>(V));
+    hipLaunchKernelGGL(cache_read_kernel<float>, grid, dim3(256), 0, st, c, begin, row_start, rows, max_rows,
+                       static_cast<float*>(K), static_cast<float*>(V), direct);
   return hipGetLastError();
 }
 
@@ -1215,10 +1293,17 @@ AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_
   p.row_rows = rows <= 16 ? 16 : rows <= 32 || mixed ? 32 : 0;
   auto cut = [](int64_t want, int64_t most) { return int(std::max<int64_t>(1, std::min(want, most))); };
   p.few = p.row_rows ? cut((1024 + heads - 1) / heads, std::min<int64_t>(128, max_len / 256)) : 1;
-  const int64_t tiles = p.tile_rows ? (rows + p.tile_rows - 1) / p.tile_rows * heads : 0;
-  p.many = p.tile_rows ? cut((p.tile_rows == 64 ? 1536 : 512) / std::max<int64_t>(1, tiles),
-                             std::min<int64_t>(64, max_len / 512))
-                       : 1;
+  p.units = 0;
+  p.direct = true;
+  if (p.tile_rows) {
+    // tiles of the longest sequence times n_seq, or, where that is less, what T tokens can fill
+    const int64_t G = H / Hkv, grid = (rows + p.tile_rows - 1) / p.tile_rows * n_seq;
+    const int64_t most = tokens * G / p.tile_rows + std::min<int64_t>(n_seq, tokens * G / (p.row_rows + 1));
+    p.direct = grid <= most || grid * Hkv <= 1024;
+    p.units = p.direct ? grid : most;
+  }
+  const int64_t tiles = p.units * Hkv;
+  p.many = tiles ? cut((p.tile_rows == 64 ? 1536 : 512) / tiles, std::min<int64_t>(64, max_len / 512)) : 1;
   p.few_floats = p.few > 1 ? size_t(p.few) * size_t(heads) * size_t(p.row_rows) * size_t(d + 2) : 0;
   p.many_floats = p.many > 1 ? size_t(p.many) * size_t(tiles) * size_t(p.tile_rows) * size_t(d + 2) : 0;
   return p;
@@ -1235,16 +1320,19 @@ hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int 
   };
   auto many = [&](auto dh, auto rr) {
     constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
-    const int64_t tiles = (int64_t(c.max_q) * G + 64 * R - 1) / (64 * R);
-    const dim3 grid(unsigned(tiles * c.n_seq * p.many * c.Hkv));
+    const dim3 grid(unsigned(p.units * p.many * c.Hkv));
     hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws_many,
-                       p.many, p.row_rows + 1);
+                       p.many, p.row_rows + 1, int(p.units), p.direct);
   };
   auto join = [&](auto dh, auto ng) {
     constexpr int DH = decltype(dh)::value, NG = decltype(ng)::value, RW = 1024 / (DH * NG);
-    const JoinArgs a{ws, ws_many, p.few, p.many, p.row_rows, p.tile_rows};
-    const dim3 grid(unsigned((int64_t(c.max_q) * H + RW - 1) / RW), unsigned(c.n_seq));
-    hipLaunchKernelGGL((cache_join_kernel<DH, NG>), grid, dim3(256), 0, st, c, H, a, O, LSE);
+    const int few_rows = int(std::min<int64_t>(p.row_rows, int64_t(c.max_q) * G));
+    const int64_t few_blocks = p.few > 1 ? int64_t((few_rows + RW - 1) / RW) * c.Hkv * c.n_seq : 0;
+    const int64_t many_blocks = p.many > 1 ? p.units * c.Hkv * (p.tile_rows / RW) : 0;
+    const JoinArgs a{ws, ws_many, p.few, p.many, p.row_rows, p.tile_rows, int(p.units), few_rows, int(few_blocks),
+                     p.direct};
+    hipLaunchKernelGGL((cache_join_kernel<DH, NG>), dim3(unsigned(few_blocks + many_blocks)), dim3(256), 0, st, c, H,
+                       a, O, LSE);
   };
   auto run = [&](auto dh) {
     const std::integral_constant<int, 1> i1{};

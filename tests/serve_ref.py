@@ -5,6 +5,7 @@ import torch
 
 F24 = 2.0 ** -24                # half a step of fp32, relative
 BF8 = 2.0 ** -8                 # half a step of bf16, relative
+F11 = 2.0 ** -11                # half a step of fp16, relative
 
 
 def f64(t):
@@ -67,7 +68,7 @@ class PlainCache:
 
 def attend64(q, k, v, before):
     """fp64 attention of one sequence: q [n, H, d], k, v [tokens, Hkv, d] (as held), with the
-    bound of what bf16 weights, fp32 scores and a bf16 output may change, per value."""
+    bound of what f16 weights, fp32 scores and a bf16 output may change, per value."""
     n, H, d = q.shape
     G = H // k.shape[1]
     q, k, v = q.double(), k.double(), v.double()
@@ -83,15 +84,20 @@ def attend64(q, k, v, before):
         # each step is off by half a unit of what it holds, in the exponent
         mag = (q[:, h].abs() @ kk.abs().t() / d ** 0.5).masked_fill(hide, 0.0).amax(1, keepdim=True)
         es = (d + 6) * F24 * mag * 2 + 2.0 ** -21
-        # weights rounded to bf16 (half a step), sums of their products in fp32; a row's two sums
-        # (numerator, denominator) both carry the scores' error; then one bf16 rounding
+        # prompts' queries enter as f16 of at least 2^14 at the row's largest entry: bf16's 8 bits fit
+        # f16's 11, and an entry that falls below f16's smallest step, 2^-24, loses at most half of it,
+        # 2^-25 = 2^-39 of the largest; times the keys' sum of magnitudes, in the exponent
+        es = es + 2.0 ** -39 * q[:, h].abs().amax(1, keepdim=True) * kk.abs().sum(1).max() / d ** 0.5
+        # weights rounded to f16 (half a step; the open page's to two bf16 terms, 2^-16), sums of their
+        # products in fp32; a row's two sums (numerator, denominator) both carry the scores' error;
+        # then one bf16 rounding
         av = p @ vv.abs()
         # what a 16-bit weight cannot hold: weights of full pages enter as f16 of at most 2^15 (the
         # largest is over 2^13: a row's maximum is rounded up to an integer, a step to a power of two),
         # so half a subnormal step, 2^-25, is at most 2^-38 of the largest weight times step; times a
         # code of at most 127, and 127 steps are a page's largest value
         small = len(kk) * 2.0 ** -38 * vv.abs().max()
-        tol[:, h] = (av * (BF8 + 2 * es + 2 * len(kk) * F24) * 1.01 + out[:, h].abs() * BF8 * 1.01 + small
+        tol[:, h] = (av * (F11 + 2 * es + 2 * len(kk) * F24) * 1.01 + out[:, h].abs() * BF8 * 1.01 + small
                      + 1e-30)
         lse[h] = torch.logsumexp(s, 1) * 1.4426950408889634
     return out, tol, lse

@@ -434,3 +434,134 @@ def test_shared_pages():
     q[1] = q[0]
     o = b.cache.attend(q, table, i32([129, 129]), i32([0, 1, 2]), 1, slots=i32([0, 1]))
     assert torch.equal(o[0], o[1]) and torch.isfinite(o.float()).all()
+
+
+@pytest.mark.parametrize("H,Hkv,page", [(4, 1, 128), (20, 4, 128), (40, 8, 32)])
+def test_cache_few_heads(H, Hkv, page):
+    """Chunks that end pages, at few key heads with many query heads, beside single tokens and empty ones."""
+    b = Batch(4, H, Hkv, 128, page, 400, seed=H)
+    b.step([142, 0, 77, 1])
+    b.step([1, 5, 130, 0])
+    b.check_rows()
+
+
+@pytest.mark.parametrize("d,long", [(64, (66,)), (128, (0, 69)), (64, (3, 30, 31))])
+def test_cache_ragged_batch(d, long):
+    """Prompts among 70 sequences that decode or rest, more than one wave's worth."""
+    b = Batch(70, 8, 8, d, 32, 2200, seed=d + len(long))
+    b.step([1 + 7 * (i % 9) for i in range(70)], attend=False)
+    counts = [int(i % 5 != 1) for i in range(70)]
+    for i in long:
+        counts[i] = 300 + i
+    b.step(counts)
+    b.step([1] * 70)
+    b.check_rows()
+
+
+def test_cache_ragged_batch_grouped():
+    """Row tiles of grouped heads that begin inside a token, few rows of one sequence beside many of another."""
+    b = Batch(66, 40, 8, 64, 64, 700, seed=8, s_a=False)
+    b.step([600 - 8 * i if i < 60 else 0 for i in range(66)], attend=False)
+    b.step([1] * 20 + [7] * 20 + [0] * 10 + [40] + [2] * 14 + [90])
+
+
+def test_ragged_entries_that_do_not_fit():
+    """In a batch whose units are searched for: bad sequences are NaN (the first max_q rows of a range that is
+    longer), the others as without them."""
+    d, P, n, Hkv = 64, 32, 70, 8
+    counts = [1] * n
+    counts[5], counts[6], counts[40], counts[65], counts[66] = 200, 90, 200, 200, 70
+    qs = [0]
+    for k in counts:
+        qs.append(qs[-1] + k)
+    T = qs[-1]
+    x = rand(2, T, 3 * Hkv * d, dtype=BF)
+    rows = torch.arange(T, device="cuda")
+
+    def run(bad):
+        cache = oq.KVCache(n * 8, P, Hkv, d, n)
+        table = torch.arange(n * 8, dtype=torch.int32, device="cuda").view(n, 8)
+        slots, length, mq = list(range(n)), [3] * n, 200
+        if bad:
+            slots[5], length[65], table[40, 1], mq = n, 8 * P - 100, n * 8, 199
+        w = Hkv * d
+        args = (table, i32(length), i32(qs), mq)
+        q = torch.full((T, w), 7.0, dtype=BF, device="cuda")
+        cache.append(x[:, :w], x[:, w:2 * w], x[:, 2 * w:], *args, slots=i32(slots), out=q)
+        o = torch.full((T, w), 7.0, dtype=BF, device="cuda")
+        cache.attend(q, *args, slots=i32(slots), out=o)
+        return q, o
+
+    (q0, o0), (q1, o1) = run(False), run(True)
+    assert torch.isfinite(q0.float()).all() and torch.isfinite(o0.float()).all()
+    lost = torch.zeros(T, dtype=torch.bool, device="cuda")
+    for i in (5, 40, 65):                           # longer than max_q now, all three
+        a, e = qs[i], qs[i] + 199
+        lost |= (rows >= a) & (rows <= e)
+        assert torch.isnan(q1[a:e].float()).all() and torch.isnan(o1[a:e].float()).all()
+        assert (q1[e] == 7).all() and (o1[e] == 7).all()
+    assert torch.equal(q1[~lost], q0[~lost]) and torch.equal(o1[~lost], o0[~lost])
+
+
+def test_outputs_in_place():
+    """The queries turned in their own rows, the output over the queries."""
+    for counts in ([130, 1, 33], [1, 1, 1]):
+        H, Hkv, d, P = 16, 2, 128, 64
+        T, W = sum(counts), H * d
+        table = torch.arange(18, dtype=torch.int32, device="cuda").view(3, 6)
+        qs = i32([0, counts[0], counts[0] + counts[1], T])
+        q, k, v = rand(3, T, W, dtype=BF), rand(4, T, Hkv * d, dtype=BF), rand(5, T, Hkv * d, dtype=BF)
+        rope, s_a = oq.rope_table(400, d), rand(6, Hkv * d).abs() + 0.5
+        got = []
+        for place in (False, True):
+            c = oq.KVCache(18, P, Hkv, d, 3)
+            args = (table, i32([9, 200, 0]), qs, max(counts))
+            x = q.clone()
+            t = c.append(x, k, v, *args, rope=rope, s_a=s_a, out=x if place else None)
+            c.k_scale.fill_(0.01)
+            c.v_scale.fill_(0.01)
+            got.append((t.clone(), c.attend(t, *args, out=t if place else None)))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+def test_cache_offsets_past_32_bits():
+    """Pages and windows that begin more than 4 GiB into their tensors."""
+    H = Hkv = 8
+    d, P = 128, 128
+    n_pages, n_slots = 2 ** 32 // (Hkv * P * d) + 64, 2 ** 32 // (2 * Hkv * P * d * 2) + 64
+    cache = oq.KVCache(n_pages, P, Hkv, d, n_slots)
+    assert cache.k_codes.numel() > 2 ** 32 and cache.k_window.numel() * 2 > 2 ** 32
+    small = oq.KVCache(3, P, Hkv, d, 1)
+    T, w = 300, Hkv * d
+    x = rand(7, T + 1, 3 * w, dtype=BF)
+    out = []
+    for c, pages, slot in ((cache, [n_pages - 1, n_pages - 40, n_pages - 2], n_slots - 1), (small, [0, 1, 2], 0)):
+        table = i32([pages])
+        for at, n in ((0, T), (T, 1)):
+            r = x[at:at + n]
+            args = (table, i32([at]), i32([0, n]), n)
+            q = c.append(r[:, :w], r[:, w:2 * w], r[:, 2 * w:], *args, slots=i32([slot]))
+            out.append(c.attend(q, *args, slots=i32([slot])))
+        k, v = c.read(table, i32([0]), i32([T]), i32([0, 1]), i32([0, T + 1]), T + 1, T + 1, slots=i32([slot]))
+        out += [k, v]
+    for a, b in zip(out[:4], out[4:]):
+        assert torch.isfinite(a.float()).all() and torch.equal(a, b)
+
+
+def test_rows_past_32_bits():
+    """The last rows of tensors of more than 2^31 elements."""
+    T, D, N = 270000, 64, 8192                      # codes [T, D], products [T, N]
+    codes = torch.randint(0, 256, (T, D), dtype=torch.uint8, device="cuda")
+    h, z = torch.full((T,), 0.01, device="cuda"), torch.full((T,), 128.0, device="cuda")
+    wc = torch.randint(0, 256, (N, D), dtype=torch.uint8, device="cuda")
+    hw, zw = torch.full((N,), 0.01, device="cuda"), torch.full((N,), 127.0, device="cuda")
+    packed, wsum = oq.int8_pack(wc)
+    y = oq.int8_linear(codes, h, z, packed, wsum, hw, zw, out_dtype=BF)
+    assert y.numel() > 2 ** 31
+    tail = slice(T - 300, T)
+    assert torch.equal(y[tail], oq.int8_linear(codes[tail].clone(), h[tail].clone(), z[tail].clone(), packed, wsum,
+                                               hw, zw, out_dtype=BF))
+    gain = torch.ones(N, device="cuda")
+    _, _, c, hh, zz = oq.rmsnorm_quant(y, gain, 8)
+    _, _, c1, h1, z1 = oq.rmsnorm_quant(y[tail].clone(), gain, 8)
+    assert torch.equal(c[tail], c1) and torch.equal(hh[tail], h1) and torch.equal(zz[tail], z1)
