@@ -675,7 +675,8 @@ oq_status oq_int8_pack(const uint8_t* codes, int64_t c_out, int64_t c_in, int8_t
  * Zero points are integers held in fp32.  The integer sum is exact, the zero
  * points enter in fp64, and then one fp32 rounding each: the sum, h_x h_w, their
  * product, the bias.  A token's outputs do not depend on the other tokens.
- * Shapes as oq_int8_pack; n_tok or c_out = 0 is a no-op that accepts NULL.
+ * Shapes as oq_int8_pack, n_tok at most 4194304 and n_tok * c_out at most 2^38 (else
+ * OQ_ERR_UNSUPPORTED); n_tok or c_out = 0 is a no-op that accepts NULL.
  */
 oq_status oq_int8_linear(const uint8_t* x, const float* h_x, const float* z_x, int64_t n_tok,
                          int64_t c_in, const int8_t* packed, const int32_t* wsum, const float* h_w,
@@ -691,10 +692,11 @@ oq_status oq_rope_table(int64_t n_pos, int head_dim, float base, float* tab, hip
  * tensor: the symmetric 8-bit quantiser over the block's page * head_dim values,
  * h = max(max|x| / 127, 1e-5), code = rint(x * (1/h)).  The open page and the one
  * before it are bf16 rows in the sequence's window (page p in half p % 2).  A
- * page is quantised once, from its bf16 rows, so its codes do not depend on how
- * its tokens arrived; the newest tokens can be dropped, back to the start of the
- * page before the last, by lowering `length`.  A page or window that several
- * sequences of one append write is a race; full pages may be shared by any.
+ * page is quantised from its bf16 rows when it fills up, so its codes do not
+ * depend on how its tokens arrived; the newest tokens can be dropped by lowering
+ * `length`, back to the start of the page before the furthest page that the window
+ * has held rows of (again and again, but never below that).  A page or window that
+ * several sequences of one append write is a race; full pages may be shared by any.
  * Layouts (lane = 16 g + r):
  *   K codes  [page/16][d/64][g][r][16]: token 16 a + r, channel 64 j + 16 g + b
  *   V codes  [page/32][d/32][g][r][2][8]: channel 32 j + 16 hh + r; element e: token
@@ -719,8 +721,10 @@ typedef struct {
  * for oq_kv_append, oq_kv_attend and oq_kv_read alike.  A sequence whose entries
  * do not fit (a row range outside [0, T] or longer than max_q, a length that with
  * the new tokens passes max_pages * page, a slot outside the cache) is not cached
- * and its outputs are NaN (rows outside every range are left as they were); a
- * page number outside the pool reads as NaN and is not written. */
+ * and its outputs are NaN (of a range longer than max_q, its first max_q rows; rows
+ * outside every range are left as they were); a page number outside the pool reads
+ * as NaN and is not written.  Row ranges must not overlap: rows that two sequences
+ * claim are undefined. */
 typedef struct {
   int n_seq, max_pages, max_q;     /* max_q: at least the largest number of new tokens */
   int64_t tokens;                  /* T, the rows of Q, K, V and the outputs           */
@@ -738,7 +742,8 @@ typedef struct {
  *   multiple of 8
  *   rope  : [n_rope, head_dim / 2, 2] (oq_rope_table) | NULL = no rotation; a position
  *           >= n_rope gives NaN
- *   s_a   : [kv_heads d] fp32 | NULL;   Q_out : bf16 [T, heads d] */
+ *   s_a   : [kv_heads d] fp32 | NULL
+ *   Q_out : bf16 [T, heads d], may be Q itself (bf16, ld_q = heads d) */
 oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,
                        const void* K, int64_t ld_k, const void* V, int64_t ld_v, oq_dtype in_dt,
                        int heads, const float* rope, int64_t n_rope, const float* s_a, void* Q_out,
@@ -747,15 +752,20 @@ oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const
 /* oq_kv_attend: causal attention of the batch's new tokens over the cache that
  * holds them (after oq_kv_append): O = softmax(Q K^T / sqrt(d)) V per head, the
  * token at position p seeing positions 0 .. p, query head h reading key head
- * h / (heads / kv_heads).  Products on bf16 matrix cores (codes are exact in
- * bf16; probabilities times the page's V step enter as bf16), sums and softmax
- * statistics fp32.
- *   Q bf16 [T, heads d], rows ld_q apart;  O bf16 [T, heads d];  LSE fp32 [heads, T]
- *   | NULL: log-sum-exp of a row's logits in base 2, as oq_attention_fwd's
+ * h / (heads / kv_heads).  Products on 16-bit matrix cores, sums and softmax
+ * statistics fp32.  Codes are exact in bf16 and fp16; queries of more than 32 rows a
+ * key head meet them as fp16 times a power of two of the row's (what is lost is
+ * below 2^-39 of the row's largest entry).  A weight times its page's V step enters
+ * as fp16, 11 bits, in units of 2^-15 of a power of two over every V step so far
+ * (below 2^-40 of that it is lost), against the open page as two bf16 terms.
+ *   Q   : bf16 [T, heads d], rows ld_q apart
+ *   O   : bf16 [T, heads d], may be Q itself (ld_q = heads d)
+ *   LSE : fp32 [heads, T] | NULL: log-sum-exp of a row's logits in base 2, as
+ *         oq_attention_fwd's
  * A row that sees a key or value that is not finite, or any token of a page that
  * holds one, is NaN; others are not touched by it.  The work of a row is split
  * over its tokens where there are few rows, by a rule on (n_seq, heads, kv_heads,
- * max_q, max_pages * page) alone.  Workspace: oq_kv_attend_workspace_size. */
+ * tokens, max_q, max_pages * page) alone.  Workspace: oq_kv_attend_workspace_size. */
 oq_status oq_kv_attend_workspace_size(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads,
                                       size_t* bytes);
 oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,

@@ -2327,9 +2327,10 @@ oq_status oq_int8_linear(const uint8_t* x, const float* h_x, const float* z_x, i
   OQ_REQ(n_tok >= 0 && c_out >= 0 && c_in > 0 && c_in % 16 == 0,
          "bad shape n_tok=%lld c_in=%lld c_out=%lld (need c_in %% 16 == 0)", (long long)n_tok, (long long)c_in,
          (long long)c_out);
-  if (c_in > I8_MAX_C_IN || c_out > INT32_MAX - 256 || n_tok > (1 << 22))
-    return fail(OQ_ERR_UNSUPPORTED, "c_in=%lld > %lld, c_out=%lld or n_tok=%lld > 4194304", (long long)c_in,
-                (long long)I8_MAX_C_IN, (long long)c_out, (long long)n_tok);
+  if (c_in > I8_MAX_C_IN || c_out > INT32_MAX - 256 || n_tok > (1 << 22) ||
+      n_tok * c_out > (int64_t(1) << 38))
+    return fail(OQ_ERR_UNSUPPORTED, "c_in=%lld > %lld, c_out=%lld, n_tok=%lld > 4194304 or more than 2^38 outputs",
+                (long long)c_in, (long long)I8_MAX_C_IN, (long long)c_out, (long long)n_tok);
   if (n_tok == 0 || c_out == 0) return OQ_OK;
   OQ_REQ(x && h_x && z_x && packed && wsum && h_w && z_w && Y, "every tensor but B is required");
   OQ_REQ(aligned16(x) && aligned16(h_x) && aligned16(z_x) && aligned16(packed) && aligned16(wsum) &&

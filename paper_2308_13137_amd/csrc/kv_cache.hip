@@ -880,8 +880,10 @@ OQ_DEV int tile_of(Unit un, int max_rows, int rows, int qw, bool direct) {
 // Many rows (prompts): one workgroup of four waves takes 64 R rows of one key head,
 // 16 R per wave, over tiles of 64 tokens.  The waves turn a tile's codes into f16
 // operands once, in LDS, a tile ahead; the raw codes of the one after are in
-// flight meanwhile.  Bound by the vector units (softmax, conversion) beside the
-// matrix instructions, two workgroups to a compute unit.
+// flight meanwhile.  Bound by the vector units (softmax, conversion: busy some two
+// thirds of the time, the matrix units one third), two workgroups to a compute
+// unit: two chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 208 us,
+// 635 TFLOP/s; 4,096 tokens at 64 heads 330 us, 830 TFLOP/s.
 //
 // Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below

@@ -1048,7 +1048,8 @@ class KVCache:
     begin, ``max_q``: the most that one has) calls :meth:`append`, then
     :meth:`attend`, both with ``length`` as before the step, and then adds the new
     tokens to ``length``.  All index tensors are int32 on the GPU and are read
-    when the kernels run."""
+    when the kernels run.  The newest tokens are dropped by lowering ``length``, at
+    most back to the start of the page before the furthest one begun."""
 
     def __init__(self, n_pages, page, kv_heads, head_dim, n_slots, device="cuda"):
         blk = page * head_dim
@@ -1092,7 +1093,8 @@ class KVCache:
                stream=None):
         """RoPE and the [Q, K] scale on the new tokens' Q [T, H d], K, V [T, Hkv d]
         (bf16 or fp32; columns of one tensor will do); K and V into the cache
-        (oq_kv_append).  Returns Q~ bf16 [T, H d] (in ``out`` if given)."""
+        (oq_kv_append).  Returns Q~ bf16 [T, H d] (in ``out`` if given; a
+        contiguous bf16 Q will do)."""
         dev = self.dev
         if stream is not None or dev != _cur_device():
             with _placed(dev, stream):
@@ -1119,8 +1121,8 @@ class KVCache:
 
     def attend(self, Q, table, length, q_start, max_q, slots=None, want_lse=False, out=None, stream=None):
         """Causal attention of the new tokens' Q (bf16 [T, H d], :meth:`append`'s) over
-        the cache that holds them (oq_kv_attend).  Returns O bf16 [T, H d], with
-        ``want_lse`` (O, LSE [H, T])."""
+        the cache that holds them (oq_kv_attend).  Returns O bf16 [T, H d] (in ``out`` if
+        given; a contiguous Q will do), with ``want_lse`` (O, LSE [H, T])."""
         dev = self.dev
         if stream is not None or dev != _cur_device():
             with _placed(dev, stream):

@@ -60,7 +60,7 @@ def test_linear_rejects():
     for name in ("x", "h", "z", "w", "ws", "hw", "zw", "Y"):
         assert lin(**{name: None}) == INVALID and lin(**{name: ODD}) == INVALID
     assert lin(B=ODD) == INVALID and lin(y_dt=5) == INVALID and lin(n=-1) == INVALID
-    assert lin(n=2 ** 22 + 1) == UNSUPPORTED
+    assert lin(n=2 ** 22 + 1) == UNSUPPORTED and lin(n=2 ** 22, c_out=2 ** 16 + 1) == UNSUPPORTED
     assert pack(c_out=0, codes=None) == OK
     assert lin(n=0, x=None) == OK and lin(c_out=0, w=None) == OK
 

@@ -565,3 +565,16 @@ def test_rows_past_32_bits():
     _, _, c, hh, zz = oq.rmsnorm_quant(y, gain, 8)
     _, _, c1, h1, z1 = oq.rmsnorm_quant(y[tail].clone(), gain, 8)
     assert torch.equal(c[tail], c1) and torch.equal(hh[tail], h1) and torch.equal(zz[tail], z1)
+
+
+def test_cache_drops_twice():
+    """Dropped, filled a little and dropped again, never below the page before the furthest."""
+    d, P = 64, 32
+    b = Batch(1, 2, 2, d, P, 400, seed=12)
+    b.step([124])
+    for to, new in ((70, 5), (64, 3), (66, 40), (97, 1), (96, 33)):
+        b.len[0] = to
+        for p in b.k + b.v:
+            p.rows = p.rows[:to]
+        b.step([new])
+        b.check_rows()
