@@ -703,7 +703,8 @@ oq_status oq_rope_table(int64_t n_pos, int head_dim, float base, float* tab, hip
  *            32 c + 16 (e / 4) + 4 g + e % 4
  *   K window [page][d];  V window [page/32][d/16][g][r][8]: channel 16 j + r, tokens
  *            as in V codes
- * head_dim 64 or 128; page 32, 64 or 128. */
+ * head_dim 64 or 128; page 32, 64 or 128; kv_heads at most 32768 and heads, a multiple
+ * of kv_heads, at most 131072. */
 typedef struct {
   int n_pages, n_slots, page, kv_heads, head_dim;
   int8_t* k_codes;                 /* [n_pages, kv_heads, page * head_dim]             */

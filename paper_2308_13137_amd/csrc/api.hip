@@ -2240,6 +2240,7 @@ CacheArgs cache_args(const oq_kv_cache* c, const oq_kv_batch* b) {
   a.lgP = c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
   a.Hkv = c->kv_heads;
   a.d = c->head_dim;
+  a.lgd = c->head_dim == 64 ? 6 : 7;
   a.table = b->table;
   a.slot = b->slot;
   a.length = b->length;
@@ -2252,8 +2253,8 @@ CacheArgs cache_args(const oq_kv_cache* c, const oq_kv_batch* b) {
 }
 
 oq_status check_heads(const oq_kv_cache* c, int heads) {
-  OQ_REQ(heads > 0 && heads % c->kv_heads == 0, "heads=%d must be a multiple of kv_heads=%d", heads,
-         c->kv_heads);
+  OQ_REQ(heads > 0 && heads <= (1 << 17) && heads % c->kv_heads == 0,
+         "heads=%d must be a multiple of kv_heads=%d, at most 131072", heads, c->kv_heads);
   return OQ_OK;
 }
 

@@ -61,10 +61,10 @@ OQ_DEV Seq seq_of(const CacheArgs& c, int i) {
 // the sequences, as (sequence, its unit); (-1, 0) past the last.  By every wave for
 // itself.  Batches whose grid of n_seq times the longest sequence's units is no
 // larger than the units' bound, or small, are numbered directly instead (a search
-// costs some 4 us: 15 chunks of up to 152 tokens 27 us, searched 32).  With 63
+// costs some 4 us: 15 chunks of up to 152 tokens 26 us, searched 30).  With 63
 // decoding sequences beside a prompt of 4,096 tokens at 64 heads the empty
 // workgroups of the direct grid took most of the time: attention 2,340 us, searched
-// 390; the append 154 and 49.
+// 390; the append 790 and 43.
 struct Unit {
   int i, k;
 };
@@ -143,16 +143,16 @@ template <typename TI>
 OQ_DEV void append_queries(const CacheArgs& c, const Seq& s, const RowIn<TI>& in, int H, const float* rope,
                            int64_t n_rope, const float* sa, uint16_t* Qout, int lo, int hi, int slice, int slices) {
   constexpr int U = 4;
-  const int d = c.d, half = d / 2, q4 = half / 4, G = H / c.Hkv, per = H * q4;
-  const int64_t items = int64_t(hi - lo) * per, step = int64_t(slices) * blockDim.x;
-  for (int64_t e0 = int64_t(slice) * blockDim.x + threadIdx.x; e0 < items; e0 += U * step) {
+  const int d = c.d, half = d / 2, lq = c.lgd - 3, G = H / c.Hkv;
+  const int items = ((hi - lo) * H) << lq, step = slices * int(blockDim.x);      // (below 2^28: H <= 2^17)
+  for (int e0 = slice * int(blockDim.x) + int(threadIdx.x); e0 < items; e0 += U * step) {
     float x[U][4], y[U][4];
     int64_t at[U];
     int sc[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      const int64_t e = min(e0 + k * step, items - 1);     // (past the end: the last one, not stored)
-      const int row = int(e / per), hh = int(e % per) / q4, p = 4 * int(e % q4), pos = lo + row;
+      const int e = min(e0 + k * step, items - 1);         // (past the end: the last one, not stored)
+      const int row = (e >> lq) / H, hh = (e >> lq) - row * H, p = 4 * (e & ((1 << lq) - 1)), pos = lo + row;
       const int64_t t = int64_t(s.b) + (pos - s.L);
       turned4(in.q + t * in.ldq + int64_t(hh) * d, rope, n_rope, pos, p, half, x[k], y[k]);
       at[k] = (t * H + hh) * d + p;
@@ -180,7 +180,10 @@ OQ_DEV void append_queries(const CacheArgs& c, const Seq& s, const RowIn<TI>& in
 // One workgroup takes one page's worth of one sequence's new tokens: the keys and
 // values of one head (blockIdx.y < kv heads), or a slice of the queries.  A thread
 // takes channels p .. p + 3 and p + d/2 .. of a head's row at a time.  HBM-bound for
-// prompts (each row read once, written once); for decoding a few loads deep.  A
+// prompts (each row read once, written once: two prompts of up to 4,096 tokens and
+// ten single ones, 64 heads, float32, 84 us, 99 with all of it read back, 4.1 TB/s);
+// for decoding a few loads deep (8 sequences, 32 heads, 7 us; 63, 6 us where no page
+// fills up).  A
 // page that fills up is gathered in LDS, the keys as rows, the values in the
 // window's operand order, so that its codes are written in whole 16-byte pieces.
 template <typename TI>
@@ -208,20 +211,20 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
       Qout[int64_t(s.b) * wide + e] = 0x7fc0;
     return;
   }
-  const int pg0 = s.L / P, pg = pg0 + un.k, end = s.L + s.n;
+  const int pg0 = s.L >> c.lgP, pg = pg0 + un.k, end = s.L + s.n;
   const int lo = max(s.L, pg * P), hi = min(end, (pg + 1) * P);
   if (lo >= hi) return;
   if (slice >= 0) {
     append_queries(c, s, in, H, rope, n_rope, sa, Qout, lo, hi, slice, slices);
     return;
   }
-  const int last = (end - 1) / P;
+  const int last = (end - 1) >> c.lgP;
   const int64_t win = int64_t(P) * d;
   auto window = [&](uint16_t* w, int page) { return w + ((int64_t(s.slot) * 2 + (page & 1)) * c.Hkv + u) * win; };
   const bool full = hi == (pg + 1) * P;
   uint16_t* sk = reinterpret_cast<uint16_t*>(s_page);
   uint16_t* sv = sk + P * d;
-  const bool old_rows = s.L % P != 0;
+  const bool old_rows = (s.L & (P - 1)) != 0;
   if (full && un.k == 0 && old_rows) {
     // the page's rows from before the call (with whatever lies behind them: the new
     // rows overwrite that)
@@ -277,11 +280,11 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
   // one of the last two.  A later page of the same half as the first must wait until
   // the first one's old rows are read: the first page's workgroup writes it.
   const bool keep = pg >= last - 1 && !(un.k > 0 && old_rows && ((pg - pg0) & 1) == 0);
-  const int q4 = half / 4;
+  const int lq = c.lgd - 3, q4 = 1 << lq;
   for (int e = tid; e < (hi - lo) * 2 * q4; e += AT) {
-    const int pos = lo + e / (2 * q4), p = 4 * (e % q4);
+    const int pos = lo + (e >> (lq + 1)), p = 4 * (e & (q4 - 1));
     uint2 a, b;
-    const bool key = (e / q4) & 1;
+    const bool key = (e >> lq) & 1;
     const int r = pos - pg * P;
     if (key) key_row(pos, p, a, b);
     else value_row(pos, p, a, b);
@@ -307,8 +310,8 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
       if ((page - pg0) & 1) continue;
       const int a0 = page * P, b0 = min(end, a0 + P);
       for (int e = tid; e < (b0 - a0) * 2 * q4; e += AT) {
-        const int pos = a0 + e / (2 * q4), p = 4 * (e % q4);
-        const bool key = (e / q4) & 1;
+        const int pos = a0 + (e >> (lq + 1)), p = 4 * (e & (q4 - 1));
+        const bool key = (e >> lq) & 1;
         uint2 a, b;
         if (key) key_row(pos, p, a, b);
         else value_row(pos, p, a, b);
@@ -367,15 +370,15 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
   };
   uint4* kd = reinterpret_cast<uint4*>(c.kc + blk * win);
   uint4* vd = reinterpret_cast<uint4*>(c.vc + blk * win);
-  const int dk = d / 64, dv = d / 32;
+  const int lk = c.lgd - 6, lv = c.lgd - 5;                // 64- and 32-channel pieces of a row
   for (int e = tid; e < P * d / 16; e += AT) {
     const int ln = e & 63, f = e >> 6, r = ln & 15, g = ln >> 4;
     // keys: piece (16-token tile, 64-channel half, g, r)
-    const uint4* ks = &s_page[((f / dk) * 16 + r) * (d / 8) + (f % dk) * 8 + 2 * g];
+    const uint4* ks = &s_page[((f >> lk) * 16 + r) * (d / 8) + (f & ((1 << lk) - 1)) * 8 + 2 * g];
     const uint2 k0 = codes8(ks[0], rk), k1 = codes8(ks[1], rk);
     kd[e] = make_uint4(k0.x, k0.y, k1.x, k1.y);
     // values: piece (32-token chunk, 32 channels, g, r), two channels of eight tokens
-    const uint4* vs = &s_page[P * d / 8 + ((f / dv) * (d / 16) + 2 * (f % dv)) * 64 + ln];
+    const uint4* vs = &s_page[P * d / 8 + ((f >> lv) * (d / 16) + 2 * (f & ((1 << lv) - 1))) * 64 + ln];
     const uint2 v0 = codes8(vs[0], rv), v1 = codes8(vs[64], rv);
     vd[e] = make_uint4(v0.x, v0.y, v1.x, v1.y);
   }
@@ -383,14 +386,15 @@ __global__ __launch_bounds__(512) void cache_append_kernel(CacheArgs c, RowIn<TI
 
 // ------------------------------------------------------------------ read
 // One workgroup: one head of 32 tokens of a sequence (a chunk lies in one page):
-// its operand pieces to rows in LDS, then to the output.
+// its operand pieces to rows in LDS, then to the output (the batch above 15 us, the
+// rate of a copy; 8 sequences' single rows 7 us, a few loads deep).
 template <typename TO>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int32_t* __restrict__ begin,
                                                          const int32_t* __restrict__ row_start, int64_t rows,
                                                          int max_rows, TO* __restrict__ K, TO* __restrict__ V,
                                                          bool direct) {
   __shared__ float s_x[32][132];
-  const int u = blockIdx.y, d = c.d, tid = threadIdx.x;
+  const int u = blockIdx.y, d = c.d, tid = threadIdx.x, lk = c.lgd - 6;
   // rows b .. e - 1 of sequence j, from its position `first` on
   int64_t first, b, e;
   auto range = [&](int j) {
@@ -412,7 +416,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int3
   if (b >= e || at0 >= e) return;
   const int64_t total = int64_t(s.L) + s.n, win = int64_t(c.P) * d;
   const bool ok = s.ok && begin[i] >= 0 && t0 < total;
-  const int pg = ok ? int(t0 / c.P) : 0, tin = ok ? int(t0 % c.P) : 0;
+  const int pg = ok ? int(t0 >> c.lgP) : 0, tin = ok ? int(t0) & (c.P - 1) : 0;
   const bool full = ok && int64_t(pg + 1) * c.P <= total;
   const int id = full ? page_of(c, i, pg) : -1;
   const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
@@ -431,7 +435,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int3
         for (int k = 0; k < 16; ++k) {
           const float x = float(int8_t(w[k >> 2] >> (8 * (k & 3)))) * h;
           if (kv) s_x[16 * ((k >> 2) & 1) + 4 * g + (k & 3)][32 * f + 16 * (k >> 3) + r] = x;
-          else s_x[16 * (f / (d / 64)) + r][64 * (f % (d / 64)) + 16 * g + k] = x;
+          else s_x[16 * (f >> lk) + r][64 * (f & ((1 << lk) - 1)) + 16 * g + k] = x;
         }
       }
     } else if (ok) {
@@ -443,13 +447,13 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int3
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           if (kv) s_x[16 * (k >> 2) + 4 * g + (k & 3)][16 * f + r] = x[k];
-          else s_x[p / (d / 8)][8 * (p % (d / 8)) + k] = x[k];
+          else s_x[p >> (c.lgd - 3)][8 * (p & (d / 8 - 1)) + k] = x[k];
         }
       }
     }
     __syncthreads();
     for (int p = tid; p < 32 * d / 8; p += 256) {
-      const int t = p / (d / 8), ch = 8 * (p % (d / 8));
+      const int t = p >> (c.lgd - 3), ch = 8 * (p & (d / 8 - 1));
       const int64_t pos = t0 + t, row = at0 + t;
       if (pos < first || row < b || row >= e) continue;
       float x[8];
@@ -1239,9 +1243,9 @@ hipError_t cache_append(const CacheArgs& c, const void* Q, int64_t ldq, const vo
                         const void* V, int64_t ldv, bool in_bf16, int H, const float* rope, int64_t n_rope,
                         const float* s_a, uint16_t* Qout, hipStream_t st) {
   // 512 threads where the pages' workgroups are few (a page that fills up is then a
-  // long walk: 26 us against 35 for 11 sequences of 142 tokens at one key head),
-  // 256 where they fill the card (91 us against 100 for twelve chunks of up to 4096
-  // float32 tokens at 64 heads).  Query slices: eight items of a thread each.
+  // long walk: 25 us against 33 for 11 sequences of 142 tokens at one key head),
+  // 256 where they fill the card (29 us against 33 for four chunks of up to 325
+  // tokens at 32 key heads).  Query slices: eight items of a thread each.
   // Pages: of the longest sequence times n_seq, or, where that is less, what T tokens
   // in at most min(n_seq, T) sequences can touch.
   const int64_t grid_pages = ((int64_t(c.max_q) + c.P - 2) / c.P + 1) * c.n_seq;

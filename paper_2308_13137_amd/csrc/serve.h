@@ -43,7 +43,7 @@ struct CacheArgs {
   int8_t *kc, *vc;          // [n_pages, Hkv, P d] operand order
   float *ks, *vs;           // [n_pages, Hkv]
   uint16_t *kw, *vw;        // [n_slots, 2, Hkv, P d] bf16 windows
-  int n_pages, n_slots, P, lgP, Hkv, d;   // P = 2^lgP
+  int n_pages, n_slots, P, lgP, Hkv, d, lgd;   // P = 2^lgP, d = 2^lgd
   const int32_t* table;     // [n_seq, max_pages]
   const int32_t* slot;      // [n_seq] | nullptr: the sequence's number
   const int32_t* length;    // [n_seq] tokens before the call
