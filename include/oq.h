@@ -690,7 +690,8 @@ oq_status oq_rope_table(int64_t n_pos, int head_dim, float base, float* tab, hip
 /* A paged key/value cache in 8 bits.  A sequence's token t is row t % page of
  * its page t / page.  A full page is int8 codes with one step per page, head and
  * tensor: the symmetric 8-bit quantiser over the block's page * head_dim values,
- * h = max(max|x| / 127, 1e-5), code = rint(x * (1/h)).  The open page and the one
+ * h = max(max|x| / 127, 1e-5), code = rint(x * (1/h)); a step of 0 (never written)
+ * stands for zeros.  The open page and the one
  * before it are bf16 rows in the sequence's window (page p in half p % 2).  A
  * page is quantised from its bf16 rows when it fills up, so its codes do not
  * depend on how its tokens arrived; the newest tokens can be dropped by lowering

@@ -2259,7 +2259,7 @@ oq_status check_heads(const oq_kv_cache* c, int heads) {
 }
 
 AttendPlan attend_plan(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
-  if (b->n_seq == 0 || b->max_q == 0) return AttendPlan{16, 0, 1, 1, 0, true, 0, 0};
+  if (b->n_seq == 0 || b->max_q == 0) return AttendPlan{16, 0, 1, 1, 0, 0, 0, 0, 0};
   return cache_attend_plan(b->n_seq, c->kv_heads, heads, b->tokens, b->max_q, int64_t(b->max_pages) * c->page,
                            c->head_dim);
 }

@@ -61,7 +61,8 @@ struct AttendPlan {
   int tile_rows;   // rows of a workgroup of the tile kernel (64, 128; 0: not used)
   int few, many;   // splits of a row's tokens in the two
   int64_t units;   // row tiles of one key head, of all sequences, at most
-  bool direct;     // numbered as n_seq times those of the longest sequence
+  int order;       // how they are numbered, with levels (kv_cache.hip, row_tile)
+  int64_t levels;
   size_t few_floats, many_floats;  // their shares in the workspace
 };
 AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d);

@@ -578,3 +578,57 @@ def test_cache_drops_twice():
             p.rows = p.rows[:to]
         b.step([new])
         b.check_rows()
+
+
+@pytest.mark.parametrize("before,counts,H,Hkv", [
+    ([300, 0, 130, 64], [200, 333, 1, 70], 2, 2),             # levels that several sequences share
+    ([0, 640, 5], [129, 257, 0], 10, 2),                      # an empty one; tiles that begin inside a token
+    ([1000, 0], [150, 140], 1, 1),                            # no level in common
+    ([33 * (i % 7) for i in range(32)], [40 + 13 * (i % 11) for i in range(32)], 4, 1),
+])
+def test_attend_longest_first(before, counts, H, Hkv):
+    b = Batch(len(counts), H, Hkv, 64, 32, 1400, seed=len(counts), s_a=False)
+    if any(before):
+        b.step(before, attend=False)
+    b.step(counts)
+
+
+def test_longest_first_entries_that_do_not_fit():
+    """A chunk longer than the table's pages, a length beyond them: NaN, the others as without them."""
+    d, P, H = 64, 32, 2
+    counts = [200, 150, 300, 170]
+    qs = [0, 200, 350, 650, 820]
+    x = rand(8, 820, 3 * H * d, dtype=BF)
+
+    def run(bad):
+        cache = oq.KVCache(32, P, H, d, 4)
+        table = torch.arange(32, dtype=torch.int32, device="cuda").view(4, 8)
+        length = i32([0, 2 ** 31 - 1 if bad else 9, 0, 50])   # the third one's 300 tokens pass 8 pages of 32
+        args = (table, length, i32(qs), 300)
+        w = H * d
+        q = cache.append(x[:, :w], x[:, w:2 * w], x[:, 2 * w:], *args)
+        return q, cache.attend(q, *args)
+
+    (q0, o0), (q1, o1) = run(False), run(True)
+    for q, o in ((q0, o0), (q1, o1)):
+        assert torch.isnan(q[350:650].float()).all() and torch.isnan(o[350:650].float()).all()
+        assert torch.isfinite(o[:200].float()).all() and torch.isfinite(o[650:].float()).all()
+    assert torch.isfinite(o0[200:350].float()).all() and torch.isnan(o1[200:350].float()).all()
+    keep = [*range(200), *range(650, 820)]
+    assert torch.equal(o0[keep], o1[keep])
+
+
+@pytest.mark.parametrize("n,H", [(1, 2), (3, 2), (70, 1), (150, 2)])
+def test_attend_pages_never_written(n, H):
+    """Zeroed pages before the new tokens: keys and values of zero."""
+    d, P, L = 64, 32, 96
+    cache = oq.KVCache(8, P, 1, d, 1)
+    x = rand(n, n, (H + 2) * d, dtype=BF)
+    args = (torch.arange(8, dtype=torch.int32, device="cuda").view(1, 8), i32([L]), i32([0, n]), n)
+    q = cache.append(x[:, :H * d], x[:, H * d:(H + 1) * d], x[:, (H + 1) * d:], *args)
+    o = cache.attend(q, *args)
+    k, v = ref.PlainCache(P, 1, d), ref.PlainCache(P, 1, d)
+    for c, at in ((k, H), (v, H + 1)):
+        c.add(torch.cat([torch.zeros(L, d, dtype=BF), x[:, at * d:(at + 1) * d].cpu()]).view(L + n, 1, d))
+    r, tol, _ = ref.attend64(q.cpu().view(n, H, d), k.values(), v.values(), L)
+    assert ((f64(o).view(n, H, d) - r).abs() <= tol).all()
