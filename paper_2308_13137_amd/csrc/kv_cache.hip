@@ -552,19 +552,22 @@ struct Window {
     k = c.kw + at;
     v = reinterpret_cast<const u32x4_t*>(c.vw + at) + ln;
   }
-  OQ_DEV u32x4_t key(int a, int ks, unsigned& bad) const {
-    const int r = lane & 15, g = lane >> 4, tok = 16 * a + r;
-    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(k + tok * DH + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1));
+  // operands as they lie there: keys 16 a + r, channels of k-step ks; values 16 j + r
+  OQ_DEV u32x4_t key(int a, int ks) const {
+    const int r = lane & 15, g = lane >> 4;
+    return *reinterpret_cast<const u32x4_t*>(k + (16 * a + r) * DH + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1));
+  }
+  OQ_DEV u32x4_t value(int j) const { return v[64 * j]; }
+  OQ_DEV void check_key(u32x4_t w, int a, unsigned& bad) const {
+    const int tok = 16 * a + (lane & 15);
     bool inf = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       inf = inf || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
     if (inf && tok < left) bad |= 1u << tok;
-    return w;
   }
-  OQ_DEV u32x4_t value(int j, unsigned& bad) const {
+  OQ_DEV u32x4_t check_value(u32x4_t w, unsigned& bad) const {
     const int g = lane >> 4;
-    u32x4_t w = v[64 * j];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int tok = 16 * (e >> 2) + 4 * g + (e & 3);
@@ -823,9 +826,16 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void cache_attend_kernel(Cache
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) kf[a][k] = __builtin_bit_cast(bf16x8_t, win.key(a, k, bad));
+      for (int k = 0; k < KS; ++k) kf[a][k] = __builtin_bit_cast(bf16x8_t, win.key(a, k));
 #pragma unroll
-    for (int j = 0; j < JD; ++j) vf[j] = __builtin_bit_cast(bf16x8_t, win.value(j, bad));
+    for (int j = 0; j < JD; ++j) vf[j] = __builtin_bit_cast(bf16x8_t, win.value(j));
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) win.check_key(__builtin_bit_cast(u32x4_t, kf[a][k]), a, bad);
+#pragma unroll
+    for (int j = 0; j < JD; ++j)
+      vf[j] = __builtin_bit_cast(bf16x8_t, win.check_value(__builtin_bit_cast(u32x4_t, vf[j]), bad));
     bad = wave_or(bad);
     const Step sp[1] = {step_of(step_parts(sc, 1.0f), vref)};
 #pragma unroll
@@ -936,8 +946,8 @@ OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int
 // operands once, in LDS, a tile ahead; the raw codes of the one after are in
 // flight meanwhile.  Bound by the vector units (softmax, conversion: busy some two
 // thirds of the time, the matrix units one third), two workgroups to a compute
-// unit: two chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 208 us,
-// 635 TFLOP/s; 4,096 tokens at 64 heads 330 us, 830 TFLOP/s.
+// unit: two chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 202 us,
+// 655 TFLOP/s; 4,096 tokens at 64 heads 330 us, 830 TFLOP/s.
 //
 // Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
@@ -952,6 +962,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
   constexpr int KS = DH / 32, JD = DH / 16, QW = 64 * R;
   constexpr int TILE = 64 * DH / 8;                      // 16-byte pieces of one operand's tile
   constexpr int CW = 2, LPW = JD / CW;                   // waves of a chunk, loads of a wave
+  static_assert(LPW == KS, "half a chunk's keys are one 16-token tile");
   __shared__ u32x4_t s_k[2][TILE], s_v[2][TILE];
   __shared__ float4 s_step[2][2];                        // [buffer][chunk], step_parts
   __shared__ unsigned s_bad[2][2][CW];
@@ -1024,7 +1035,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
                : -1;
   };
   int idn = id_of(k0);
-  auto load = [&](int t) {                               // tile t, if its chunk is in a full page
+  auto load = [&](int t) __attribute__((always_inline)) {   // tile t, if its chunk is in a full page
     const int t0 = 64 * t + 32 * cc, id = page_in(c, __builtin_amdgcn_readfirstlane(idn));
     if (t0 < closed) {
       const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
@@ -1048,7 +1059,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
   };
   // Operands of tile t into buffer b, fragment f of a chunk (64 lanes) at 64 f: f16,
   // or bf16 where the tile reaches into the open page (from ntc on).
-  auto store = [&](int t, int b) {
+  auto store = [&](int t, int b) __attribute__((always_inline)) {
     const int t0 = 64 * t + 32 * cc;
     u32x4_t* dst = (vals ? s_v[b] : s_k[b]) + cc * JD * 64 + lane;
     if (t0 < closed) {
@@ -1063,15 +1074,25 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
       }
       steps(b);
     } else {
-      // one operand at a time (past every row's limit zeros, any finite operands)
+      // (past every row's limit zeros, any finite operands)
       unsigned bad = 0;
-      const Window<DH> win(c, s, u, min(t0, max(seen - 1, 0) / 32 * 32), total, lane);
-      const bool in = t0 < seen;
+      if (t0 < seen) {
+        const Window<DH> win(c, s, u, t0, total, lane);
 #pragma unroll 1
-      for (int f = 0; f < 2 * LPW; ++f) {
-        u32x4_t w = {0u, 0u, 0u, 0u};
-        if (in) w = vals ? win.value(f, bad) : win.key(f / KS, f % KS, bad);
-        dst[64 * f] = w;
+        for (int half = 0; half < 2; ++half) {
+          u32x4_t w[LPW];
+#pragma unroll
+          for (int j = 0; j < LPW; ++j) w[j] = vals ? win.value(LPW * half + j) : win.key(half, j);
+#pragma unroll
+          for (int j = 0; j < LPW; ++j) {
+            if (vals) w[j] = win.check_value(w[j], bad);
+            else win.check_key(w[j], half, bad);
+            dst[64 * (half * LPW + j)] = w[j];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int f = 0; f < 2 * LPW; ++f) dst[64 * f] = u32x4_t{0u, 0u, 0u, 0u};
       }
       bad = wave_or(bad);
       if (lane == 0) {
@@ -1086,7 +1107,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     if (k0 + 1 < k1) load(k0 + 1);
   }
   // OPEN: the tile reaches into the open page; the weights enter as pairs of bf16 terms.
-  auto tile = [&](int t, auto open) {
+  auto tile = [&](int t, auto open) __attribute__((always_inline)) {
     constexpr bool OPEN = decltype(open)::value;
     const int b = (t - k0) & 1, t0 = 64 * t;
     __syncthreads();                                     // tile t is in buffer b, the other is free
