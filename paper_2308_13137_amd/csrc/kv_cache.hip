@@ -1354,8 +1354,12 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
 // How a call is cut up, from its sizes alone.  Rows of a key head: up to 32 go to
 // the row kernel, more to the tile kernel; a batch of prompts and decoding
 // sequences (tokens well below n_seq * max_q) runs both, each on its own.
-// Splits of the tokens: as many as give 1024 workgroups of the row kernel, which
-// streams the codes.  Tiles of 128 rows are bound by arithmetic, and 512 workgroups
+// Splits of the tokens: as many as fill the card once with the row kernel, three
+// workgroups of 16 rows to a compute unit or two of 32, to the nearest (against 1024
+// rounded up: one row of 8 heads over 131,072 tokens 53 -> 49 us, four rows 62 -> 53,
+// 16 sequences of four over up to 4,096 33 -> 26; rounded down, 64 sequences of up to
+// 8,192 102 -> 107); 1024 where it has only a ragged batch's shorter sequences (8 of up
+// to 48 tokens 154 -> 130).  Tiles of 128 rows are bound by arithmetic, and 512 workgroups
 // are all that run at once (4 times as many: 119 -> 145 us for 512 rows a head over
 // 32768 tokens, the join's traffic); tiles of 64 rows wait for memory like the row
 // kernel and lengths are ragged, so 1536 (200 -> 126 us for 35 sequences of up to 27
@@ -1367,7 +1371,8 @@ AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_
   p.tile_rows = rows <= 32 ? 0 : rows <= 64 ? 64 : 128;
   p.row_rows = rows <= 16 ? 16 : rows <= 32 || mixed ? 32 : 0;
   auto cut = [](int64_t want, int64_t most) { return int(std::max<int64_t>(1, std::min(want, most))); };
-  p.few = p.row_rows ? cut((1024 + heads - 1) / heads, std::min<int64_t>(128, max_len / 256)) : 1;
+  const int64_t fit = p.tile_rows ? 1024 : p.row_rows == 16 ? 768 : 512;
+  p.few = p.row_rows ? cut((fit + heads / 2) / heads, std::min<int64_t>(128, max_len / 256)) : 1;
   p.units = 0;
   p.order = BY_PLACE;
   p.levels = 0;

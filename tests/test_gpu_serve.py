@@ -632,3 +632,26 @@ def test_attend_pages_never_written(n, H):
         c.add(torch.cat([torch.zeros(L, d, dtype=BF), x[:, at * d:(at + 1) * d].cpu()]).view(L + n, 1, d))
     r, tol, _ = ref.attend64(q.cpu().view(n, H, d), k.values(), v.values(), L)
     assert ((f64(o).view(n, H, d) - r).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("n,H,before", [(1, 4, 200), (7, 2, 40), (40, 2, 70), (150, 2, 33), (150, 2, 0)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_attend_queries_that_are_not_finite(n, H, before, bad):
+    """One head's query with a value that is not finite: that row is NaN, the others are as without it."""
+    d, P = 64, 32
+    cache = oq.KVCache(8, P, 1, d, 1)
+    x = rand(before, before + n, (H + 2) * d, dtype=BF)
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(1, 8)
+    for at, m in ((0, before), (before, n)):
+        if m:
+            r = x[at:at + m]
+            args = (table, i32([at]), i32([0, m]), m)
+            q = cache.append(r[:, :H * d], r[:, H * d:(H + 1) * d], r[:, (H + 1) * d:], *args)
+    clean = cache.attend(q, *args).view(n, H, d)
+    row, head = n // 2, H - 1
+    q.view(n, H, d)[row, head, 11] = bad
+    got = cache.attend(q, *args).view(n, H, d)
+    assert torch.isnan(got[row, head].float()).all()
+    keep = torch.ones(n, H, dtype=torch.bool, device="cuda")
+    keep[row, head] = False
+    assert torch.equal(got[keep], clean[keep])
