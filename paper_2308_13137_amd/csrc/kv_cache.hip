@@ -699,9 +699,10 @@ OQ_DEV void put4(const Out& o, int row, int64_t t, int64_t hd, int DH, int ch, f
 // softmax of its own, the four are joined in LDS and the splits by a second kernel.
 //   S^T = K Q^T: a lane holds query row r, tokens 4 g + 0..3 of both 16-token
 //   tiles, which is the B operand of O^T = V^T P^T as it stands.
-// HBM-bound: 131,072 tokens x 8 key heads 50 us (5.3 TB/s), 256 sequences of up to
-// 1,024 tokens x 32 heads 218 us (5.1 TB/s; 254 with two waves to a SIMD, 302 with
-// loads that stay in the caches as well).  Sequences with more rows are the tile
+// HBM-bound: 131,072 tokens x 8 key heads 44 us (6.1 TB/s, some from the last-level
+// cache), 64 sequences of up to 8,192 x 8 heads 100 us (5.1 TB/s).  Three waves to a
+// SIMD and loads past the caches: 256 sequences of up to 1,024 x 32 heads took 218 us,
+// 254 with two waves, 302 without either.  Sequences with more rows are the tile
 // kernel's.
 template <int DH, int R>
 __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void cache_attend_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
@@ -945,9 +946,9 @@ OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int
 // 16 R per wave, over tiles of 64 tokens.  The waves turn a tile's codes into f16
 // operands once, in LDS, a tile ahead; the raw codes of the one after are in
 // flight meanwhile.  Bound by the vector units (softmax, conversion: busy some two
-// thirds of the time, the matrix units one third), two workgroups to a compute
-// unit: two chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 202 us,
-// 655 TFLOP/s; 4,096 tokens at 64 heads 330 us, 830 TFLOP/s.
+// thirds of the time, the matrix units one third, with two waves on every SIMD), two workgroups to a compute
+// unit: two chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 199 us,
+// 665 TFLOP/s; 4,096 tokens at 64 heads 330 us, 830 TFLOP/s.
 //
 // Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
