@@ -595,7 +595,9 @@ hipError_t int8_linear(const I8Args& a, bool y_bf16, hipStream_t st) {
   //   (4,096 x 4,096, 64 tokens: 32 x 32 9.0, 64 x 32 10.9, 64 x 64 14.5; 256
   //   tokens: 28.7, 19.8, 14.7 and 128 x 64 20.6; 5,120 x 13,824, 256 tokens: 128 x
   //   64 52, 128 x 128 36, 256 x 256 63): small tiles split K over more waves and
-  //   larger ones read the operands fewer times; two 128 x 128 workgroups fit a
+  //   larger ones read the operands fewer times (the K halves in two groups of waves
+  //   also with 128 x 64: 384 tokens of 4,096 x 4,096 20.6 -> 19.0, of 11,008 x 4,096
+  //   46 -> 42; rings one or two stages deeper or shallower: no gain); two 128 x 128 workgroups fit a
   //   compute unit with rings of two stages (8,192 x 28,672, 256 tokens: 90
   //   against 123 by 256 x 256 tiles);
   //   256 x 256 tiles beyond (1,024 tokens, 4,096 x 11,008: 61 against 75)
@@ -603,7 +605,7 @@ hipError_t int8_linear(const I8Args& a, bool y_bf16, hipStream_t st) {
   if (tiles(32, 32) <= 256) launch_ring<2, 2, 2, 1, 4, 4>(a, y_bf16, st);
   else if (tiles(64, 32) <= 256) launch_ring<4, 2, 2, 2, 2, 4>(a, y_bf16, st);
   else if (tiles(64, 64) <= 256) launch_ring<4, 4, 2, 2, 2, 4>(a, y_bf16, st);
-  else if (tiles(128, 64) <= 256) launch_ring<8, 4, 4, 2, 1, 4>(a, y_bf16, st);
+  else if (tiles(128, 64) <= 256) launch_ring<8, 4, 4, 2, 2, 3>(a, y_bf16, st);
   else if (tiles(128, 128) <= 256) launch_ring<8, 8, 2, 4, 1, 4>(a, y_bf16, st);
   else if (tiles(128, 128) <= 512) launch_ring<8, 8, 2, 4, 1, 2>(a, y_bf16, st);   // two per compute unit
   else {
