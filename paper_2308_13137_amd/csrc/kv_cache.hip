@@ -1355,6 +1355,9 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
 // How a call is cut up, from its sizes alone.  Rows of a key head: up to 32 go to
 // the row kernel, more to the tile kernel; a batch of prompts and decoding
 // sequences (tokens well below n_seq * max_q) runs both, each on its own.
+// Rows of a tile: 128 where such tiles, split into pieces of 512 tokens, are more than
+// the 512 workgroups that run at once, else 64 (a prompt of 512 tokens at 32 heads
+// 23 -> 17 us, of 1,024 38 -> 29, but 256 tokens over 8,192 62 -> 71).
 // Splits of the tokens: as many as fill the card once with the row kernel, three
 // workgroups of 16 rows to a compute unit or two of 32, to the nearest (against 1024
 // rounded up: one row of 8 heads over 131,072 tokens 53 -> 49 us, four rows 62 -> 53,
@@ -1362,14 +1365,16 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
 // 8,192 102 -> 107); 1024 where it has only a ragged batch's shorter sequences (8 of up
 // to 48 tokens 154 -> 130).  Tiles of 128 rows are bound by arithmetic, and 512 workgroups
 // are all that run at once (4 times as many: 119 -> 145 us for 512 rows a head over
-// 32768 tokens, the join's traffic); tiles of 64 rows wait for memory like the row
-// kernel and lengths are ragged, so 1536 (200 -> 126 us for 35 sequences of up to 27
+// 32768 tokens, the join's traffic); 64 rows or fewer wait for memory like the row
+// kernel's and lengths are ragged, so 1536 (200 -> 126 us for 35 sequences of up to 27
 // tokens at 4 key heads of 8, up to 16741 long; 252 -> 136 us for 8 of 48, up to 16384).
 AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d) {
   const int64_t rows = int64_t(max_q) * (H / Hkv), heads = int64_t(n_seq) * Hkv;
   const bool mixed = n_seq > 1 && 4 * tokens < 3 * int64_t(n_seq) * max_q;
   AttendPlan p;
-  p.tile_rows = rows <= 32 ? 0 : rows <= 64 ? 64 : 128;
+  // (a double: sizes that are refused later must not wrap here)
+  const double wide = double((rows + 127) / 128) * double(heads) * double(std::max<int64_t>(1, max_len / 512));
+  p.tile_rows = rows <= 32 ? 0 : rows <= 64 || wide <= 512 ? 64 : 128;
   p.row_rows = rows <= 16 ? 16 : rows <= 32 || mixed ? 32 : 0;
   auto cut = [](int64_t want, int64_t most) { return int(std::max<int64_t>(1, std::min(want, most))); };
   const int64_t fit = p.tile_rows ? 1024 : p.row_rows == 16 ? 768 : 512;
@@ -1383,11 +1388,11 @@ AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_
     const int64_t most = tokens * G / p.tile_rows + std::min<int64_t>(n_seq, tokens * G / (p.row_rows + 1));
     p.levels = std::max(max_len * G, rows) / p.tile_rows + 1;   // (a chunk that does not fit counts from 0)
     if (n_seq > 1 && n_seq <= 32 && rows > p.tile_rows && p.levels <= (1 << 24)) p.order = BY_LEVEL;
-    else if (grid > most && grid * Hkv > 1024) p.order = BY_SEARCH;
+    else if (grid > most && grid > 1024 / Hkv) p.order = BY_SEARCH;
     p.units = p.order == BY_PLACE ? grid : std::min(grid, most);
   }
   const int64_t tiles = p.units * Hkv;
-  p.many = tiles ? cut((p.tile_rows == 64 ? 1536 : 512) / tiles, std::min<int64_t>(64, max_len / 512)) : 1;
+  p.many = tiles ? cut((rows <= 64 ? 1536 : 512) / tiles, std::min<int64_t>(64, max_len / 512)) : 1;
   p.few_floats = p.few > 1 ? size_t(p.few) * size_t(heads) * size_t(p.row_rows) * size_t(d + 2) : 0;
   p.many_floats = p.many > 1 ? size_t(p.many) * size_t(tiles) * size_t(p.tile_rows) * size_t(d + 2) : 0;
   return p;

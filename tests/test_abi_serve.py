@@ -135,9 +135,12 @@ def test_attend_rejects_and_sizes():
     big = batch(n_seq=4096, max_pages=4096, max_q=1, tokens=4096)
     assert L.oq_kv_attend_workspace_size(C.byref(cache()), C.byref(big), 64, C.byref(m)) == OK and m.value < 1 << 30
     assert L.oq_kv_attend_workspace_size(C.byref(cache()), C.byref(b), 3, C.byref(n)) == INVALID
+    assert L.oq_kv_attend_workspace_size(C.byref(cache()), C.byref(b), 1 << 18, C.byref(n)) == INVALID
     assert L.oq_kv_attend_workspace_size(C.byref(cache()), C.byref(b), 4, None) == INVALID
     huge = batch(n_seq=65535, max_q=2 ** 20, tokens=2 ** 30)
     assert attend(None, huge, heads=64, lq=8192) == UNSUPPORTED
+    huge = batch(n_seq=65535, max_q=2 ** 30, tokens=2 ** 31 - 1, max_pages=2 ** 24)
+    assert attend(None, huge, heads=1 << 17, lq=1 << 24) == UNSUPPORTED
 
 
 def test_read_and_table_reject():

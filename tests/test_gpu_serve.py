@@ -133,6 +133,11 @@ def test_linear_every_tile(T, N, K):
     check_linear(T, K, N, BF if K == 208 else F32, bias=K == 144, seed=K)
 
 
+@pytest.mark.parametrize("T,K", [(200, 1040), (193, 2064), (256, 48)])
+def test_linear_several_token_tiles(T, K):
+    check_linear(T, K, 8190, BF, bias=True, seed=T)
+
+
 @pytest.mark.parametrize("T", [1, 40, 300])
 @pytest.mark.parametrize("top,zspread", [(3, 0.0), (15, 5.0), (63, 1000.0), (255, 30000.0)])
 def test_linear_widths_and_far_zero_points(T, top, zspread):
@@ -655,3 +660,13 @@ def test_attend_queries_that_are_not_finite(n, H, before, bad):
     keep = torch.ones(n, H, dtype=torch.bool, device="cuda")
     keep[row, head] = False
     assert torch.equal(got[keep], clean[keep])
+
+
+@pytest.mark.parametrize("d,H,Hkv,before,counts", [(128, 4, 4, [0], [400]), (64, 8, 2, [0, 70], [129, 33]),
+                                                   (128, 10, 2, [30], [65]), (64, 1, 1, [1100, 1], [90, 200])])
+def test_attend_short_prompts(d, H, Hkv, before, counts):
+    """Prompts too few to fill the card in tiles of 128 rows."""
+    b = Batch(len(counts), H, Hkv, d, 64, 1300, seed=d + H, s_a=False)
+    if any(before):
+        b.step(before, attend=False)
+    b.step(counts)
