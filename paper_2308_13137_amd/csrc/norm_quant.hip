@@ -49,15 +49,22 @@ __global__ __launch_bounds__(NTH) void norm_quant_kernel(
   const int nch = int(D / 8);
   const bool quant = bits < 16;
   const float qmax = quant ? float((1 << bits) - 1) : 0.0f;
-  float gn[CH][8], bs[CH][8];
+  // 1,024 threads have 128 registers each: gain and shift come from the caches per
+  // row there, and a row's loads wait for the row before (2,048 x 32,768 bf16 with
+  // both 141 us, 291 with everything held and spilled)
+  constexpr bool KEEP = NTH < 1024;
+  float gn[KEEP ? CH : 1][8], bs[KEEP ? CH : 1][8];
+  auto gains = [&](int k, int j) {
+    load8(gain + 8 * j, gn[k]);
+    if (bias) load8(bias + 8 * j, bs[k]);
+  };
+  if constexpr (KEEP) {
 #pragma unroll
-  for (int k = 0; k < CH; ++k) {
-    const int j = tid + NTH * k;
+    for (int k = 0; k < CH; ++k) {
+      const int j = tid + NTH * k;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) gn[k][e] = bs[k][e] = 0.0f;
-    if (j < nch) {
-      load8(gain + 8 * j, gn[k]);
-      if (bias) load8(bias + 8 * j, bs[k]);
+      for (int e = 0; e < 8; ++e) gn[k][e] = bs[k][e] = 0.0f;
+      if (j < nch) gains(k, j);
     }
   }
   Raw8<TX> nx[CH];
@@ -73,16 +80,17 @@ __global__ __launch_bounds__(NTH) void norm_quant_kernel(
       }
     }
   };
-  fetch(blockIdx.x);
+  if constexpr (KEEP) fetch(blockIdx.x);
   for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
     float v[CH][8], rv[CH][8];
     double ss = 0.0;
+    if constexpr (!KEEP) fetch(row);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       nx[k].get(v[k]);
       nr[k].get(rv[k]);
     }
-    fetch(row + gridDim.x);
+    if constexpr (KEEP) fetch(row + gridDim.x);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int j = tid + NTH * k;
@@ -113,11 +121,13 @@ __global__ __launch_bounds__(NTH) void norm_quant_kernel(
     for (int k = 0; k < CH; ++k) {
       const int j = tid + NTH * k;
       if (j < nch) {
+        const int kg = KEEP ? k : 0;
+        if constexpr (!KEEP) gains(kg, j);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] * rs * gn[k][e];
+        for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] * rs * gn[kg][e];
         if (bias) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] + bs[k][e];
+          for (int e = 0; e < 8; ++e) v[k][e] = v[k][e] + bs[kg][e];
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
