@@ -1365,7 +1365,9 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
 // 8,192 102 -> 107); 1024 where it has only a ragged batch's shorter sequences (8 of up
 // to 48 tokens 154 -> 130).  Tiles of 128 rows are bound by arithmetic, and 512 workgroups
 // are all that run at once (4 times as many: 119 -> 145 us for 512 rows a head over
-// 32768 tokens, the join's traffic); 64 rows or fewer wait for memory like the row
+// 32768 tokens, the join's traffic), or twice that where there are several sequences
+// of different lengths (18 chunks of up to 84 tokens over up to 5,318 116 -> 92, 8 of
+// 512 over up to 4,096 135 -> 147); 64 rows or fewer wait for memory like the row
 // kernel's and lengths are ragged, so 1536 (200 -> 126 us for 35 sequences of up to 27
 // tokens at 4 key heads of 8, up to 16741 long; 252 -> 136 us for 8 of 48, up to 16384).
 AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d) {
@@ -1392,7 +1394,7 @@ AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_
     p.units = p.order == BY_PLACE ? grid : std::min(grid, most);
   }
   const int64_t tiles = p.units * Hkv;
-  p.many = tiles ? cut((rows <= 64 ? 1536 : 512) / tiles, std::min<int64_t>(64, max_len / 512)) : 1;
+  p.many = tiles ? cut((rows <= 64 ? 1536 : n_seq > 1 ? 1024 : 512) / tiles, std::min<int64_t>(64, max_len / 512)) : 1;
   p.few_floats = p.few > 1 ? size_t(p.few) * size_t(heads) * size_t(p.row_rows) * size_t(d + 2) : 0;
   p.many_floats = p.many > 1 ? size_t(p.many) * size_t(tiles) * size_t(p.tile_rows) * size_t(d + 2) : 0;
   return p;
