@@ -691,7 +691,7 @@ oq_status oq_rope_table(int64_t n_pos, int head_dim, float base, float* tab, hip
  * its page t / page.  A full page is int8 codes with one step per page, head and
  * tensor: the symmetric 8-bit quantiser over the block's page * head_dim values,
  * h = max(max|x| / 127, 1e-5), code = rint(x * (1/h)); a step of 0 (never written)
- * stands for zeros.  The open page and the one
+ * stands for zeros, whatever the codes.  The open page and the one
  * before it are bf16 rows in the sequence's window (page p in half p % 2).  A
  * page is quantised from its bf16 rows when it fills up, so its codes do not
  * depend on how its tokens arrived; the newest tokens can be dropped by lowering
@@ -757,7 +757,8 @@ oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const
  * h / (heads / kv_heads).  Products on 16-bit matrix cores, sums and softmax
  * statistics fp32.  Codes are exact in bf16 and fp16; queries of more than 32 rows a
  * key head meet them as fp16 times a power of two of the row's (what is lost is
- * below 2^-39 of the row's largest entry).  A weight times its page's V step enters
+ * below 2^-39 of the row's largest entry, or 2^-110).  A step of 0 counts as 2^-60 in
+ * the scores (below 2^-25 for queries below 2^20).  A weight times its page's V step enters
  * as fp16, 11 bits, in units of 2^-15 of a power of two over every V step so far
  * (below 2^-40 of that it is lost), against the open page as two bf16 terms.
  *   Q   : bf16 [T, heads d], rows ld_q apart

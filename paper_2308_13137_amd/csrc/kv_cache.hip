@@ -604,10 +604,12 @@ OQ_DEV float row_sum(float v) { return over32(over16(v, true), true); }
 struct Step {
   float f, lw, winv;
 };
-// A page that was never written has steps of zero and stands for zeros: its steps
-// count as these, with which the smallest query factor leaves a masked score -inf
-// (times zero it would be NaN) and every weight vanishes as fp16.
-constexpr float KS_MIN = 9.5367431640625e-07f;           // 2^-20
+// A page that was never written has steps of zero and stands for zeros, whatever its
+// codes (a pool's pages are used again): its steps count as these.  A score of its codes
+// is at most 2^7 d |q| times that, below 2^-25 for queries below 2^20, while the smallest
+// query factor leaves a masked score -inf (times zero it would be NaN); every weight
+// vanishes as fp16.  (A branch that clears the codes cost the tile kernel 1 to 3%.)
+constexpr float KS_MIN = 8.6736173798840355e-19f;        // 2^-60
 constexpr float VS_MIN = 8.6736173798840355e-19f;        // 2^-60
 // `q` = (key step x scale, value step, its log2, its inverse); vr = vref, a power of two.
 OQ_DEV float4 step_parts(float ks_sc, float vs) {
@@ -952,7 +954,8 @@ OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int
 //
 // Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
-// 2^-39 of that entry.
+// 2^-39 of that entry.  (Of a row below 2^-71 what is lost is below 2^-110: a smaller
+// factor times KS_MIN would leave fp32.)
 template <int DH, int R>
 __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
                                                                        int64_t ldq, int H,
@@ -999,7 +1002,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(float(qf[h][k][e])));
-    const int e = min(max(int(__float_as_uint(row_max(top)) >> 23), 20), 253);
+    const int e = min(max(int(__float_as_uint(row_max(top)) >> 23), 56), 253);
     const float up = __uint_as_float(uint32_t(268 - e) << 23);   // 2^(14 - exponent)
     qs[h] = __uint_as_float(uint32_t(e - 14) << 23);
 #pragma unroll

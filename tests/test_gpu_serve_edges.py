@@ -1,0 +1,56 @@
+"""Calls at the edges of what the serving operators' header allows."""
+import pytest
+import torch
+
+from paper_2308_13137_amd import oq
+from tests import serve_ref as ref
+from tests.serve_ref import f64
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def rand(seed, *shape, scale=1.0, dtype=F32):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(dtype).cuda()
+
+
+def split(x, H, Hkv, d):
+    return x[:, :H * d], x[:, H * d:(H + Hkv) * d], x[:, (H + Hkv) * d:]
+
+
+# (new tokens, query heads of one key head): 16 and 32 rows of a workgroup, tiles of 64 rows (the first of
+# them with a full page and the open one in a tile) and of 128
+ROWS = [(1, 2), (3, 2), (9, 2), (5, 8), (70, 1), (150, 2)]
+
+
+# ------------------------------------------------------------------ steps of zero
+@pytest.mark.parametrize("n,H", ROWS)
+@pytest.mark.parametrize("which", ["k", "v", "kv"])
+def test_zero_steps_stand_for_zeros_whatever_the_codes(n, H, which):
+    """Pages whose steps are zero but whose codes are not (a pool's recycled pages): attention as over the
+    rows that KVCache.read returns, which are zeros."""
+    d, P, L = 64, 32, 96
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(1, 8)
+    args = (table, i32([L]), i32([0, n]), n)
+    x = rand(n, n, (H + 2) * d, dtype=BF)
+    x[:, :H * d] *= 16.0
+    c = oq.KVCache(8, P, 1, d, 1)
+    g = torch.Generator().manual_seed(7)
+    for name, codes, step in (("k", c.k_codes, c.k_scale), ("v", c.v_codes, c.v_scale)):
+        codes.copy_(torch.randint(-127, 128, codes.shape, generator=g).to(torch.int8))
+        step.fill_(0.02)
+        if name in which:
+            step[:3] = 0.0
+    q = c.append(*split(x, H, 1, d), *args)
+    o, lse = c.attend(q, *args, want_lse=True)
+    k, v = c.read(table, i32([0]), i32([L]), i32([0, n]), i32([0, L + n]), L + n, L + n, dtype=F32)
+    for name, t in (("k", k), ("v", v)):
+        assert (t[:L] == 0).all() == (name in which)
+    r, tol, rl = ref.attend64(q.cpu().view(n, H, d), k.cpu().view(-1, 1, d), v.cpu().view(-1, 1, d), L)
+    assert ((f64(o).view(n, H, d) - r).abs() <= tol).all()
+    assert ((f64(lse) - rl).abs() <= 1e-4 + 1e-5 * rl.abs()).all()
