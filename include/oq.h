@@ -638,7 +638,8 @@ oq_status oq_llama_block_forward(const oq_llama_desc* desc, const void* h0,
  * oq_rmsnorm_quant: the residual addition, RMSNorm and the per-token quantiser
  * of oq_act_fakequant_fwd in one pass.
  *   X [T, D] (x_dt); R [T, D] (r_dt) | NULL
- *   H [T, D] (x_dt) | NULL = X + R rounded to x_dt (needs R; may be X or R itself)
+ *   H [T, D] (x_dt) | NULL = X + R rounded to x_dt (needs R; may be X itself, or R if
+ *   r_dt = x_dt; any other overlap with them is refused)
  *   y = (H rstd) gain + bias,  rstd = 1 / sqrt(mean(H^2) + eps), of H as stored:
  *   the result equals the addition followed by a call without R
  *   gain [D] fp32, bias [D] fp32 | NULL (oq_let_absorb's outputs, or the norm's own)

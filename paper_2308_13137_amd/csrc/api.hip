@@ -2199,6 +2199,17 @@ oq_status oq_llama_calibrate(const oq_llama_desc* d, int n_samples, int epochs,
 // ------------------------------------------------------------------ serving operators
 namespace {
 
+// Whether n > 0 rows of `width` bytes, `ld` bytes apart, share a byte with the `bytes` at
+// `out`: such an output overwrites rows that other workgroups may still have to read.
+bool rows_meet(const void* rows, int64_t n, __int128 ld, __int128 width, const void* out, __int128 bytes) {
+  const __int128 lo = __int128(reinterpret_cast<uintptr_t>(out)) - __int128(reinterpret_cast<uintptr_t>(rows));
+  const __int128 hi = lo + bytes;
+  if (!rows || !out || hi <= 0 || lo >= (n - 1) * ld + width) return false;
+  if (lo < 0) return true;
+  const __int128 r = lo / ld;                                 // the row at or before out, and the next one
+  return lo < r * ld + width || (r + 1 < n && hi > (r + 1) * ld);
+}
+
 oq_status check_cache(const oq_kv_cache* c, const oq_kv_batch* b) {
   OQ_REQ(c && b, "cache and batch are required");
   if ((c->head_dim != 64 && c->head_dim != 128) || (c->page != 32 && c->page != 64 && c->page != 128))
@@ -2296,6 +2307,10 @@ oq_status oq_rmsnorm_quant(const void* X, oq_dtype x_dt, const void* R, oq_dtype
                         static_cast<const void*>(codes), static_cast<const void*>(h),
                         static_cast<const void*>(z)})
     OQ_REQ(aligned16(p), "pointers must be 16-byte aligned");
+  const __int128 row_x = D * esize(x_dt), row_r = D * esize(r_dt);
+  OQ_REQ(H == X || !rows_meet(X, T, row_x, row_x, H, T * row_x), "H may be X, but not overlap it otherwise");
+  OQ_REQ((H == R && x_dt == r_dt) || !rows_meet(R, T, row_r, row_r, H, T * row_x),
+         "H may be R where both have the same type, but not overlap it otherwise");
   const double n = double(T) * D;
   ProfScope ps(PK_OTHER, st,
                n * (esize(x_dt) * (H ? 2.0 : 1.0) + (R ? esize(r_dt) : 0) + (codes ? 1 : 0) +
