@@ -746,7 +746,8 @@ typedef struct {
  *   rope  : [n_rope, head_dim / 2, 2] (oq_rope_table) | NULL = no rotation; a position
  *           >= n_rope gives NaN
  *   s_a   : [kv_heads d] fp32 | NULL
- *   Q_out : bf16 [T, heads d], may be Q itself (bf16, ld_q = heads d) */
+ *   Q_out : bf16 [T, heads d], may be Q itself (bf16, ld_q = heads d); any other overlap
+ *   with Q, K or V is refused */
 oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,
                        const void* K, int64_t ld_k, const void* V, int64_t ld_v, oq_dtype in_dt,
                        int heads, const float* rope, int64_t n_rope, const float* s_a, void* Q_out,
@@ -763,7 +764,8 @@ oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const
  * as fp16, 11 bits, in units of 2^-15 of a power of two over every V step so far
  * (below 2^-40 of that it is lost), against the open page as two bf16 terms.
  *   Q   : bf16 [T, heads d], rows ld_q apart
- *   O   : bf16 [T, heads d], may be Q itself (ld_q = heads d)
+ *   O   : bf16 [T, heads d], may be Q itself (ld_q = heads d); any other overlap with Q
+ *   is refused
  *   LSE : fp32 [heads, T] | NULL: log-sum-exp of a row's logits in base 2, as
  *         oq_attention_fwd's
  * A row that sees a key or value that is not finite, or any token of a page that

@@ -2384,6 +2384,13 @@ oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const
   OQ_REQ(Q && K && V && Q_out, "Q, K, V and Q_out are required");
   OQ_REQ(aligned16(Q) && aligned16(K) && aligned16(V) && aligned16(rope) && aligned16(s_a) && aligned16(Q_out),
          "pointers must be 16-byte aligned");
+  const int64_t T = batch->tokens, es = esize(in_dt);
+  auto meets = [&](const void* in, int64_t ld, int64_t w) {
+    return rows_meet(in, T, __int128(ld) * es, __int128(w) * es, Q_out, __int128(T) * wq * 2);
+  };
+  OQ_REQ((Q_out == Q && in_dt == OQ_BF16 && (ld_q == wq || T == 1)) || !meets(Q, ld_q, wq),
+         "Q_out may be Q where that is bf16 with rows of heads * head_dim, but not overlap it otherwise");
+  OQ_REQ(!meets(K, ld_k, wk) && !meets(V, ld_v, wk), "Q_out must not overlap K or V");
   ProfScope ps(PK_OTHER, st, double(batch->tokens) * ((wq + 2.0 * wk) * esize(in_dt) + 2.0 * wq + 2.0 * wk));
   OQ_HIP(cache_append(cache_args(cache, batch), Q, ld_q, K, ld_k, V, ld_v, in_dt == OQ_BF16, heads, rope, n_rope,
                       s_a, static_cast<uint16_t*>(Q_out), st),
@@ -2410,6 +2417,10 @@ oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const
   if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
   OQ_REQ(Q && O, "Q and O are required");
   OQ_REQ(aligned16(Q) && aligned16(O) && aligned16(LSE) && aligned16(ws), "pointers must be 16-byte aligned");
+  const __int128 wide = 2 * int64_t(heads) * cache->head_dim;
+  OQ_REQ((O == Q && (2 * __int128(ld_q) == wide || batch->tokens == 1)) ||
+             !rows_meet(Q, batch->tokens, 2 * __int128(ld_q), wide, O, batch->tokens * wide),
+         "O may be Q where its rows are heads * head_dim, but not overlap it otherwise");
   const AttendPlan plan = attend_plan(cache, batch, heads);
   const int64_t rows = int64_t(batch->max_q) * (heads / cache->kv_heads);
   if (plan.tile_rows && (rows > (1 << 30) || plan.units * cache->kv_heads * plan.many >= (1 << 24)))
