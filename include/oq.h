@@ -770,7 +770,7 @@ oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const
  *         oq_attention_fwd's
  * A row that sees a key or value that is not finite, or any token of a page that
  * holds one, is NaN, and so is one with such a query; others are not touched by it.
- * (Values of the open page from 2^100 on may overflow fp32's range in the sums.)  The work of a row is split
+ * (Values from 2^100 on may overflow fp32's range in the sums.)  The work of a row is split
  * over its tokens where there are few rows, by a rule on (n_seq, heads, kv_heads,
  * tokens, max_q, max_pages * page) alone.  Workspace: oq_kv_attend_workspace_size. */
 oq_status oq_kv_attend_workspace_size(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads,

@@ -615,9 +615,15 @@ constexpr float VS_MIN = 8.6736173798840355e-19f;        // 2^-60
 OQ_DEV float4 step_parts(float ks_sc, float vs) {
   return make_float4(ks_sc, vs, __builtin_amdgcn_logf(vs), 1.0f / vs);
 }
-OQ_DEV Step step_of(float4 q, float vr) {
+// A full page's weights lie below 2^LW_MIN only where fp16 holds none of them: they stay
+// there (their exponential would leave fp32 with V steps far apart), so that the sum,
+// which takes the factor out again, has them all.  The open page's step is 1, its factor
+// 2^-106 at least, and its weights have to be what they are.
+constexpr float LW_MIN = -70.0f, WINV_MAX = 1.1805916207174113e+21f;
+OQ_DEV Step step_of(float4 q, float vr, bool full) {
   const float e = float(int(__float_as_uint(vr) >> 23) - 127 - 15);
-  return {q.x, q.z - e, q.w * (vr * (1.0f / WUNIT))};
+  const float lw = q.z - e, winv = q.w * (vr * (1.0f / WUNIT));
+  return {q.x, full ? fmaxf(lw, LW_MIN) : lw, full ? fminf(winv, WINV_MAX) : winv};
 }
 
 // A row's running softmax: m, the maximum of its logits in base 2 rounded up to an
@@ -780,7 +786,7 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void cache_attend_kernel(Cache
       cur.vs = fmaxf(cur.vs, VS_MIN);
       const float vr = fmaxf(vref, pow2_above(cur.vs));
       const float shrink = vref * pow2_inv(vr);
-      const Step sp[1] = {step_of(step_parts(cur.ks * sc, cur.vs), vr)};
+      const Step sp[1] = {step_of(step_parts(cur.ks * sc, cur.vs), vr, true)};
       bf16x8_t kf[2][KS];
 #pragma unroll
       for (int a = 0; a < 2; ++a)
@@ -840,7 +846,7 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void cache_attend_kernel(Cache
     for (int j = 0; j < JD; ++j)
       vf[j] = __builtin_bit_cast(bf16x8_t, win.check_value(__builtin_bit_cast(u32x4_t, vf[j]), bad));
     bad = wave_or(bad);
-    const Step sp[1] = {step_of(step_parts(sc, 1.0f), vref)};
+    const Step sp[1] = {step_of(step_parts(sc, 1.0f), vref, false)};
 #pragma unroll
     for (int h = 0; h < R; ++h) {
       if (bad && lim[h] >= t0 + __ffs(int(bad)) - 1) l[h] = NAN;
@@ -1166,7 +1172,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     const float vr = fmaxf(vref, fmaxf(pow2_above(q0.y), pow2_above(q1.y)));
     const float shrink = vref * pow2_inv(vr);
     vref = vr;
-    const Step s0 = step_of(q0, vr), s1 = step_of(q1, vr);
+    const Step s0 = step_of(q0, vr, !OPEN || t0 < closed), s1 = step_of(q1, vr, !OPEN);
     u32x4_t vf[AH];
 #pragma unroll
     for (int x = 0; x < AH; ++x) vf[x] = sv[64 * x];

@@ -54,3 +54,34 @@ def test_zero_steps_stand_for_zeros_whatever_the_codes(n, H, which):
     r, tol, rl = ref.attend64(q.cpu().view(n, H, d), k.cpu().view(-1, 1, d), v.cpu().view(-1, 1, d), L)
     assert ((f64(o).view(n, H, d) - r).abs() <= tol).all()
     assert ((f64(lse) - rl).abs() <= 1e-4 + 1e-5 * rl.abs()).all()
+
+
+# ------------------------------------------------------------------ values of very different sizes
+@pytest.mark.parametrize("n,H", ROWS)
+@pytest.mark.parametrize("big", [2.0 ** 60, 2.0 ** 90, 2.0 ** 96, 2.0 ** 118])
+@pytest.mark.parametrize("small", [0.0, 1e-4, 1.0])
+def test_value_steps_far_apart(n, H, big, small):
+    """One page of very large values, whose keys point away from every query, beside pages of small ones or
+    pages never written: every token counts in the log-sum-exp, and the output keeps the header's bound."""
+    d, P, L = 64, 32, 288
+    table = torch.arange(15, dtype=torch.int32, device="cuda").view(1, 15)
+    x = rand(n + H, L + n, (H + 2) * d, dtype=BF)
+    x[:, :H * d] *= 3.0
+    x[:, (H + 1) * d:] *= small if small else 1e-4
+    for at in range(0, H * d, d):
+        x[:, at] = 8.0
+    x[:, H * d] = 0.0
+    x[32:64, H * d] = -16.0                          # their scores are 16 lower
+    x[32:64, (H + 1) * d:] = rand(3, 32, d).clamp(-2, 2).mul(big / 2).to(BF)
+    c = oq.KVCache(15, P, 1, d, 1)
+    if small:
+        c.append(*split(x[:L], H, 1, d), table, i32([0]), i32([0, L]), L)
+    else:                                            # (the others' codes and steps stay zero)
+        c.append(*split(x[32:64], H, 1, d), table[:, 1:].contiguous(), i32([0]), i32([0, 32]), 32)
+    args = (table, i32([L]), i32([0, n]), n)
+    q = c.append(*split(x[L:], H, 1, d), *args)
+    o, lse = c.attend(q, *args, want_lse=True)
+    k, v = c.read(table, i32([0]), i32([L]), i32([0, n]), i32([0, L + n]), L + n, L + n, dtype=F32)
+    r, tol, rl = ref.attend64(q.cpu().view(n, H, d), k.cpu().view(-1, 1, d), v.cpu().view(-1, 1, d), L)
+    assert ((f64(lse) - rl).abs() <= 1e-4 + 1e-5 * rl.abs()).all()
+    assert ((f64(o).view(n, H, d) - r).abs() <= tol).all()
