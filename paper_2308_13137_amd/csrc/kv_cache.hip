@@ -687,9 +687,11 @@ OQ_DEV Out out_of(uint16_t* O, float* LSE, float* part, int splits, int split, i
                   int64_t unit, int unit_rows, int DH) {
   return {O, LSE, part, splits, H, T, (split * units + unit) * unit_rows, splits * units * unit_rows * DH};
 }
+// A row whose every score is -inf (an infinite query) is NaN, like its output 0 / 0.
+OQ_DEV float lse_of(float m, float l) { return l > 0.0f ? m + log2f(l) : NAN; }
 OQ_DEV void put_ml(const Out& o, int row, int64_t t, int64_t hd, float m, float l) {
   if (o.splits > 1) reinterpret_cast<float2*>(o.part + o.ml)[o.at + row] = make_float2(m, l);
-  else if (o.LSE) o.LSE[hd * o.T + t] = m + log2f(l);
+  else if (o.LSE) o.LSE[hd * o.T + t] = lse_of(m, l);
 }
 OQ_DEV void put4(const Out& o, int row, int64_t t, int64_t hd, int DH, int ch, float4 x, float l) {
   if (o.splits > 1) {
@@ -1313,7 +1315,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, Joi
   const int64_t t = int64_t(s.b) + j;
   *reinterpret_cast<uint2*>(O + (t * H + hd) * DH + 4 * lane) =
       make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
-  if (LSE && lane == 0) LSE[hd * c.T + t] = m + log2f(l);
+  if (LSE && lane == 0) LSE[hd * c.T + t] = lse_of(m, l);
 }
 
 }  // namespace

@@ -85,3 +85,26 @@ def test_value_steps_far_apart(n, H, big, small):
     r, tol, rl = ref.attend64(q.cpu().view(n, H, d), k.cpu().view(-1, 1, d), v.cpu().view(-1, 1, d), L)
     assert ((f64(lse) - rl).abs() <= 1e-4 + 1e-5 * rl.abs()).all()
     assert ((f64(o).view(n, H, d) - r).abs() <= tol).all()
+
+
+# ------------------------------------------------------------------ rows that are NaN
+@pytest.mark.parametrize("n,H,L", [(1, 2, 96), (1, 2, 2100), (9, 2, 96), (70, 1, 96), (70, 1, 2100), (150, 2, 33)])
+def test_log_sum_exp_of_a_row_that_is_nan(n, H, L):
+    """An infinite query against keys of one sign: every score is -inf, output and log-sum-exp are NaN."""
+    d, P = 64, 32
+    pages = -(-(L + n) // P)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, pages)
+    x = rand(n, L + n, (H + 2) * d, dtype=BF)
+    x[:, H * d + 5] = 1.0
+    c = oq.KVCache(pages, P, 1, d, 1)
+    c.append(*split(x[:L], H, 1, d), table, i32([0]), i32([0, L]), L)
+    args = (table, i32([L]), i32([0, n]), n)
+    q = c.append(*split(x[L:], H, 1, d), *args)
+    clean, clean_lse = c.attend(q, *args, want_lse=True)
+    q.view(n, H, d)[n // 2, H - 1, 5] = -float("inf")
+    o, lse = c.attend(q, *args, want_lse=True)
+    bad = torch.zeros(n, H, dtype=torch.bool, device="cuda")
+    bad[n // 2, H - 1] = True
+    assert torch.isnan(o.view(n, H, d)[bad].float()).all() and torch.isnan(lse.t()[bad]).all()
+    assert torch.equal(o.view(n, H, d)[~bad], clean.view(n, H, d)[~bad])
+    assert torch.equal(lse.t()[~bad], clean_lse.t()[~bad])
