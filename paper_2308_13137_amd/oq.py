@@ -1161,6 +1161,6 @@ class KVCache:
         k = table.new_empty((rows, self.kv_heads * self.head_dim), dtype=dtype)
         v = torch.empty_like(k)
         _check(lib().oq_kv_read(C.byref(self.desc), C.byref(b), _arg(begin, "begin", _I32, (n,), dev),
-                                _arg(row_start, "row_start", _I32, (n + 1,), dev), rows, max_rows, k.data_ptr(),
-                                v.data_ptr(), _dt(k), _raw_stream(dev)))
+                                _arg(row_start, "row_start", _I32, (n + 1,), dev), rows,
+                                min(max_rows, rows), k.data_ptr(), v.data_ptr(), _dt(k), _raw_stream(dev)))
         return k, v

@@ -108,3 +108,19 @@ def test_log_sum_exp_of_a_row_that_is_nan(n, H, L):
     assert torch.isnan(o.view(n, H, d)[bad].float()).all() and torch.isnan(lse.t()[bad]).all()
     assert torch.equal(o.view(n, H, d)[~bad], clean.view(n, H, d)[~bad])
     assert torch.equal(lse.t()[~bad], clean_lse.t()[~bad])
+
+
+# ------------------------------------------------------------------ bounds far above the batch
+@pytest.mark.parametrize("most", [70, 1 << 20, (1 << 31) - 1, 1 << 31, (1 << 32) + 1, 1 << 40])
+def test_read_with_a_bound_far_above_the_rows(most):
+    """max_rows is at least the largest number of rows: any larger one gives the same."""
+    d, P, n = 64, 32, 70
+    c = oq.KVCache(3, P, 1, d, 1)
+    x = rand(1, n, 3 * d, dtype=BF)
+    table = i32([[2, 0, 1]])
+    c.append(*split(x, 1, 1, d), table, i32([0]), i32([0, n]), n)
+    torch.full((2, n, d), 7.0, dtype=BF, device="cuda")      # (what an output's memory may hold)
+    k, v = c.read(table, i32([0]), i32([n]), i32([0, 0]), i32([0, n]), n, most)
+    k1, v1 = c.read(table, i32([0]), i32([n]), i32([0, 0]), i32([0, n]), n, n)
+    assert torch.equal(k, k1) and torch.equal(v, v1)
+    assert torch.equal(k[64:], x[64:, d:2 * d]) and torch.equal(v[64:], x[64:, 2 * d:])
