@@ -124,3 +124,50 @@ def test_read_with_a_bound_far_above_the_rows(most):
     k1, v1 = c.read(table, i32([0]), i32([n]), i32([0, 0]), i32([0, n]), n, n)
     assert torch.equal(k, k1) and torch.equal(v, v1)
     assert torch.equal(k[64:], x[64:, d:2 * d]) and torch.equal(v[64:], x[64:, 2 * d:])
+
+
+# ------------------------------------------------------------------ row ranges outside the batch
+@pytest.mark.parametrize("H", [1, 4])
+@pytest.mark.parametrize("starts,clean,ok,nan", [
+    ([0, 40, 300], [0, 40, 80], [(0, 40)], [(40, 80)]),      # past the batch's rows: those inside are NaN
+    ([-1, 40, 80], [0, 40, 80], [(40, 80)], [(0, 40)]),      # before them
+    ([0, 50, 40], None, [], [(0, 40)]),                      # longer than max_q: its first max_q rows; decreasing
+    ([0, 41, 60], [1, 41, 60], [(41, 60)], [(0, 40)]),
+])
+def test_row_ranges_outside_the_batch(H, starts, clean, ok, nan):
+    """Such a sequence is not cached and its rows inside the batch are NaN, in the queries, the output and the
+    log-sum-exp; its neighbour is as without it and rows of no sequence are left as they were."""
+    d, P, T = 64, 32, 80
+    x = rand(5, T, (H + 2) * d, dtype=BF)
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2)
+
+    def run(qs):
+        c = oq.KVCache(4, P, 1, d, 2)
+        q, o = (torch.full((T, H * d), 7.0, dtype=BF, device="cuda") for _ in range(2))
+        args = (table, i32([0, 0]), i32(qs), 40)
+        c.append(*split(x, H, 1, d), *args, out=q)
+        _, lse = c.attend(q, *args, want_lse=True, out=o)
+        return c, q, o, lse.t()
+
+    c, q, o, lse = run(starts)
+    left = torch.ones(T, dtype=torch.bool)
+    for a, b in nan:
+        left[a:b] = False
+        for t in (q, o, lse):
+            assert torch.isnan(t[a:b].float()).all()
+    for a, b in ok:
+        left[a:b] = False
+    assert (q[left] == 7).all() and (o[left] == 7).all()
+    if clean is None:
+        assert not c.k_window.any() and not c.v_window.any() and not c.k_scale.any() and not c.v_scale.any()
+        return
+    c1, q1, o1, lse1 = run(clean)
+    for a, b in ok:
+        for t, t1 in ((q, q1), (o, o1), (lse, lse1)):
+            assert torch.isfinite(t[a:b].float()).all() and torch.equal(t[a:b], t1[a:b])
+    good = 0 if ok[0][0] == 0 else 1
+    for t, t1 in ((c.k_window, c1.k_window), (c.v_window, c1.v_window)):
+        assert torch.equal(t[good], t1[good]) and not t[1 - good].any()
+    for t, t1 in ((c.k_codes, c1.k_codes), (c.v_codes, c1.v_codes), (c.k_scale, c1.k_scale), (c.v_scale, c1.v_scale)):
+        assert torch.equal(t[2 * good:2 * good + 2], t1[2 * good:2 * good + 2])
+        assert not t[2 * (1 - good):2 * (1 - good) + 2].any()
