@@ -171,3 +171,21 @@ def test_row_ranges_outside_the_batch(H, starts, clean, ok, nan):
     for t, t1 in ((c.k_codes, c1.k_codes), (c.v_codes, c1.v_codes), (c.k_scale, c1.k_scale), (c.v_scale, c1.v_scale)):
         assert torch.equal(t[2 * good:2 * good + 2], t1[2 * good:2 * good + 2])
         assert not t[2 * (1 - good):2 * (1 - good) + 2].any()
+
+
+# ------------------------------------------------------------------ few tokens, very many channels
+@pytest.mark.parametrize("T", [1, 16, 17])
+@pytest.mark.parametrize("K", [144, 1040])
+@pytest.mark.parametrize("N", [40001, 65553, 70000])
+def test_linear_few_tokens_over_very_many_channels(T, K, N):
+    """Tiles of 128 and 256 tokens that hold few: all of a tile's other rows repeat the last one."""
+    g = torch.Generator().manual_seed(T + K + N)
+    codes = torch.randint(0, 256, (T, K), generator=g).to(torch.uint8).cuda()
+    w = torch.randint(0, 256, (N, K), generator=g).to(torch.uint8).cuda()
+    z, zw = (torch.round(127 + 30 * torch.randn(m, generator=g)).cuda() for m in (T, N))
+    h, hw = (torch.rand(m, generator=g).cuda() * 0.01 + 1e-4 for m in (T, N))
+    packed, wsum = oq.int8_pack(w)
+    y = oq.int8_linear(codes, h, z, packed, wsum, hw, zw)
+    r = ref.linear64(codes, h, z, w, hw, zw, None)
+    # the integer sum rounded to fp32, h_x h_w, their product
+    assert ((f64(y) - r).abs() <= 3.01 * ref.F24 * r.abs()).all()
