@@ -633,6 +633,10 @@ oq_status oq_llama_block_forward(const oq_llama_desc* desc, const void* h0,
  * inputs and quantised keys and values), in the order a block runs them:
  *   oq_rmsnorm_quant -> oq_int8_linear (q, k, v) -> oq_kv_append ->
  *   oq_kv_attend -> oq_act_fakequant_fwd -> oq_int8_linear (o) -> oq_rmsnorm_quant ...
+ * Linear inputs and weights have the calibrated bit widths (codes of up to 8 bits, a
+ * byte each).  Attention does not have the calibration's quantiser: there Q, K and V are
+ * quantised per token, asymmetric, at the activation bits; here K and V are symmetric 8
+ * bits per page and head whatever those are, and Q stays bf16.
  * None of them allocates, and all can be captured into a graph.
  *
  * oq_rmsnorm_quant: the residual addition, RMSNorm and the per-token quantiser
@@ -699,6 +703,7 @@ oq_status oq_rope_table(int64_t n_pos, int head_dim, float base, float* tab, hip
  * `length`, back to the start of the page before the furthest page that the window
  * has held rows of (again and again, but never below that).  A page or window that
  * several sequences of one append write is a race; full pages may be shared by any.
+ * (A sequence that drops tokens of a page and fills it again writes that page.)
  * Layouts (lane = 16 g + r):
  *   K codes  [page/16][d/64][g][r][16]: token 16 a + r, channel 64 j + 16 g + b
  *   V codes  [page/32][d/32][g][r][2][8]: channel 32 j + 16 hh + r; element e: token
@@ -795,7 +800,8 @@ oq_status oq_kv_read(const oq_kv_cache* cache, const oq_kv_batch* batch, const i
  * forward, 11 attention backward, 12 the 8-bit linear, 13 the 8-bit cache's
  * attention.  oq_profile_read synchronises the
  * recorded events and returns launch count, total milliseconds and the
- * algorithmic work (FLOP for GEMMs, bytes for the others) of that kind.
+ * algorithmic work (FLOP for GEMMs, bytes for the others) of that kind; kind 13's is
+ * the bytes of Q and O alone, since the lengths are on the device: it gives no rate.
  */
 #define OQ_PROF_KINDS 14
 oq_status oq_profile_enable(int on);
