@@ -600,7 +600,11 @@ hipError_t int8_linear(const I8Args& a, bool y_bf16, hipStream_t st) {
   //   46 -> 42; rings one or two stages deeper or shallower: no gain); two 128 x 128 workgroups fit a
   //   compute unit with rings of two stages (8,192 x 28,672, 256 tokens: 90
   //   against 123 by 256 x 256 tiles);
-  //   256 x 256 tiles beyond (1,024 tokens, 4,096 x 11,008: 61 against 75)
+  //   256 x 256 tiles beyond (1,024 tokens, 4,096 x 11,008: 61 against 75).
+  //   Over very many channels few tokens take these tiles too: they wait for the
+  //   weight's bytes all the same up to 65,536 channels of 8,192 inputs (57,344: 1 to
+  //   64 tokens 91 to 101 us, the bytes alone 93); by 256 x 256 tiles 128,256 channels
+  //   take 221 us for one token and 251 to 259 for 4 to 128, the bytes alone 208.
   auto tiles = [&](int ch, int tok) { return ((a.N + ch - 1) / ch) * ((a.T + tok - 1) / tok); };
   if (tiles(32, 32) <= 256) launch_ring<2, 2, 2, 1, 4, 4>(a, y_bf16, st);
   else if (tiles(64, 32) <= 256) launch_ring<4, 2, 2, 2, 2, 4>(a, y_bf16, st);

@@ -64,7 +64,7 @@ OQ_DEV Seq seq_of(const CacheArgs& c, int i) {
 // costs some 4 us: 15 chunks of up to 152 tokens 26 us, searched 30).  With 63
 // decoding sequences beside a prompt of 4,096 tokens at 64 heads the empty
 // workgroups of the direct grid took most of the time: attention 2,340 us, searched
-// 390; the append 790 and 43.
+// 390; the append 786 and 45.
 struct Unit {
   int i, k;
 };
@@ -955,10 +955,12 @@ OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int
 // Many rows (prompts): one workgroup of four waves takes 64 R rows of one key head,
 // 16 R per wave, over tiles of 64 tokens.  The waves turn a tile's codes into f16
 // operands once, in LDS, a tile ahead; the raw codes of the one after are in
-// flight meanwhile.  Bound by the vector units (softmax, conversion: busy some two
-// thirds of the time, the matrix units one third, with two waves on every SIMD), two workgroups to a compute
-// unit: two chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 199 us,
-// 665 TFLOP/s; 4,096 tokens at 64 heads 330 us, 830 TFLOP/s.
+// flight meanwhile.  Two workgroups to a compute unit.  Neither unit is busy all the
+// time: over a whole launch the vector units (softmax, conversion) 50%, the matrix
+// units 27%, at 1.5 of 2 waves a SIMD, so a wave's products, softmax and products again
+// mostly follow one another, and a quarter of the wave slots is empty at the ends.  Two
+// chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 199 us, 665 TFLOP/s;
+// 4,096 tokens at 64 heads 330 us, 830 TFLOP/s.
 //
 // Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
@@ -1363,9 +1365,16 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
   return hipGetLastError();
 }
 
-// How a call is cut up, from its sizes alone.  Rows of a key head: up to 32 go to
-// the row kernel, more to the tile kernel; a batch of prompts and decoding
-// sequences (tokens well below n_seq * max_q) runs both, each on its own.
+// How a call is cut up, from its sizes alone (the lengths are on the device: a table
+// wider than they need makes the plan one for longer sequences; a prompt of 512 tokens
+// at 32 heads 17.6 us, 30.3 with a table eight times as wide, which takes 128-row tiles;
+// 8 sequences decoding at 1,000 tokens 11.2 and 12.4; 64 of them the same).
+// Rows of a key head: up to 32 go to the row kernel, more to the tile kernel; a batch of
+// prompts and decoding sequences (fewer tokens than three quarters of n_seq * max_q) runs
+// both, each on its own: of 16 sequences over 2,000 tokens with 64 or 1 new ones at 32
+// heads, 8 key heads, 84 -> 81 us at 63% of n_seq * max_q, 75 -> 61 at 51%, 66 -> 50 at 8%,
+// but 91 -> 97 at 88% (at 75% 86 and 84); 32 key heads 93 -> 96, 91 -> 89, 86 -> 82, 98
+// -> 113 (95 and 102).
 // Rows of a tile: 128 where such tiles, split into pieces of 512 tokens, are more than
 // the 512 workgroups that run at once, else 64 (a prompt of 512 tokens at 32 heads
 // 23 -> 17 us, of 1,024 38 -> 29, but 256 tokens over 8,192 62 -> 71).
@@ -1376,11 +1385,18 @@ hipError_t cache_read(const CacheArgs& c, const int32_t* begin, const int32_t* r
 // 8,192 102 -> 107); 1024 where it has only a ragged batch's shorter sequences (8 of up
 // to 48 tokens 154 -> 130).  Tiles of 128 rows are bound by arithmetic, and 512 workgroups
 // are all that run at once (4 times as many: 119 -> 145 us for 512 rows a head over
-// 32768 tokens, the join's traffic), or twice that where there are several sequences
-// of different lengths (18 chunks of up to 84 tokens over up to 5,318 116 -> 92, 8 of
-// 512 over up to 4,096 135 -> 147); 64 rows or fewer wait for memory like the row
+// 32768 tokens, the join's traffic), or twice that for several sequences, whose lengths
+// the host does not know.  Uneven ones gain (18 chunks of up to 84 tokens over up to 5,318
+// at 32 heads, 8 key heads, 176 -> 138 us; 8 of up to 512 over up to 4,096, 8 heads, 135
+// -> 112), equal ones lose 3 to 7% (8 of 512 over 4,096, 8 heads, 116 -> 123; 4 of 256
+// over 8,192 184 -> 190; 18 of 84 over 5,318, 16 heads, 140 -> 149); three times loses for
+// most.  64 rows or fewer wait for memory like the row
 // kernel's and lengths are ragged, so 1536 (200 -> 126 us for 35 sequences of up to 27
 // tokens at 4 key heads of 8, up to 16741 long; 252 -> 136 us for 8 of 48, up to 16384).
+// Smallest splits: 256 tokens for the row kernel (one row over 1,024 tokens, 32 heads, 8.9
+// us, with 512 10.7, with 128 8.7; 256 tokens 5.8 unsplit, 7.7 in two; over 2,048 to 16,384
+// within 15% either way), 512 for the tile kernel (512 tokens 17.4, with 256 24.7; 64 over
+// 4,096, 32 heads, 24.2 and 26.6, with 1,024 33.5; at 8 heads 22.0 and 18.2, 31.5).
 AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d) {
   const int64_t rows = int64_t(max_q) * (H / Hkv), heads = int64_t(n_seq) * Hkv;
   const bool mixed = n_seq > 1 && 4 * tokens < 3 * int64_t(n_seq) * max_q;

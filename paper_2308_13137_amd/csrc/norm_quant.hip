@@ -50,8 +50,10 @@ __global__ __launch_bounds__(NTH) void norm_quant_kernel(
   const bool quant = bits < 16;
   const float qmax = quant ? float((1 << bits) - 1) : 0.0f;
   // 1,024 threads have 128 registers each: gain and shift come from the caches per
-  // row there, and a row's loads wait for the row before (2,048 x 32,768 bf16 with
-  // both 141 us, 291 with everything held and spilled)
+  // row there, and a row's loads wait for the row before.  The row and its residual, raw
+  // and as fp32, still pass the 128: 10 (bf16) to 77 (fp32) registers spill, 44 to 248
+  // bytes a lane.  2,048 x 32,768 with both: bf16 146 us (3.2 TB/s; 291 with everything
+  // held), fp32 380 us (2.3 TB/s); every narrower kernel keeps all of it in registers.
   constexpr bool KEEP = NTH < 1024;
   float gn[KEEP ? CH : 1][8], bs[KEEP ? CH : 1][8];
   auto gains = [&](int k, int j) {

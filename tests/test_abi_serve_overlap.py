@@ -53,8 +53,8 @@ def test_attend_output_over_queries_still_to_be_read():
                   (4096, FAKE + 8192 + 1008), (4096, FAKE + 2 * 8192 - 16)):
         assert attend(None, long, lq=lq, Q=FAKE, O=O, ws=None) == INVALID, (lq, O)
     # the queries themselves; the gap between two rows; before and behind them
-    for lq, O in ((512, FAKE), (4096, FAKE + 1024), (4096, FAKE + 8192 - 3072), (4096, FAKE + 2 * 8192 + 1024),
-                  (512, FAKE - 3072), (512, FAKE + 3072)):
+    for lq, O in ((512, FAKE), (4096, FAKE + 1024), (4096, FAKE + 8192 - 3 * 1024), (4096, FAKE + 2 * 8192 + 1024),
+                  (512, FAKE - 3 * 1024), (512, FAKE + 3 * 1024)):
         assert attend(None, long, lq=lq, Q=FAKE, O=O, ws=None) == WORKSPACE, (lq, O)
     one = batch(n_seq=1, max_pages=512, max_q=1, tokens=1)       # a single row has no stride
     assert attend(None, one, lq=4096, Q=FAKE, O=FAKE, ws=None) == WORKSPACE
