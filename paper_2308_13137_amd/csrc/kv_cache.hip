@@ -648,15 +648,39 @@ OQ_DEV float softmax_step(f32x4_t (&st)[2 * NC], const Step (&sp)[NC], float& m,
   const float alpha = mn == m ? 1.0f : m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
   l *= alpha;
   m = mn;
+  float f[NC], less = off;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) f[c] = sp[c].f;
+  // From 2^12 on the maximum is subtracted from rounded products before the factor is
+  // added: in the one multiply-add below, lw - off would lose the factor's bits, and from
+  // 2^24 on the exact product may pass the rounded maximum and its weight fp16 (NaN).
+  // Rows that are not there keep their bits.  (It costs prompts 1 to 2%; a second
+  // run over the tokens in this form, only where it is needed, cost 10 to 50%, since the
+  // kernels then spill.)
+  if (__any(fabsf(off) >= 4096.0f)) {
+    const bool far = fabsf(off) >= 4096.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int a = 2 * c; a < 2 * c + 2; ++a)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float x = __fsub_rn(__fmul_rn(st[a][q], f[c]), off);
+          st[a][q] = far ? x : st[a][q];
+        }
+      f[c] = far ? 1.0f : f[c];
+    }
+    less = far ? 0.0f : off;
+  }
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const float e = sp[c].lw - off;
+    const float e = sp[c].lw - less;
     float w = 0.0f;
 #pragma unroll
     for (int a = 2 * c; a < 2 * c + 2; ++a)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        st[a][q] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[a][q], sp[c].f, e));
+        st[a][q] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[a][q], f[c], e));
         w += st[a][q];
       }
     l = __builtin_fmaf(w, sp[c].winv, l);
@@ -959,8 +983,8 @@ OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int
 // time: over a whole launch the vector units (softmax, conversion) 50%, the matrix
 // units 27%, at 1.5 of 2 waves a SIMD, so a wave's products, softmax and products again
 // mostly follow one another, and a quarter of the wave slots is empty at the ends.  Two
-// chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 199 us, 665 TFLOP/s;
-// 4,096 tokens at 64 heads 330 us, 830 TFLOP/s.
+// chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 204 us, 650 TFLOP/s;
+// 4,096 tokens at 64 heads, 8 key heads, 334 us, 823 TFLOP/s.
 //
 // Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below

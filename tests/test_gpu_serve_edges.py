@@ -189,3 +189,44 @@ def test_linear_few_tokens_over_very_many_channels(T, K, N):
     r = ref.linear64(codes, h, z, w, hw, zw, None)
     # the integer sum rounded to fp32, h_x h_w, their product
     assert ((f64(y) - r).abs() <= 3.01 * ref.F24 * r.abs()).all()
+
+
+# ------------------------------------------------------------------ very large scores
+@pytest.mark.parametrize("n,H", ROWS)
+@pytest.mark.parametrize("scale", [2.0 ** 8, 2.0 ** 12, 2.0 ** 20, 2.0 ** 40])
+@pytest.mark.parametrize("mode", ["above", "below", "below, then zero"])
+def test_scores_far_beyond_fp32s_integers(n, H, scale, mode):
+    """Keys c scale e_0 with whole c up to 127 and queries +-scale e_0: codes and products are exact, tokens of
+    the same c tie bit for bit and any other lies at least scale^2 / 8 below, so a row's output is the mean of
+    the values at its largest score.  What remains of the error: fp16 weights, the fp32 sums and a bf16 rounding."""
+    d, P, L = 64, 32, 288
+    T = L + n
+    g = torch.Generator().manual_seed(n + H)
+    c = torch.randint(1, 128, (T,), generator=g).float()
+    c[::P], c[7::P] = 127.0, 1.0
+    if mode == "below, then zero":
+        c[256:288] = 0.0
+    x = rand(n, T, (H + 2) * d)
+    x[:, :(H + 1) * d] = 0.0
+    for at in range(0, H * d, d):
+        x[:, at] = scale if mode == "above" else -scale
+    x[:, H * d] = c.cuda() * scale
+    x = x.to(BF)
+    pages = -(-T // P)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, pages)
+    cache = oq.KVCache(pages, P, 1, d, 1)
+    cache.append(*split(x[:L], H, 1, d), table, i32([0]), i32([0, L]), L)
+    args = (table, i32([L]), i32([0, n]), n)
+    q = cache.append(*split(x[L:], H, 1, d), *args)
+    o, lse = cache.attend(q, *args, want_lse=True)
+    k, v = cache.read(table, i32([0]), i32([L]), i32([0, n]), i32([0, T]), T, T, dtype=F32)
+    assert torch.equal(k[:, 0].cpu(), c * scale) and not k[:, 1:].any()
+    r, _, rl = ref.attend64(q.cpu().view(n, H, d), k.cpu().view(-1, 1, d), v.cpu().view(-1, 1, d), L)
+    best = c if mode == "above" else -c
+    for j in range(n):
+        top = best[:L + j + 1] == best[:L + j + 1].max()
+        w = v[:L + j + 1].cpu().double()[top]
+        assert (r[j] - w.mean(0)).abs().max() < 1e-12
+        tol = w.abs().mean(0) * (ref.F11 + 2 * T * ref.F24) * 1.01 + r[j].abs() * ref.BF8 * 1.01
+        assert ((f64(o[j]).view(H, d) - r[j]).abs() <= tol).all()
+    assert ((f64(lse) - rl).abs() <= 1e-4 + 1e-5 * rl.abs()).all()
