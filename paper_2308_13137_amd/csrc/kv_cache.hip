@@ -980,8 +980,8 @@ OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int
 // 16 R per wave, over tiles of 64 tokens.  The waves turn a tile's codes into f16
 // operands once, in LDS, a tile ahead; the raw codes of the one after are in
 // flight meanwhile.  Two workgroups to a compute unit.  Neither unit is busy all the
-// time: over a whole launch the vector units (softmax, conversion) 50%, the matrix
-// units 27%, at 1.5 of 2 waves a SIMD, so a wave's products, softmax and products again
+// time: over a whole launch the vector units (softmax, conversion) 49%, the matrix
+// units 26%, at 1.5 of 2 waves a SIMD, so a wave's products, softmax and products again
 // mostly follow one another, and a quarter of the wave slots is empty at the ends.  Two
 // chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 204 us, 650 TFLOP/s;
 // 4,096 tokens at 64 heads, 8 key heads, 334 us, 823 TFLOP/s.
