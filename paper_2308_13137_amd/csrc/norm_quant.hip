@@ -117,7 +117,18 @@ __global__ __launch_bounds__(NTH) void norm_quant_kernel(
     ss = s_sum[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) ss += s_sum[w];
-    const float rs = float(1.0 / sqrt(ss / double(D) + double(eps)));
+    const double rstd = 1.0 / sqrt(ss / double(D) + double(eps));
+    float rs = float(rstd);
+    // one that fp32 holds with fewer bits, or not at all (subnormal rows, eps 0): a power of
+    // two of it goes to the values first
+    if (!(rs >= 0x1p-126f && rs <= 0x1p126f)) {
+      const float k = rs < 1.0f ? 0x1p-64f : 0x1p64f;
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * k;
+      rs = float(rstd / double(k));
+    }
     float mx = -INFINITY, mn = INFINITY, bad = 0.0f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {

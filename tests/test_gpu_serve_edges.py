@@ -230,3 +230,26 @@ def test_scores_far_beyond_fp32s_integers(n, H, scale, mode):
         tol = w.abs().mean(0) * (ref.F11 + 2 * T * ref.F24) * 1.01 + r[j].abs() * ref.BF8 * 1.01
         assert ((f64(o[j]).view(H, d) - r[j]).abs() <= tol).all()
     assert ((f64(lse) - rl).abs() <= 1e-4 + 1e-5 * rl.abs()).all()
+
+
+# ------------------------------------------------------------------ norms at the ends of fp32
+@pytest.mark.parametrize("D", [64, 1032, 4096, 8200, 20480])
+@pytest.mark.parametrize("dtype,scale", [(BF, 2.0 ** 127), (F32, 2.0 ** 127), (F32, 2.0 ** 120), (BF, 2.0 ** -130),
+                                         (F32, 2.0 ** -126), (F32, 2.0 ** -140)])
+def test_norm_of_the_largest_and_smallest_values(D, dtype, scale):
+    """Rows whose 1 / rms is below fp32's normal numbers or above its largest: the same roundings as elsewhere
+    (rstd, its product with H, the product with the gain: half a step each)."""
+    g = torch.Generator().manual_seed(D)
+    X = ((torch.rand(3, D, generator=g) * 2 - 1) * scale).to(dtype).cuda()
+    X[1] = X[1] * 0.0
+    X[1, ::7] = scale                                   # (few large values, many zeros)
+    if scale == 2.0 ** 127:
+        X[2] = torch.finfo(dtype).max * X[2].sign()
+    gain = (torch.randn(D, generator=g) + 1.0).cuda()
+    eps = 1e-5 if scale > 1 else 0.0
+    _, y, _, _, _ = oq.rmsnorm_quant(X, gain, 16, eps=eps, dq_dtype=F32)
+    _, ry, ry0 = ref.norm64(X, None, gain, None, eps)
+    assert ((f64(y) - ry).abs() <= 3.1 * ref.F24 * ry0.abs()).all()
+    _, _, codes, h, z = oq.rmsnorm_quant(X, gain, 8, eps=eps)
+    _, rcodes, rh, rz = oq.act_fakequant_fwd(y, 8)
+    assert torch.equal(codes, rcodes) and torch.equal(h, rh) and torch.equal(z, rz)
