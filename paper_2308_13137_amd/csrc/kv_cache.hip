@@ -990,7 +990,12 @@ OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
 // 2^-39 of that entry.  (Of a row below 2^-71 what is lost is below 2^-110: a smaller
 // factor times KS_MIN would leave fp32.)
-template <int DH, int R>
+//
+// TWO: pages of 32 tokens, a tile's chunks lie in two pages.  A row's unit of the weights
+// is its own then: rows that see only the first chunk must not lose bits to the other
+// page's V step (two chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 210
+// -> 217 us).  Larger pages hold both chunks: one step and one unit for all rows.
+template <int DH, int R, bool TWO>
 __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
                                                                        int64_t ldq, int H,
                                                                        uint16_t* __restrict__ O,
@@ -1025,7 +1030,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
   float qs[R];
   int lim[R];                                            // the last token this lane's row sees
   f32x4_t acc[R][JD];
-  float m[R], l[R], vref = VREF0;
+  float m[R], l[R], vref[TWO ? R : 1];
   auto row_of = [&](int h) { return min(row0 + 16 * (R * wave + h) + r, rows - 1); };
 #pragma unroll
   for (int h = 0; h < R; ++h) {
@@ -1048,6 +1053,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     }
     m[h] = -INFINITY;
     l[h] = 0.0f;
+    vref[TWO ? h : 0] = VREF0;
 #pragma unroll
     for (int j = 0; j < JD; ++j) acc[h][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
@@ -1196,16 +1202,23 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
         if (bad1 && lim[h] >= t0 + 32 + __ffs(int(bad1)) - 1) l[h] = NAN;
       }
     }
-    const float4 q0 = s_step[b][0], q1 = s_step[b][1];
-    const float vr = fmaxf(vref, fmaxf(pow2_above(q0.y), pow2_above(q1.y)));
-    const float shrink = vref * pow2_inv(vr);
-    vref = vr;
-    const Step s0 = step_of(q0, vr, !OPEN || t0 < closed), s1 = step_of(q1, vr, !OPEN);
+    const float4 q0 = s_step[b][0], q1 = TWO ? s_step[b][1] : q0;
+    float shrink;
+    Step s0, s1;
+    auto unit = [&](float& vref, bool both) {
+      const float vr = fmaxf(vref, TWO && both ? fmaxf(pow2_above(q0.y), pow2_above(q1.y)) : pow2_above(q0.y));
+      shrink = vref * pow2_inv(vr);
+      vref = vr;
+      s0 = step_of(q0, vr, !OPEN || (TWO && t0 < closed));
+      s1 = TWO ? step_of(q1, vr, !OPEN) : s0;
+    };
+    if constexpr (!TWO) unit(vref[0], true);
     u32x4_t vf[AH];
 #pragma unroll
     for (int x = 0; x < AH; ++x) vf[x] = sv[64 * x];
 #pragma unroll
     for (int h = 0; h < R; ++h) {
+      if constexpr (TWO) unit(vref[h], lim[h] >= t0 + 32);
       Step sp[2] = {s0, s1};
       if constexpr (!OPEN) {
         sp[0].f *= qs[h];
@@ -1267,7 +1280,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, 
     const int64_t tok = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
 #pragma unroll
     for (int j = 0; j < JD; ++j) {
-      const f32x4_t o = acc[h][j] * (vref / WUNIT);
+      const f32x4_t o = acc[h][j] * (vref[TWO ? h : 0] / WUNIT);
       put4(out, row - row0, tok, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), l[h]);
     }
     if (g == 0) put_ml(out, row - row0, tok, hd, m[h], l[h]);
@@ -1460,11 +1473,16 @@ hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int 
     const dim3 grid(unsigned(p.few), unsigned(c.Hkv), unsigned(c.n_seq));
     hipLaunchKernelGGL((cache_attend_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, p.few);
   };
-  auto many = [&](auto dh, auto rr) {
+  auto many_of = [&](auto dh, auto rr, auto two) {
     constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
+    constexpr bool TWO = decltype(two)::value;
     const dim3 grid(unsigned(p.units * p.many * c.Hkv));
-    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws_many,
+    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R, TWO>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws_many,
                        p.many, p.row_rows + 1, int(p.units), p.order, int(p.levels));
+  };
+  auto many = [&](auto dh, auto rr) {
+    if (c.P == 32) many_of(dh, rr, std::true_type{});
+    else many_of(dh, rr, std::false_type{});
   };
   auto join = [&](auto dh, auto ng) {
     constexpr int DH = decltype(dh)::value, NG = decltype(ng)::value, RW = 1024 / (DH * NG);

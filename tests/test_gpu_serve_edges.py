@@ -253,3 +253,30 @@ def test_norm_of_the_largest_and_smallest_values(D, dtype, scale):
     _, _, codes, h, z = oq.rmsnorm_quant(X, gain, 8, eps=eps)
     _, rcodes, rh, rz = oq.act_fakequant_fwd(y, 8)
     assert torch.equal(codes, rcodes) and torch.equal(h, rh) and torch.equal(z, rz)
+
+
+# ------------------------------------------------------------------ what a row does not see
+@pytest.mark.parametrize("n,H", [(70, 1), (150, 2), (96, 8)])
+@pytest.mark.parametrize("P", [32, 64])
+@pytest.mark.parametrize("L", [0, 64, 96])
+@pytest.mark.parametrize("big", [2.0 ** 12, 2.0 ** 30, 2.0 ** 60])
+def test_later_values_do_not_touch_earlier_rows(n, H, P, L, big):
+    """A prompt whose values become very large from some page on: the rows before it are as accurate as if it
+    were not there."""
+    d = 64
+    x = rand(n + L, L + n, (H + 2) * d, dtype=BF)
+    at = -(-(L + 32) // P) * P                       # the first row of the large page
+    x[at:, (H + 1) * d:] *= big
+    pages = -(-(L + n) // P)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, pages)
+    c = oq.KVCache(pages, P, 1, d, 1)
+    if L:
+        c.append(*split(x[:L], H, 1, d), table, i32([0]), i32([0, L]), L)
+    args = (table, i32([L]), i32([0, n]), n)
+    q = c.append(*split(x[L:], H, 1, d), *args)
+    o, lse = c.attend(q, *args, want_lse=True)
+    k, v = c.read(table, i32([0]), i32([L]), i32([0, n]), i32([0, L + n]), L + n, L + n, dtype=F32)
+    m = at - L                                       # rows that do not see it
+    r, tol, rl = ref.attend64(q[:m].cpu().view(m, H, d), k[:at].cpu().view(-1, 1, d), v[:at].cpu().view(-1, 1, d), L)
+    assert ((f64(o[:m]).view(m, H, d) - r).abs() <= tol).all()
+    assert ((f64(lse[:, :m]) - rl).abs() <= 1e-4 + 1e-5 * rl.abs()).all()
