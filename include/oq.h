@@ -766,8 +766,9 @@ oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const
  * key head meet them as fp16 times a power of two of the row's (what is lost is
  * below 2^-39 of the row's largest entry, or 2^-110).  A step of 0 counts as 2^-60 in
  * the scores (below 2^-25 for queries below 2^20).  A weight times its page's V step enters
- * as fp16, 11 bits, in units of 2^-15 of a power of two over every V step so far
- * (below 2^-40 of that it is lost), against the open page as two bf16 terms.
+ * as fp16, 11 bits, in units of 2^-15 of a power of two over the V steps that the row
+ * has met so far (below 2^-40 of that it is lost), against the open page as two bf16
+ * terms.
  *   Q   : bf16 [T, heads d], rows ld_q apart
  *   O   : bf16 [T, heads d], may be Q itself (ld_q = heads d); any other overlap with Q
  *   is refused

@@ -980,11 +980,11 @@ OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int
 // 16 R per wave, over tiles of 64 tokens.  The waves turn a tile's codes into f16
 // operands once, in LDS, a tile ahead; the raw codes of the one after are in
 // flight meanwhile.  Two workgroups to a compute unit.  Neither unit is busy all the
-// time: over a whole launch the vector units (softmax, conversion) 49%, the matrix
+// time: over a whole launch the vector units (softmax, conversion) 48%, the matrix
 // units 26%, at 1.5 of 2 waves a SIMD, so a wave's products, softmax and products again
 // mostly follow one another, and a quarter of the wave slots is empty at the ends.  Two
-// chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 204 us, 650 TFLOP/s;
-// 4,096 tokens at 64 heads, 8 key heads, 334 us, 823 TFLOP/s.
+// chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 203 us, 652 TFLOP/s;
+// 4,096 tokens at 64 heads, 8 key heads, 339 us, 812 TFLOP/s.
 //
 // Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
 // largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
