@@ -794,6 +794,96 @@ oq_status oq_kv_read(const oq_kv_cache* cache, const oq_kv_batch* batch, const i
                      oq_dtype out_dt, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Drafted tokens (speculative decoding): several continuations of each sequence, a tree
+ * of them, go through the block at once, and the part that the block agrees with is
+ * kept.  A step, in place of oq_kv_append and oq_kv_attend:
+ *   ... -> oq_kv_append_tree -> oq_kv_attend_tree -> ... (every block) -> the logits ->
+ *   oq_token_probs -> oq_tree_verify -> oq_kv_commit (every block's cache);
+ *   then length[i] += count[i], and next[i] is the first node of the next tree.
+ * None of them allocates, and all can be captured into a graph.
+ *
+ * A sequence's new tokens in oq_kv_batch are its tree's nodes, at most a page's
+ * (max_q <= page, else OQ_ERR_UNSUPPORTED).  parent [T] int32 (device, 4-byte aligned, read
+ * when the kernels run): the node, counted within the sequence, that a node stands behind,
+ * an earlier one; -1 stands behind the sequence itself.  A sequence with any other entry
+ * does not fit, like those that oq_kv_batch names.
+ *
+ * oq_kv_append_tree: oq_kv_append for a tree: node j is turned as the token at position
+ * length + depth (the number of its ancestors), and its key and value go to row
+ * length + j of the window, as bf16.  No page is filled: codes and steps stay as they
+ * are until oq_kv_commit.  A step that is not committed leaves the cache as it was before
+ * (rows behind `length` mean nothing), but for how far tokens can be dropped: the
+ * window has then held rows up to length + nodes. */
+oq_status oq_kv_append_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* parent, const void* Q,
+                            int64_t ld_q, const void* K, int64_t ld_k, const void* V, int64_t ld_v, oq_dtype in_dt,
+                            int heads, const float* rope, int64_t n_rope, const float* s_a, void* Q_out,
+                            hipStream_t stream);
+
+/* oq_kv_attend_tree: oq_kv_attend for a tree: a node sees the sequence's `length` tokens, its
+ * ancestors and itself.  Pages that the sequence has filled are read as codes; what lies
+ * behind them, the open page's tokens and the tree, as bf16 rows of the window (so a node's
+ * output does not depend on nodes that it does not see, bit for bit but for rounding
+ * to the units that oq_kv_attend names).  Arguments, precision, rows that are NaN and the
+ * workspace rule as oq_kv_attend. */
+oq_status oq_kv_attend_tree_workspace_size(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads,
+                                           size_t* bytes);
+oq_status oq_kv_attend_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* parent, const void* Q,
+                            int64_t ld_q, int heads, void* O, float* LSE, void* ws, size_t ws_bytes,
+                            hipStream_t stream);
+
+/* oq_kv_commit: keeps part of each sequence's tree: node path[i, k] becomes the token at
+ * position length[i] + k for k < count[i], and a page that is filled by that becomes codes.
+ *   path  : int32 [n_seq, max_path] node numbers, ascending; entries from count[i] on are
+ *           not read
+ *   count : int32 [n_seq], 0 .. the tree's nodes
+ * `batch` is the append's (length before the tree).  For a path from a root down (a node
+ * without a parent, then a child each) the cache is then, bit for bit, what oq_kv_append of
+ * those tokens leaves, codes, steps and the window's rows up to length + count.  Of a
+ * sequence that does not fit (as in oq_kv_batch; a count or a path that is not as above)
+ * nothing is kept or moved. */
+oq_status oq_kv_commit(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* path, int max_path,
+                       const int32_t* count, hipStream_t stream);
+
+/* oq_token_probs: P[t, :] = softmax(logits[t, :] / temperature[t]).
+ *   logits [n_rows, vocab] (dt), rows ld apart; P fp32, rows ld_p apart, no overlap; both aligned
+ *   to their elements only; vocab at most 2^20 (else OQ_ERR_UNSUPPORTED)
+ *   temperature : fp32 [n_rows] | NULL (ones); 0 puts all of it on the first of the largest
+ *   logits
+ * A logit of -inf has probability 0.  A row with a NaN or +inf, one of -inf alone, and one whose
+ * temperature is negative or not finite is NaN. */
+oq_status oq_token_probs(const void* logits, oq_dtype dt, int64_t ld, int64_t n_rows, int64_t vocab,
+                         const float* temperature, float* P, int64_t ld_p, hipStream_t stream);
+
+/* oq_tree_verify: which of the drafted tokens are kept, and the token after them, such that
+ * the sequence of tokens is distributed as the target's.
+ *   q_start, parent : the trees, as above; node 0 of a tree is the token that is known
+ *           already (the last one drawn), and is kept; other nodes without a parent never are
+ *   token : int32 [tokens], the nodes' tokens (node 0's is not read; one outside
+ *           [0, vocab) is rejected)
+ *   P     : fp32 [tokens, vocab], rows ld_p apart: the target's distribution after each node
+ *   Q     : the same for the draft, from whose row of the parent a node's token was drawn |
+ *           NULL: the tokens were chosen without chance
+ *   replace : with Q: 1 if siblings were drawn independently, 0 if without replacement (in
+ *           the order of the nodes)
+ *   u     : fp32 [tokens], u_next fp32 [n_seq]: uniform random numbers in [0, 1)
+ *   path  : int32 [n_seq, max_path], max_path >= max_q: the kept nodes, then -1
+ *   count : int32 [n_seq] how many;  next : int32 [n_seq] the token after them
+ * At the last kept node c, with r = P[c], q = Q[c] and R = Z = 1 at first, the children are
+ * tried in order.  One with token x is kept if r(x) > 0 and u q(x) R < r(x) Z, and the walk
+ * goes on from it.  Else r <- max(r / R - q / Z, 0), R <- sum r; without replacement then
+ * q(x) <- 0, Z <- sum q.  (Without Q: kept if r(x) > 0 and u R < r(x); else R <- R - r(x),
+ * r(x) <- 0.)  If nothing is left of r the walk ends with the r before.  After the last
+ * child `next` is the first x at which the running sum of r passes u_next sum r (the last x
+ * with r(x) > 0, should rounding leave none).  In fp64; rows are taken to sum to one.
+ * `next` is -1 where r has no mass or is not finite.  A sequence without nodes, or that
+ * does not fit (its rows, a parent), has count 0 and next -1.  Trees of at most 128 nodes, vocab at most 2^20
+ * (else OQ_ERR_UNSUPPORTED); pointers 4-byte aligned. */
+oq_status oq_tree_verify(int n_seq, int max_q, int64_t tokens, const int32_t* q_start, const int32_t* parent,
+                         const int32_t* token, const float* P, int64_t ld_p, const float* Q, int64_t ld_q,
+                         int64_t vocab, int replace, const float* u, const float* u_next, int32_t* path, int max_path,
+                         int32_t* count, int32_t* next, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Kernel timing on the launching stream (HIP events around each launch).
  * Kinds: 0 forward GEMM, 1 weight-gradient GEMM, 2 input-gradient GEMM,
  * 3 LWC forward, 4 LWC backward, 5 activation quant forward, 6 activation

@@ -19,7 +19,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "liboq.so")
 SOURCES = ["gemm.hip", "packed_linear_b23.hip", "packed_linear_b45.hip", "packed_linear_b67.hip",
            "quant.hip", "misc.hip", "packed.hip", "attention.hip", "block_ops.hip",
-           "norm_quant.hip", "int8_linear.hip", "kv_cache.hip", "api.hip"]
+           "norm_quant.hip", "int8_linear.hip", "kv_cache.hip", "kv_tree.hip", "tree_verify.hip",
+           "api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -36,7 +37,7 @@ FLAGS = [
 # per source: the attention kernels keep their accumulators in VGPRs (the
 # matrix instructions read and write them there, no AGPR copies around each)
 _VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-EXTRA = {"attention.hip": _VGPR_FORM, "kv_cache.hip": _VGPR_FORM}
+EXTRA = {"attention.hip": _VGPR_FORM, "kv_cache.hip": _VGPR_FORM, "kv_tree.hip": _VGPR_FORM}
 
 
 def _compile(src):

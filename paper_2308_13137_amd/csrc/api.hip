@@ -2260,6 +2260,7 @@ CacheArgs cache_args(const oq_kv_cache* c, const oq_kv_batch* b) {
   a.max_pages = b->max_pages;
   a.max_q = b->max_q;
   a.T = b->tokens;
+  a.parent = nullptr;
   return a;
 }
 
@@ -2273,6 +2274,68 @@ AttendPlan attend_plan(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
   if (b->n_seq == 0 || b->max_q == 0) return AttendPlan{16, 0, 1, 1, 0, 0, 0, 0, 0};
   return cache_attend_plan(b->n_seq, c->kv_heads, heads, b->tokens, b->max_q, int64_t(b->max_pages) * c->page,
                            c->head_dim);
+}
+
+// What an append checks of its rows, a batch's or a tree's.
+oq_status check_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q,
+                       const void* K, int64_t ld_k, const void* V, int64_t ld_v, oq_dtype in_dt, int heads,
+                       const float* rope, int64_t n_rope, const float* s_a, void* Q_out) {
+  OQ_REQ(dtype_ok(in_dt), "bad input dtype");
+  const int64_t wq = int64_t(heads) * cache->head_dim, wk = int64_t(cache->kv_heads) * cache->head_dim;
+  OQ_REQ(ld_q >= wq && ld_k >= wk && ld_v >= wk && ld_q % 8 == 0 && ld_k % 8 == 0 && ld_v % 8 == 0,
+         "rows ld_q=%lld ld_k=%lld ld_v=%lld: multiples of 8, at least the widths %lld and %lld",
+         (long long)ld_q, (long long)ld_k, (long long)ld_v, (long long)wq, (long long)wk);
+  OQ_REQ(!rope || n_rope > 0, "an empty rope table");
+  if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
+  OQ_REQ(Q && K && V && Q_out, "Q, K, V and Q_out are required");
+  OQ_REQ(aligned16(Q) && aligned16(K) && aligned16(V) && aligned16(rope) && aligned16(s_a) && aligned16(Q_out),
+         "pointers must be 16-byte aligned");
+  const int64_t T = batch->tokens, es = esize(in_dt);
+  auto meets = [&](const void* in, int64_t ld, int64_t w) {
+    return rows_meet(in, T, __int128(ld) * es, __int128(w) * es, Q_out, __int128(T) * wq * 2);
+  };
+  OQ_REQ((Q_out == Q && in_dt == OQ_BF16 && (ld_q == wq || T == 1)) || !meets(Q, ld_q, wq),
+         "Q_out may be Q where that is bf16 with rows of heads * head_dim, but not overlap it otherwise");
+  OQ_REQ(!meets(K, ld_k, wk) && !meets(V, ld_v, wk), "Q_out must not overlap K or V");
+  return OQ_OK;
+}
+
+oq_status check_queries(const oq_kv_cache* cache, const oq_kv_batch* batch, const void* Q, int64_t ld_q, int heads,
+                        const void* O, const float* LSE, const void* ws) {
+  OQ_REQ(ld_q >= int64_t(heads) * cache->head_dim && ld_q % 8 == 0,
+         "rows ld_q=%lld: a multiple of 8, at least heads * head_dim", (long long)ld_q);
+  if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
+  OQ_REQ(Q && O, "Q and O are required");
+  OQ_REQ(aligned16(Q) && aligned16(O) && aligned16(LSE) && aligned16(ws), "pointers must be 16-byte aligned");
+  const __int128 wide = 2 * int64_t(heads) * cache->head_dim;
+  OQ_REQ((O == Q && (2 * __int128(ld_q) == wide || batch->tokens == 1)) ||
+             !rows_meet(Q, batch->tokens, 2 * __int128(ld_q), wide, O, batch->tokens * wide),
+         "O may be Q where its rows are heads * head_dim, but not overlap it otherwise");
+  return OQ_OK;
+}
+
+oq_status check_plan(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads, const AttendPlan& plan,
+                     const void* ws, size_t ws_bytes) {
+  const int64_t rows = int64_t(batch->max_q) * (heads / cache->kv_heads);
+  if (plan.tile_rows && (rows > (1 << 30) || plan.units * cache->kv_heads * plan.many >= (1 << 24)))
+    return fail(OQ_ERR_UNSUPPORTED, "%lld tokens of up to %lld query rows a key head: too many for one call",
+                (long long)batch->tokens, (long long)rows);
+  const size_t need = (plan.few_floats + plan.many_floats) * 4;
+  if (need && (!ws || ws_bytes < need))
+    return fail(OQ_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws ? ws_bytes : size_t(0), need);
+  return OQ_OK;
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// A tree's nodes lie in the two pages that a window holds.
+oq_status check_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* parent) {
+  if (batch->max_q > cache->page)
+    return fail(OQ_ERR_UNSUPPORTED, "trees of up to %d tokens, pages of %d: a tree has at most a page's", batch->max_q,
+                cache->page);
+  if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
+  OQ_REQ(parent && aligned4(parent), "parent (4-byte aligned) is required");
+  return OQ_OK;
 }
 
 #define OQ_TRY(expr)              \
@@ -2374,23 +2437,9 @@ oq_status oq_kv_append(const oq_kv_cache* cache, const oq_kv_batch* batch, const
                        const float* rope, int64_t n_rope, const float* s_a, void* Q_out, hipStream_t st) {
   OQ_TRY(check_cache(cache, batch));
   OQ_TRY(check_heads(cache, heads));
-  OQ_REQ(dtype_ok(in_dt), "bad input dtype");
-  const int64_t wq = int64_t(heads) * cache->head_dim, wk = int64_t(cache->kv_heads) * cache->head_dim;
-  OQ_REQ(ld_q >= wq && ld_k >= wk && ld_v >= wk && ld_q % 8 == 0 && ld_k % 8 == 0 && ld_v % 8 == 0,
-         "rows ld_q=%lld ld_k=%lld ld_v=%lld: multiples of 8, at least the widths %lld and %lld",
-         (long long)ld_q, (long long)ld_k, (long long)ld_v, (long long)wq, (long long)wk);
-  OQ_REQ(!rope || n_rope > 0, "an empty rope table");
+  OQ_TRY(check_append(cache, batch, Q, ld_q, K, ld_k, V, ld_v, in_dt, heads, rope, n_rope, s_a, Q_out));
   if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
-  OQ_REQ(Q && K && V && Q_out, "Q, K, V and Q_out are required");
-  OQ_REQ(aligned16(Q) && aligned16(K) && aligned16(V) && aligned16(rope) && aligned16(s_a) && aligned16(Q_out),
-         "pointers must be 16-byte aligned");
-  const int64_t T = batch->tokens, es = esize(in_dt);
-  auto meets = [&](const void* in, int64_t ld, int64_t w) {
-    return rows_meet(in, T, __int128(ld) * es, __int128(w) * es, Q_out, __int128(T) * wq * 2);
-  };
-  OQ_REQ((Q_out == Q && in_dt == OQ_BF16 && (ld_q == wq || T == 1)) || !meets(Q, ld_q, wq),
-         "Q_out may be Q where that is bf16 with rows of heads * head_dim, but not overlap it otherwise");
-  OQ_REQ(!meets(K, ld_k, wk) && !meets(V, ld_v, wk), "Q_out must not overlap K or V");
+  const int64_t wq = int64_t(heads) * cache->head_dim, wk = int64_t(cache->kv_heads) * cache->head_dim;
   ProfScope ps(PK_OTHER, st, double(batch->tokens) * ((wq + 2.0 * wk) * esize(in_dt) + 2.0 * wq + 2.0 * wk));
   OQ_HIP(cache_append(cache_args(cache, batch), Q, ld_q, K, ld_k, V, ld_v, in_dt == OQ_BF16, heads, rope, n_rope,
                       s_a, static_cast<uint16_t*>(Q_out), st),
@@ -2412,23 +2461,10 @@ oq_status oq_kv_attend(const oq_kv_cache* cache, const oq_kv_batch* batch, const
                        int heads, void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t st) {
   OQ_TRY(check_cache(cache, batch));
   OQ_TRY(check_heads(cache, heads));
-  OQ_REQ(ld_q >= int64_t(heads) * cache->head_dim && ld_q % 8 == 0,
-         "rows ld_q=%lld: a multiple of 8, at least heads * head_dim", (long long)ld_q);
+  OQ_TRY(check_queries(cache, batch, Q, ld_q, heads, O, LSE, ws));
   if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
-  OQ_REQ(Q && O, "Q and O are required");
-  OQ_REQ(aligned16(Q) && aligned16(O) && aligned16(LSE) && aligned16(ws), "pointers must be 16-byte aligned");
-  const __int128 wide = 2 * int64_t(heads) * cache->head_dim;
-  OQ_REQ((O == Q && (2 * __int128(ld_q) == wide || batch->tokens == 1)) ||
-             !rows_meet(Q, batch->tokens, 2 * __int128(ld_q), wide, O, batch->tokens * wide),
-         "O may be Q where its rows are heads * head_dim, but not overlap it otherwise");
   const AttendPlan plan = attend_plan(cache, batch, heads);
-  const int64_t rows = int64_t(batch->max_q) * (heads / cache->kv_heads);
-  if (plan.tile_rows && (rows > (1 << 30) || plan.units * cache->kv_heads * plan.many >= (1 << 24)))
-    return fail(OQ_ERR_UNSUPPORTED, "%lld tokens of up to %lld query rows a key head: too many for one call",
-                (long long)batch->tokens, (long long)rows);
-  const size_t need = (plan.few_floats + plan.many_floats) * 4;
-  if (need && (!ws || ws_bytes < need))
-    return fail(OQ_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws ? ws_bytes : size_t(0), need);
+  OQ_TRY(check_plan(cache, batch, heads, plan, ws, ws_bytes));
   ProfScope ps(PK_CACHE_ATTN, st, 4.0 * double(batch->tokens) * heads * cache->head_dim);
   OQ_HIP(cache_attend(cache_args(cache, batch), static_cast<const uint16_t*>(Q), ld_q, heads,
                       static_cast<uint16_t*>(O), LSE, static_cast<float*>(ws), plan, st),
@@ -2451,6 +2487,114 @@ oq_status oq_kv_read(const oq_kv_cache* cache, const oq_kv_batch* batch, const i
   ProfScope ps(PK_OTHER, st, 2.0 * double(rows) * cache->kv_heads * cache->head_dim * (1 + esize(out_dt)));
   OQ_HIP(cache_read(cache_args(cache, batch), begin, row_start, rows, max_rows, K, V, out_dt == OQ_BF16, st),
          "kv_read");
+  return OQ_OK;
+}
+
+oq_status oq_kv_append_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* parent, const void* Q,
+                            int64_t ld_q, const void* K, int64_t ld_k, const void* V, int64_t ld_v, oq_dtype in_dt,
+                            int heads, const float* rope, int64_t n_rope, const float* s_a, void* Q_out,
+                            hipStream_t st) {
+  OQ_TRY(check_cache(cache, batch));
+  OQ_TRY(check_heads(cache, heads));
+  OQ_TRY(check_tree(cache, batch, parent));
+  OQ_TRY(check_append(cache, batch, Q, ld_q, K, ld_k, V, ld_v, in_dt, heads, rope, n_rope, s_a, Q_out));
+  if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
+  const int64_t wq = int64_t(heads) * cache->head_dim, wk = int64_t(cache->kv_heads) * cache->head_dim;
+  ProfScope ps(PK_OTHER, st, double(batch->tokens) * ((wq + 2.0 * wk) * esize(in_dt) + 2.0 * wq + 4.0 * wk));
+  CacheArgs c = cache_args(cache, batch);
+  c.parent = parent;
+  OQ_HIP(cache_append_tree(c, Q, ld_q, K, ld_k, V, ld_v, in_dt == OQ_BF16, heads, rope, n_rope, s_a,
+                           static_cast<uint16_t*>(Q_out), st),
+         "kv_append_tree");
+  return OQ_OK;
+}
+
+oq_status oq_kv_attend_tree_workspace_size(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads,
+                                           size_t* bytes) {
+  OQ_REQ(bytes, "bytes is required");
+  OQ_TRY(check_cache(cache, batch));
+  OQ_TRY(check_heads(cache, heads));
+  const AttendPlan p = attend_plan(cache, batch, heads);
+  *bytes = (p.few_floats + p.many_floats) * 4;
+  return OQ_OK;
+}
+
+oq_status oq_kv_attend_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* parent, const void* Q,
+                            int64_t ld_q, int heads, void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t st) {
+  OQ_TRY(check_cache(cache, batch));
+  OQ_TRY(check_heads(cache, heads));
+  OQ_TRY(check_tree(cache, batch, parent));
+  OQ_TRY(check_queries(cache, batch, Q, ld_q, heads, O, LSE, ws));
+  if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
+  const AttendPlan plan = attend_plan(cache, batch, heads);
+  OQ_TRY(check_plan(cache, batch, heads, plan, ws, ws_bytes));
+  ProfScope ps(PK_CACHE_ATTN, st, 4.0 * double(batch->tokens) * heads * cache->head_dim);
+  CacheArgs c = cache_args(cache, batch);
+  c.parent = parent;
+  OQ_HIP(cache_attend_tree(c, static_cast<const uint16_t*>(Q), ld_q, heads, static_cast<uint16_t*>(O), LSE,
+                           static_cast<float*>(ws), plan, st),
+         "kv_attend_tree");
+  return OQ_OK;
+}
+
+oq_status oq_kv_commit(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* path, int max_path,
+                       const int32_t* count, hipStream_t st) {
+  OQ_TRY(check_cache(cache, batch));
+  if (batch->max_q > cache->page)
+    return fail(OQ_ERR_UNSUPPORTED, "trees of up to %d tokens, pages of %d: a tree has at most a page's", batch->max_q,
+                cache->page);
+  OQ_REQ(max_path >= 0, "bad max_path=%d", max_path);
+  if (batch->n_seq == 0 || batch->max_q == 0 || max_path == 0) return OQ_OK;
+  OQ_REQ(path && count && aligned4(path) && aligned4(count), "path and count (4-byte aligned) are required");
+  ProfScope ps(PK_OTHER, st, 8.0 * double(batch->tokens) * cache->kv_heads * cache->head_dim);
+  OQ_HIP(cache_commit(cache_args(cache, batch), path, max_path, count, st), "kv_commit");
+  return OQ_OK;
+}
+
+oq_status oq_token_probs(const void* logits, oq_dtype dt, int64_t ld, int64_t n_rows, int64_t vocab,
+                         const float* temperature, float* P, int64_t ld_p, hipStream_t st) {
+  OQ_REQ(dtype_ok(dt), "bad logits dtype");
+  OQ_REQ(n_rows >= 0 && n_rows <= INT32_MAX && vocab > 0 && ld >= vocab && ld_p >= vocab,
+         "bad shape n_rows=%lld vocab=%lld, rows ld=%lld ld_p=%lld", (long long)n_rows, (long long)vocab,
+         (long long)ld, (long long)ld_p);
+  if (vocab > VOCAB_MAX) return fail(OQ_ERR_UNSUPPORTED, "vocab=%lld > %lld", (long long)vocab, (long long)VOCAB_MAX);
+  if (n_rows == 0) return OQ_OK;
+  OQ_REQ(logits && P, "logits and P are required");
+  OQ_REQ((reinterpret_cast<uintptr_t>(logits) & (esize(dt) - 1)) == 0 && aligned4(temperature) && aligned4(P),
+         "pointers must be aligned to their elements");
+  OQ_REQ(!rows_meet(logits, n_rows, __int128(ld) * esize(dt), __int128(vocab) * esize(dt), P,
+                    (__int128(n_rows - 1) * ld_p + vocab) * 4),
+         "P must not overlap the logits");
+  ProfScope ps(PK_OTHER, st, double(n_rows) * vocab * (esize(dt) + 4));
+  OQ_HIP(token_probs(logits, dt == OQ_BF16, ld, n_rows, vocab, temperature, P, ld_p, st), "token_probs");
+  return OQ_OK;
+}
+
+oq_status oq_tree_verify(int n_seq, int max_q, int64_t tokens, const int32_t* q_start, const int32_t* parent,
+                         const int32_t* token, const float* P, int64_t ld_p, const float* Q, int64_t ld_q,
+                         int64_t vocab, int replace, const float* u, const float* u_next, int32_t* path, int max_path,
+                         int32_t* count, int32_t* next, hipStream_t st) {
+  OQ_REQ(n_seq >= 0 && max_q >= 0 && tokens >= 0 && tokens <= INT32_MAX && max_q <= tokens && max_path >= max_q &&
+             vocab > 0 && ld_p >= vocab && (!Q || ld_q >= vocab),
+         "bad n_seq=%d max_q=%d tokens=%lld max_path=%d vocab=%lld, rows ld_p=%lld ld_q=%lld", n_seq, max_q,
+         (long long)tokens, max_path, (long long)vocab, (long long)ld_p, (long long)ld_q);
+  if (max_q > VERIFY_MAX_NODES || vocab > VOCAB_MAX)
+    return fail(OQ_ERR_UNSUPPORTED, "trees of up to %d nodes (at most %d), vocab=%lld (at most %lld)", max_q,
+                VERIFY_MAX_NODES, (long long)vocab, (long long)VOCAB_MAX);
+  if (n_seq == 0) return OQ_OK;
+  OQ_REQ(q_start && count && next && (path || max_path == 0), "q_start, path, count and next are required");
+  OQ_REQ(tokens == 0 || (parent && token && P && u), "parent, token, P and u are required");
+  OQ_REQ(u_next, "u_next is required");
+  for (const void* p : {static_cast<const void*>(q_start), static_cast<const void*>(parent),
+                        static_cast<const void*>(token), static_cast<const void*>(P), static_cast<const void*>(Q),
+                        static_cast<const void*>(u), static_cast<const void*>(u_next),
+                        static_cast<const void*>(path), static_cast<const void*>(count),
+                        static_cast<const void*>(next)})
+    OQ_REQ(aligned4(p), "pointers must be 4-byte aligned");
+  ProfScope ps(PK_OTHER, st, double(n_seq) * vocab * (Q ? 8 : 4));
+  const VerifyArgs a{q_start, parent, token,  P,    Q,    u,     u_next, path,    count,
+                     next,    tokens, vocab, ld_p, ld_q, n_seq, max_q,  max_path, replace != 0};
+  OQ_HIP(tree_verify(a, st), "tree_verify");
   return OQ_OK;
 }
 

@@ -50,6 +50,7 @@ struct CacheArgs {
   const int32_t* q_start;   // [n_seq + 1]
   int n_seq, max_pages, max_q;
   int64_t T;                // rows of the batch's tensors
+  const int32_t* parent;    // [T] | nullptr: the new tokens are a tree (kv_tree.hip)
 };
 hipError_t cache_append(const CacheArgs& c, const void* Q, int64_t ldq, const void* K, int64_t ldk,
                         const void* V, int64_t ldv, bool in_bf16, int H, const float* rope, int64_t n_rope,
@@ -68,5 +69,30 @@ struct AttendPlan {
 AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d);
 hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int H, uint16_t* O, float* LSE,
                         float* ws, const AttendPlan& p, hipStream_t st);
+
+
+// ---------------------------------------------------------------- trees of drafted tokens (c.parent)
+hipError_t cache_append_tree(const CacheArgs& c, const void* Q, int64_t ldq, const void* K, int64_t ldk,
+                             const void* V, int64_t ldv, bool in_bf16, int H, const float* rope, int64_t n_rope,
+                             const float* s_a, uint16_t* Qout, hipStream_t st);
+hipError_t cache_attend_tree(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int H, uint16_t* O, float* LSE,
+                             float* ws, const AttendPlan& p, hipStream_t st);
+hipError_t cache_commit(const CacheArgs& c, const int32_t* path, int max_path, const int32_t* count, hipStream_t st);
+
+// ---------------------------------------------------------------- drafted tokens against the target
+constexpr int64_t VOCAB_MAX = 1 << 20;
+constexpr int VERIFY_MAX_NODES = 128;
+hipError_t token_probs(const void* logits, bool bf16, int64_t ldl, int64_t T, int64_t V, const float* temperature,
+                       float* P, int64_t ldp, hipStream_t st);
+struct VerifyArgs {
+  const int32_t *q_start, *parent, *token;   // [n_seq + 1], [T], [T]
+  const float *P, *Q;                        // [T, V], rows ldp and ldq apart; Q | nullptr
+  const float *u, *u_next;                   // [T], [n_seq]
+  int32_t *path, *count, *next;              // [n_seq, max_path], [n_seq], [n_seq]
+  int64_t T, V, ldp, ldq;
+  int n_seq, max_q, max_path;
+  bool replace;
+};
+hipError_t tree_verify(const VerifyArgs& a, hipStream_t st);
 
 }  // namespace oq

@@ -1,0 +1,376 @@
+// Drafted tokens against the target: logits to probabilities, and the walk down a tree
+// of drafts that keeps the target's distribution.
+#include <math.h>
+
+#include <type_traits>
+
+#include "common.h"
+#include "serve.h"
+
+namespace oq {
+namespace {
+
+constexpr int NT = 1024, NW = NT / 64;
+
+// Rows of a vocabulary start at any element: 16 bytes at an address of any alignment.
+template <typename T>
+OQ_DEV T load_any(const void* p) {
+  T v;
+  __builtin_memcpy(&v, p, sizeof(T));
+  return v;
+}
+
+// ------------------------------------------------------------------ probabilities
+// P = softmax(logits / t) = 2^((x - max x) log2(e) / t) over their sum.  One workgroup
+// a row: up to NV 16-byte pieces a thread stay in registers between the maximum, the sum
+// and the output; what is beyond them is read again.
+template <typename TI, int NV>
+__global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int64_t ldx, int64_t V,
+                                                   const float* __restrict__ temperature, float* __restrict__ P,
+                                                   int64_t ldp) {
+  constexpr int E = 16 / sizeof(TI);
+  typedef unsigned raw_t __attribute__((ext_vector_type(4)));
+  __shared__ float s_a[NW];
+  __shared__ int s_i[NW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const TI* x = X + int64_t(blockIdx.x) * ldx;
+  float* out = P + int64_t(blockIdx.x) * ldp;
+  const int n = int(V / E), rest = int(V) - n * E;         // whole pieces, values behind them
+  const float t = temperature ? temperature[blockIdx.x] : 1.0f;
+  auto value = [&](raw_t w, int e) {
+    if constexpr (E == 8) return __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+    else return __uint_as_float(w[e]);
+  };
+  raw_t held[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (tid + NT * k < n) held[k] = load_any<raw_t>(x + int64_t(E) * (tid + NT * k));
+  const float tail = tid < rest ? load1(x + int64_t(n) * E + tid) : -INFINITY;
+  // f(piece number, its values) of every whole piece of this thread
+  auto pieces = [&](auto f) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (tid + NT * k < n) f(tid + NT * k, held[k]);
+    for (int i = tid + NT * NV; i < n; i += NT) f(i, load_any<raw_t>(x + int64_t(E) * i));
+  };
+  float m = tail;
+  bool odd = !(tail < INFINITY);                           // NaN or +inf
+  pieces([&](int, raw_t w) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      m = fmaxf(m, value(w, e));
+      odd = odd || !(value(w, e) < INFINITY);
+    }
+  });
+  m = wave_max(m);
+  if (lane == 0) s_a[wave] = m;
+  odd = __syncthreads_or(odd);
+#pragma unroll
+  for (int w = 0; w < NW; ++w) m = fmaxf(m, s_a[w]);
+  // a row without a maximum, or without a temperature, is no distribution
+  if (odd || m == -INFINITY || !(t >= 0.0f && t < INFINITY)) {
+    for (int64_t i = tid; i < V; i += NT) out[i] = NAN;
+    return;
+  }
+  if (t == 0.0f) {                                         // all of it on the first maximum
+    int first = tail == m ? n * E + tid : 0x7fffffff;
+    pieces([&](int i, raw_t w) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (value(w, e) == m) first = min(first, i * E + e);
+    });
+    for (int off = 1; off < 64; off <<= 1) first = min(first, __shfl_xor(first, off));
+    if (lane == 0) s_i[wave] = first;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) first = min(first, s_i[w]);
+    for (int64_t i = tid; i < V; i += NT) out[i] = i == first ? 1.0f : 0.0f;
+    return;
+  }
+  const float k = fminf(1.4426950408889634f / t, 3.0e38f);
+  auto weight = [&](float v) { return __builtin_amdgcn_exp2f((v - m) * k); };
+  float sum = tid < rest ? weight(tail) : 0.0f;
+  pieces([&](int, raw_t w) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum += weight(value(w, e));
+  });
+  sum = wave_sum(sum);
+  __syncthreads();                                         // s_a is read
+  if (lane == 0) s_a[wave] = sum;
+  __syncthreads();
+  sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) sum += s_a[w];
+  const float inv = 1.0f / sum;
+  pieces([&](int i, raw_t w) {
+    float y[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = weight(value(w, e)) * inv;
+    __builtin_memcpy(out + int64_t(i) * E, y, sizeof(y));
+  });
+  if (tid < rest) out[int64_t(n) * E + tid] = weight(tail) * inv;
+}
+
+// ------------------------------------------------------------------ verification
+// The walk of one tree.  At node c the target's distribution is r = P[c]; its children
+// are tried in order.  A child with token x that the draft took from q (its own row Q[c])
+// is accepted if u q(x) / Z < r(x) / R; otherwise r becomes max(r / R - q / Z, 0), what the
+// target has beyond the draft, and R its mass; where siblings differ, x leaves q and Z is
+// what q has left.  (R = Z = 1 at first: rows are distributions.)  Without Q a child is
+// certain: q is one at x, and r loses x.  After the last accepted node the next token
+// is drawn from r.  Numbers that decide are fp64: a sum over the vocabulary that fp32 held
+// would move the border between two tokens by more than most tokens have.
+//
+// After m rejections r(x) follows from p(x), q(x) and the masses of each step alone,
+// so a child's test reads two numbers (all of them are fetched at the start), and only a
+// mass needs a pass over the vocabulary: before a further sibling, and for the draw.
+template <bool CERTAIN>
+OQ_DEV double residual(float p, float q, int x, int levels, const double* s_ir, const double* s_iz, const int* s_rej) {
+  double r = p;
+  if constexpr (CERTAIN) {
+    for (int t = 0; t < levels; ++t) r = x == s_rej[t] ? 0.0 : r;
+  } else {
+    for (int t = 0; t < levels; ++t) {
+      const double d = r * s_ir[t] - double(q) * s_iz[t];
+      r = d > 0.0 ? d : d * 0.0;                           // (a NaN stays one)
+    }
+  }
+  return r > 0.0 ? r : r * 0.0;
+}
+OQ_DEV double wave_sum64(double v) {
+  for (int off = 1; off < 64; off <<= 1) v += __shfl_xor(v, off);
+  return v;
+}
+
+template <bool CERTAIN>
+__global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
+  constexpr int M = VERIFY_MAX_NODES;
+  __shared__ int s_par[M], s_tok[M], s_rej[M], s_path[M];
+  __shared__ float s_u[M], s_p[M], s_q[M];
+  __shared__ double s_ir[M], s_iz[M], s_sum[NW], s_sumq[NW];
+  __shared__ int s_hit;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = blockIdx.x;
+  const int64_t b = a.q_start[i], e = a.q_start[i + 1];
+  int32_t* path = a.path + int64_t(i) * a.max_path;
+  const int V = int(a.V);
+  bool none = b < 0 || e <= b || e > a.T || e - b > a.max_q;   // no tree, or one that does not fit
+  const int n = none ? 0 : int(e - b);
+  const int par_t = tid < n ? a.parent[b + tid] : -1;
+  none = __syncthreads_or(none || par_t < -1 || (par_t >= 0 && par_t >= tid));
+  if (none) {
+    for (int k = tid; k < a.max_path; k += NT) path[k] = -1;
+    if (tid == 0) {
+      a.count[i] = 0;
+      a.next[i] = -1;
+    }
+    return;
+  }
+  if (tid < n) {
+    const int par = par_t, tok = a.token[b + tid];
+    const bool fits = par >= 0 && par < tid && tok >= 0 && tok < V;
+    s_par[tid] = par;
+    s_tok[tid] = tok;
+    s_u[tid] = a.u[b + tid];
+    s_p[tid] = fits ? a.P[(b + par) * a.ldp + tok] : 0.0f;
+    s_q[tid] = fits && !CERTAIN ? a.Q[(b + par) * a.ldq + tok] : 1.0f;
+  }
+  __syncthreads();
+  const int par0 = lane < n ? s_par[lane] : -2, par1 = lane + 64 < n ? s_par[lane + 64] : -2;
+  // the next child of c behind node j, n if there is none
+  auto child_after = [&](int c, int j) {
+    const uint64_t lo = __ballot(par0 == c && lane > j), hi = __ballot(par1 == c && lane + 64 > j);
+    return lo ? __ffsll(static_cast<unsigned long long>(lo)) - 1 : hi ? __ffsll(static_cast<unsigned long long>(hi)) + 63 : n;
+  };
+  const float *p = a.P + b * a.ldp, *q = CERTAIN ? nullptr : a.Q + b * a.ldq;
+  int levels = 0;
+  // sums of r (and of q) over values x0 .. x1 - 1 of the row, by one wave
+  auto range_sum = [&](int x0, int x1, double& sr, double& sq) {
+    double r = 0.0, w = 0.0;
+    for (int x = x0 + 4 * lane; x < x1; x += 256) {
+      float pv[4], qv[4] = {0.f, 0.f, 0.f, 0.f};
+      if (x + 4 <= x1) {
+        const float4 f = load_any<float4>(p + x);
+        pv[0] = f.x; pv[1] = f.y; pv[2] = f.z; pv[3] = f.w;
+        if constexpr (!CERTAIN) {
+          const float4 h = load_any<float4>(q + x);
+          qv[0] = h.x; qv[1] = h.y; qv[2] = h.z; qv[3] = h.w;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          pv[k] = x + k < x1 ? p[x + k] : 0.0f;
+          if constexpr (!CERTAIN) qv[k] = x + k < x1 ? q[x + k] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        r += residual<CERTAIN>(pv[k], qv[k], x + k, levels, s_ir, s_iz, s_rej);
+        w += double(qv[k]);
+      }
+    }
+    sr = wave_sum64(r);
+    sq = wave_sum64(w);
+  };
+  // Values of a wave: sixteenths of the row, in whole steps of a wave.
+  const int part = ((V + NW - 1) / NW + 255) / 256 * 256;
+  auto row_sums = [&](double& sr, double& sq) {
+    __syncthreads();
+    double r, w;
+    range_sum(min(V, wave * part), min(V, (wave + 1) * part), r, w);
+    if (lane == 0) {
+      s_sum[wave] = r;
+      s_sumq[wave] = w;
+    }
+    __syncthreads();
+    sr = sq = 0.0;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      sr += s_sum[k];
+      sq += s_sumq[k];
+    }
+  };
+  int cur = 0, count = 1;
+  double R = 1.0, Z = 1.0, gone = 0.0;                     // gone: what has left q
+  if (tid == 0) s_path[0] = 0;
+  for (int j = child_after(0, 0); j < n;) {
+    const int x = s_tok[j];
+    if (x < 0 || x >= V) {                                 // no token: rejected, and nothing learned
+      j = child_after(cur, j);
+      continue;
+    }
+    const float px = s_p[j], qx = s_q[j];
+    bool again = false;                                    // an earlier sibling had this token
+    for (int t = 0; t < levels; ++t) again = again || s_rej[t] == x;
+    const double r = residual<CERTAIN>(px, qx, x, levels, s_ir, s_iz, s_rej);
+    const double qm = !CERTAIN && !a.replace && again ? 0.0 : double(qx);
+    if (r > 0.0 && double(s_u[j]) * qm * R < r * Z) {
+      cur = j;
+      if (tid == 0) s_path[count] = j;
+      ++count;
+      p = a.P + (b + j) * a.ldp;
+      if constexpr (!CERTAIN) q = a.Q + (b + j) * a.ldq;
+      levels = 0;
+      R = Z = 1.0;
+      gone = 0.0;
+      j = child_after(j, j);
+      continue;
+    }
+    __syncthreads();                                       // (every wave has read this level's numbers)
+    if (tid == 0) {
+      s_rej[levels] = x;
+      s_ir[levels] = 1.0 / R;
+      s_iz[levels] = Z > 0.0 ? 1.0 / Z : 0.0;
+    }
+    __syncthreads();
+    ++levels;
+    j = child_after(cur, j);
+    if constexpr (CERTAIN) {
+      R -= r;
+    } else {
+      if (!again) gone += double(qx);
+      if (j < n) {
+        double sr, sq;
+        row_sums(sr, sq);
+        if (sr == 0.0) break;                              // nothing is left: the draw steps back
+        R = sr;
+        if (!a.replace) Z = sq - gone;
+      }
+    }
+  }
+  // the draw
+  int next = -1;
+  while (true) {
+    double total, sq;
+    row_sums(total, sq);
+    if (total == 0.0 && levels > 0) {                      // no mass: from the distribution before
+      --levels;
+      continue;
+    }
+    if (!(total > 0.0 && total < INFINITY)) break;
+    const double want = double(a.u_next[i]) * total;
+    // the wave's part that holds it (the last one with mass, should rounding leave none), then the
+    // sixteenth of that, then the value
+    double before = 0.0, upto = 0.0;
+    int at = 0;
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      const double v = s_sum[k];
+      if (!found && v > 0.0) {
+        before = upto;
+        at = k;
+        found = upto + v > want;
+      }
+      upto += v;
+    }
+    __syncthreads();
+    const int x0 = at * part, sub = part / NW;             // (a multiple of 16)
+    double r, w;
+    range_sum(min(V, x0 + wave * sub), min(V, x0 + (wave + 1) * sub), r, w);
+    if (lane == 0) s_sum[wave] = r;
+    __syncthreads();
+    upto = before;
+    int at2 = 0;
+    found = false;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      const double v = s_sum[k];
+      if (!found && v > 0.0) {
+        before = upto;
+        at2 = k;
+        found = upto + v > want;
+      }
+      upto += v;
+    }
+    if (wave == 0) {
+      // 64 values at a time
+      const int lo = min(V, x0 + at2 * sub), hi = min(V, lo + sub);
+      int hit = -1, last = -1;
+      for (int y = lo; y < hi && hit < 0; y += 64) {
+        const int xx = y + lane;
+        const float pv = xx < hi ? p[xx] : 0.0f, qv = !CERTAIN && xx < hi ? q[xx] : 0.0f;
+        const double rv = residual<CERTAIN>(pv, qv, xx, levels, s_ir, s_iz, s_rej);
+        double c = rv;
+        for (int off = 1; off < 64; off <<= 1) {
+          const double o = __shfl_up(c, off);
+          if (lane >= off) c += o;
+        }
+        const uint64_t over = __ballot(rv > 0.0 && before + c > want), some = __ballot(rv > 0.0);
+        if (over) hit = y + __ffsll(static_cast<unsigned long long>(over)) - 1;
+        if (some) last = y + 63 - __clzll(static_cast<long long>(some));
+        before += __shfl(c, 63);
+      }
+      if (lane == 0) s_hit = hit >= 0 ? hit : last;
+    }
+    __syncthreads();
+    next = s_hit;
+    break;
+  }
+  for (int k = tid; k < a.max_path; k += NT) path[k] = k < count ? s_path[k] : -1;
+  if (tid == 0) {
+    a.count[i] = count;
+    a.next[i] = next;
+  }
+}
+
+}  // namespace
+
+hipError_t token_probs(const void* logits, bool bf16, int64_t ldl, int64_t T, int64_t V, const float* temperature,
+                       float* P, int64_t ldp, hipStream_t st) {
+  auto go = [&](auto ti, auto nv) {
+    using TI = decltype(ti);
+    hipLaunchKernelGGL((probs_kernel<TI, decltype(nv)::value>), dim3(unsigned(T)), dim3(NT), 0, st,
+                       static_cast<const TI*>(logits), ldl, V, temperature, P, ldp);
+  };
+  if (bf16) go(uint16_t{}, std::integral_constant<int, 16>{});
+  else go(float{}, std::integral_constant<int, 16>{});
+  return hipGetLastError();
+}
+
+hipError_t tree_verify(const VerifyArgs& a, hipStream_t st) {
+  if (a.Q) hipLaunchKernelGGL(verify_kernel<false>, dim3(unsigned(a.n_seq)), dim3(NT), 0, st, a);
+  else hipLaunchKernelGGL(verify_kernel<true>, dim3(unsigned(a.n_seq)), dim3(NT), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace oq

@@ -874,6 +874,12 @@ _SIGS_SERVE = {
     "oq_kv_attend_workspace_size": (_I, [_P, _P, _I, _PSZ]),
     "oq_kv_attend": (_I, [_P, _P, _P, _I64, _I, _P, _P, _P, _SZ, _P]),
     "oq_kv_read": (_I, [_P, _P, _P, _P, _I64, _I, _P, _P, _I, _P]),
+    "oq_kv_append_tree": (_I, [_P, _P, _P, _P, _I64, _P, _I64, _P, _I64, _I, _I, _P, _I64, _P, _P, _P]),
+    "oq_kv_attend_tree_workspace_size": (_I, [_P, _P, _I, _PSZ]),
+    "oq_kv_attend_tree": (_I, [_P, _P, _P, _P, _I64, _I, _P, _P, _P, _SZ, _P]),
+    "oq_kv_commit": (_I, [_P, _P, _P, _I, _P, _P]),
+    "oq_token_probs": (_I, [_P, _I, _I64, _I64, _I64, _P, _P, _I64, _P]),
+    "oq_tree_verify": (_I, [_I, _I, _I64, _P, _P, _P, _P, _I64, _P, _I64, _I64, _I, _P, _P, _P, _I, _P, _P, _P]),
 }
 SIGNATURES.update(_SIGS_SERVE)
 
@@ -1095,10 +1101,21 @@ class KVCache:
         (bf16 or fp32; columns of one tensor will do); K and V into the cache
         (oq_kv_append).  Returns Q~ bf16 [T, H d] (in ``out`` if given; a
         contiguous bf16 Q will do)."""
+        return self._append(None, Q, K, V, table, length, q_start, max_q, rope, s_a, slots, out, stream)
+
+    def append_tree(self, Q, K, V, table, length, q_start, max_q, parent, rope=None, s_a=None, slots=None,
+                    out=None, stream=None):
+        """:meth:`append` for trees of drafted tokens (oq_kv_append_tree): ``parent`` int32 [T]
+        is the node, counted within its sequence, that each one stands behind, -1 the sequence
+        itself.  RoPE goes by a node's depth; K and V wait in the windows for :meth:`commit`.
+        A tree has at most ``page`` nodes."""
+        return self._append(parent, Q, K, V, table, length, q_start, max_q, rope, s_a, slots, out, stream)
+
+    def _append(self, parent, Q, K, V, table, length, q_start, max_q, rope, s_a, slots, out, stream):
         dev = self.dev
         if stream is not None or dev != _cur_device():
             with _placed(dev, stream):
-                return self.append(Q, K, V, table, length, q_start, max_q, rope, s_a, slots, out)
+                return self._append(parent, Q, K, V, table, length, q_start, max_q, rope, s_a, slots, out, None)
         dt, d = Q.dtype, self.head_dim
         T, W = Q.shape
         kv = self.kv_heads * d
@@ -1115,18 +1132,33 @@ class KVCache:
         ps = None if s_a is None else _arg(s_a, "s_a", _F32T, (kv,), dev)
         if out is None:
             out = Q.new_empty((T, W), dtype=_BF16)
-        _check(lib().oq_kv_append(C.byref(self.desc), C.byref(b), pq, lq, pk, lk, pv, lv, _dt(Q), W // d, pt,
-                                  n_rope, ps, _arg(out, "out", _BF16, (T, W), dev), _raw_stream(dev)))
+        po = _arg(out, "out", _BF16, (T, W), dev)
+        if parent is None:
+            _check(lib().oq_kv_append(C.byref(self.desc), C.byref(b), pq, lq, pk, lk, pv, lv, _dt(Q), W // d, pt,
+                                      n_rope, ps, po, _raw_stream(dev)))
+        else:
+            _check(lib().oq_kv_append_tree(C.byref(self.desc), C.byref(b), _arg(parent, "parent", _I32, (T,), dev),
+                                           pq, lq, pk, lk, pv, lv, _dt(Q), W // d, pt, n_rope, ps, po,
+                                           _raw_stream(dev)))
         return out
 
     def attend(self, Q, table, length, q_start, max_q, slots=None, want_lse=False, out=None, stream=None):
         """Causal attention of the new tokens' Q (bf16 [T, H d], :meth:`append`'s) over
         the cache that holds them (oq_kv_attend).  Returns O bf16 [T, H d] (in ``out`` if
         given; a contiguous Q will do), with ``want_lse`` (O, LSE [H, T])."""
+        return self._attend(None, Q, table, length, q_start, max_q, slots, want_lse, out, stream)
+
+    def attend_tree(self, Q, table, length, q_start, max_q, parent, slots=None, want_lse=False, out=None,
+                    stream=None):
+        """:meth:`attend` for trees of drafted tokens behind :meth:`append_tree`
+        (oq_kv_attend_tree): each node sees its sequence, its ancestors and itself."""
+        return self._attend(parent, Q, table, length, q_start, max_q, slots, want_lse, out, stream)
+
+    def _attend(self, parent, Q, table, length, q_start, max_q, slots, want_lse, out, stream):
         dev = self.dev
         if stream is not None or dev != _cur_device():
             with _placed(dev, stream):
-                return self.attend(Q, table, length, q_start, max_q, slots, want_lse, out)
+                return self._attend(parent, Q, table, length, q_start, max_q, slots, want_lse, out, None)
         d = self.head_dim
         T, W = Q.shape
         pq, lq = _rows(Q, "Q", T, W, _BF16, dev)
@@ -1136,15 +1168,35 @@ class KVCache:
         cache, b = C.byref(self.desc), C.byref(self._batch(table, length, q_start, max_q, T, slots))
         n = C.c_size_t(0)
         L = lib()
-        _check(L.oq_kv_attend_workspace_size(cache, b, heads, C.byref(n)))
+        size = L.oq_kv_attend_workspace_size if parent is None else L.oq_kv_attend_tree_workspace_size
+        _check(size(cache, b, heads, C.byref(n)))
         if out is None:
             out = Q.new_empty((T, W))
         lse = Q.new_empty((heads, T), dtype=_F32T) if want_lse else None
         ws = Q.new_empty(n.value, dtype=_U8) if n.value else None
-        _check(L.oq_kv_attend(cache, b, pq, lq, heads, _arg(out, "out", _BF16, (T, W), dev),
-                              None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
-                              n.value, _raw_stream(dev)))
+        rest = (pq, lq, heads, _arg(out, "out", _BF16, (T, W), dev), None if lse is None else lse.data_ptr(),
+                None if ws is None else ws.data_ptr(), n.value, _raw_stream(dev))
+        if parent is None:
+            _check(L.oq_kv_attend(cache, b, *rest))
+        else:
+            _check(L.oq_kv_attend_tree(cache, b, _arg(parent, "parent", _I32, (T,), dev), *rest))
         return (out, lse) if want_lse else out
+
+    def commit(self, path, count, table, length, q_start, max_q, slots=None, stream=None):
+        """Keeps part of the trees that :meth:`append_tree` left (oq_kv_commit): node path[i, k] of
+        sequence i becomes its token length[i] + k, for k < count[i] (:func:`tree_verify`'s
+        outputs).  Pages that fill up become codes.  The caller then adds ``count`` to ``length``."""
+        dev = self.dev
+        if stream is not None or dev != _cur_device():
+            with _placed(dev, stream):
+                return self.commit(path, count, table, length, q_start, max_q, slots)
+        n, m = path.shape
+        # (the batch's rows themselves are not touched: any count holds them)
+        b = KVBatch(n, table.shape[1], max_q, 0x7fff0000, _arg(table, "table", _I32, (n, table.shape[1]), dev),
+                    None if slots is None else _arg(slots, "slots", _I32, (n,), dev),
+                    _arg(length, "length", _I32, (n,), dev), _arg(q_start, "q_start", _I32, (n + 1,), dev))
+        _check(lib().oq_kv_commit(C.byref(self.desc), C.byref(b), _arg(path, "path", _I32, (n, m), dev), m,
+                                  _arg(count, "count", _I32, (n,), dev), _raw_stream(dev)))
 
     def read(self, table, begin, length, q_start, row_start, rows, max_rows, slots=None,
              dtype=torch.bfloat16, stream=None):
@@ -1164,3 +1216,49 @@ class KVCache:
                                 _arg(row_start, "row_start", _I32, (n + 1,), dev), rows,
                                 min(max_rows, rows), k.data_ptr(), v.data_ptr(), _dt(k), _raw_stream(dev)))
         return k, v
+
+
+# ------------------------------------------------------------------ drafted tokens
+def token_probs(logits, temperature=None, out=None, stream=None):
+    """softmax(logits / temperature) of each row, fp32 [T, V] (oq_token_probs).  logits: bf16 or fp32
+    [T, V] (columns of a wider tensor will do); ``temperature``: fp32 [T], 0 = all of it on the
+    first of the largest logits.  ``out``: an existing output."""
+    dev = _gpu(logits, "logits")
+    if stream is not None or dev != _cur_device():
+        with _placed(dev, stream):
+            return token_probs(logits, temperature, out)
+    T, V = logits.shape
+    px, ld = _rows(logits, "logits", T, V, logits.dtype, dev)
+    pt = None if temperature is None else _arg(temperature, "temperature", _F32T, (T,), dev)
+    if out is None:
+        out = logits.new_empty((T, V), dtype=_F32T)
+    po, ldo = _rows(out, "out", T, V, _F32T, dev)
+    _check(lib().oq_token_probs(px, _dt(logits), ld, T, V, pt, po, ldo, _raw_stream(dev)))
+    return out
+
+
+def tree_verify(token, parent, q_start, max_q, P, u, u_next, Q=None, replace=True, stream=None):
+    """Which drafted tokens the target keeps, and the token after them (oq_tree_verify).
+
+    ``token``, ``parent`` int32 [T] and ``q_start`` int32 [n + 1]: the trees, whose node 0 is known
+    already; ``P`` fp32 [T, V]: the target's distribution after each node; ``Q``: the draft's, from
+    which each node's token was drawn at its parent (siblings with ``replace``, or without
+    replacement), None for tokens chosen without chance; ``u`` fp32 [T], ``u_next`` fp32 [n]:
+    uniform in [0, 1).  Returns (path [n, max_q] with -1 behind the kept nodes, count [n],
+    next token [n]), int32."""
+    dev = _gpu(token, "token")
+    if stream is not None or dev != _cur_device():
+        with _placed(dev, stream):
+            return tree_verify(token, parent, q_start, max_q, P, u, u_next, Q, replace)
+    T, V = P.shape
+    n = u_next.shape[0]
+    pp, lp = _rows(P, "P", T, V, _F32T, dev)
+    pq, lq = (None, V) if Q is None else _rows(Q, "Q", T, V, _F32T, dev)
+    path = token.new_empty((n, max_q))
+    count, nxt = token.new_empty(n), token.new_empty(n)
+    _check(lib().oq_tree_verify(
+        n, min(max_q, T), T, _arg(q_start, "q_start", _I32, (n + 1,), dev), _arg(parent, "parent", _I32, (T,), dev),
+        _arg(token, "token", _I32, (T,), dev), pp, lp, pq, lq, V, int(bool(replace)), _arg(u, "u", _F32T, (T,), dev),
+        _arg(u_next, "u_next", _F32T, (n,), dev), path.data_ptr(), max_q, count.data_ptr(), nxt.data_ptr(),
+        _raw_stream(dev)))
+    return path, count, nxt
