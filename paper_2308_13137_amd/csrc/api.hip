@@ -2338,6 +2338,11 @@ oq_status check_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, const i
   return OQ_OK;
 }
 
+TreePlan tree_plan(const oq_kv_cache* c, const oq_kv_batch* b, int heads) {
+  return tree_attend_plan(b->n_seq, c->kv_heads, heads, b->tokens, b->max_q, int64_t(b->max_pages) * c->page,
+                          c->head_dim);
+}
+
 #define OQ_TRY(expr)              \
   do {                            \
     oq_status s_ = (expr);        \
@@ -2514,8 +2519,9 @@ oq_status oq_kv_attend_tree_workspace_size(const oq_kv_cache* cache, const oq_kv
   OQ_REQ(bytes, "bytes is required");
   OQ_TRY(check_cache(cache, batch));
   OQ_TRY(check_heads(cache, heads));
-  const AttendPlan p = attend_plan(cache, batch, heads);
-  *bytes = (p.few_floats + p.many_floats) * 4;
+  *bytes = batch->n_seq == 0 || batch->max_q == 0
+               ? 0
+               : tree_plan(cache, batch, heads).bytes;
   return OQ_OK;
 }
 
@@ -2526,8 +2532,12 @@ oq_status oq_kv_attend_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, 
   OQ_TRY(check_tree(cache, batch, parent));
   OQ_TRY(check_queries(cache, batch, Q, ld_q, heads, O, LSE, ws));
   if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
-  const AttendPlan plan = attend_plan(cache, batch, heads);
-  OQ_TRY(check_plan(cache, batch, heads, plan, ws, ws_bytes));
+  const TreePlan plan = tree_plan(cache, batch, heads);
+  if (plan.tiles * cache->kv_heads > (1 << 22))
+    return fail(OQ_ERR_UNSUPPORTED, "%lld row tiles of %d key heads: too many for one call", (long long)plan.tiles,
+                cache->kv_heads);
+  if (!ws || ws_bytes < plan.bytes)
+    return fail(OQ_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws ? ws_bytes : size_t(0), plan.bytes);
   ProfScope ps(PK_CACHE_ATTN, st, 4.0 * double(batch->tokens) * heads * cache->head_dim);
   CacheArgs c = cache_args(cache, batch);
   c.parent = parent;

@@ -246,6 +246,637 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int3
   }
 }
 
+// ------------------------------------------------------------------ attention
+// Few rows (decoding): one workgroup takes 16 R rows of one key head and a split's
+// tokens, dealt to its four waves in chunks of 32.  Codes go from memory straight
+// into operand registers, the next chunk's in flight meanwhile; each wave has a
+// softmax of its own, the four are joined in LDS and the splits by a second kernel.
+//   S^T = K Q^T: a lane holds query row r, tokens 4 g + 0..3 of both 16-token
+//   tiles, which is the B operand of O^T = V^T P^T as it stands.
+// HBM-bound: 131,072 tokens x 8 key heads 44 us (6.1 TB/s, some from the last-level
+// cache), 64 sequences of up to 8,192 x 8 heads 100 us (5.1 TB/s).  Three waves to a
+// SIMD and loads past the caches: 256 sequences of up to 1,024 x 32 heads took 218 us,
+// 254 with two waves, 302 without either.  Sequences with more rows are the tile
+// kernel's.
+template <int DH, int R>
+__global__ __launch_bounds__(256, R == 1 ? 3 : 2) void cache_attend_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
+                                                           int64_t ldq, int H, uint16_t* __restrict__ O,
+                                                           float* __restrict__ LSE, float* __restrict__ part,
+                                                           int splits) {
+  constexpr int KS = DH / 32, JD = DH / 16;
+  __shared__ float s_o[4][16 * R][DH + 4];
+  __shared__ float s_ml[4][16 * R][2];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int split = blockIdx.x, u = blockIdx.y, i = blockIdx.z;
+  const int G = H / c.Hkv, P = c.P;
+  const Seq s = seq_of(c, i);
+  const int rows = s.n * G;
+  if (rows == 0 || rows > 16 * R) return;
+  const int total = s.ok ? s.L + s.n : 0;
+  const float sc = 1.4426950408889634f / sqrtf(float(DH));
+
+  bf16x8_t qf[R][KS];
+  int lim[R];                                            // the last token this lane's row sees
+  f32x4_t acc[R][JD];
+  float m[R], l[R], vref = VREF0;
+#pragma unroll
+  for (int h = 0; h < R; ++h) {
+    const int row = min(16 * h + r, rows - 1);
+    lim[h] = s.L + row / G;
+    load_q<DH>(qf[h], Q, ldq, s, u, G, row, g);
+    m[h] = -INFINITY;
+    l[h] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < JD; ++j) acc[h][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const int nch = (total + 31) / 32, ncode = (total >> c.lgP) * (P / 32), per = (nch + splits - 1) / splits;
+  const int c0 = split * per + wave, c1 = min(nch, (split + 1) * per), c1c = min(c1, ncode);
+  auto id_of = [&](int ch) { return ch < c1c ? c.table[int64_t(i) * c.max_pages + ((32 * ch) >> c.lgP)] : -1; };
+  auto scores = [&](int h, const bf16x8_t (&kf)[2][KS], int t0, f32x4_t (&st)[2]) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      st[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) st[a] = mfma(kf[a][k], qf[h][k], st[a]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) st[a][q] = t0 + 16 * a + 4 * g + q > lim[h] ? -INFINITY : st[a][q];
+    }
+  };
+  auto rescale = [&](int h, float alpha) {
+    if (__any(alpha != 1.0f)) {
+#pragma unroll
+      for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * alpha;
+    }
+  };
+  int ch = c0;
+  if (ch < c1c) {
+    Codes<DH> nx;
+    nx.load(c, id_of(ch), u, 32 * ch & (P - 1), lane);
+    int idn = id_of(ch + 4);
+    for (; ch < c1c; ch += 4) {
+      const int t0 = 32 * ch;
+      Codes<DH> cur = nx;
+      if (ch + 4 < c1c) {
+        nx.load(c, idn, u, 32 * (ch + 4) & (P - 1), lane);
+        idn = id_of(ch + 8);
+      }
+      // a page that stands for NaN: rows that see it are NaN, any finite step will do
+      if (!(cur.ks < INFINITY && cur.vs < INFINITY)) {
+#pragma unroll
+        for (int h = 0; h < R; ++h)
+          if (lim[h] >= t0) l[h] = NAN;
+        cur.ks = cur.vs = 1.0f;
+      }
+      cur.ks = fmaxf(cur.ks, KS_MIN);
+      cur.vs = fmaxf(cur.vs, VS_MIN);
+      const float vr = fmaxf(vref, pow2_above(cur.vs));
+      const float shrink = vref * pow2_inv(vr);
+      const Step sp[1] = {step_of(step_parts(cur.ks * sc, cur.vs), vr, true)};
+      bf16x8_t kf[2][KS];
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int j = 0; j < KS / 2; ++j) {
+          const u32x4_t w = cur.k[a * (KS / 2) + j];
+          kf[a][2 * j] = codes_bf16(w[0], w[1]);
+          kf[a][2 * j + 1] = codes_bf16(w[2], w[3]);
+        }
+      f16x8_t pb[R];
+#pragma unroll
+      for (int h = 0; h < R; ++h) {
+        f32x4_t st[2];
+        scores(h, kf, t0, st);
+        rescale(h, softmax_step<1>(st, sp, m[h], l[h]) * shrink);
+        u32x4_t w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack_f16(st[e >> 1][2 * (e & 1)], st[e >> 1][2 * (e & 1) + 1]);
+        pb[h] = __builtin_bit_cast(f16x8_t, w);
+      }
+      vref = vr;
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        const f16x8_t v0 = codes_f16(cur.v[j][0], cur.v[j][1]), v1 = codes_f16(cur.v[j][2], cur.v[j][3]);
+#pragma unroll
+        for (int h = 0; h < R; ++h) {
+          acc[h][2 * j] = mfma_h(v0, pb[h], acc[h][2 * j]);
+          acc[h][2 * j + 1] = mfma_h(v1, pb[h], acc[h][2 * j + 1]);
+        }
+      }
+    }
+  }
+  if (ch < c1) {                                         // the open page's step is 1
+    const float vr = fmaxf(vref, 1.0f), shrink = vref * pow2_inv(vr);
+#pragma unroll
+    for (int h = 0; h < R; ++h)
+#pragma unroll
+      for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * shrink;
+    vref = vr;
+  }
+  for (; ch < c1; ch += 4) {
+    const int t0 = 32 * ch;
+    bf16x8_t kf[2][KS], vf[JD];
+    const Window<DH> win(c, s, u, t0, total, lane);
+    unsigned bad = 0;
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[a][k] = __builtin_bit_cast(bf16x8_t, win.key(a, k));
+#pragma unroll
+    for (int j = 0; j < JD; ++j) vf[j] = __builtin_bit_cast(bf16x8_t, win.value(j));
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) win.check_key(__builtin_bit_cast(u32x4_t, kf[a][k]), a, bad);
+#pragma unroll
+    for (int j = 0; j < JD; ++j)
+      vf[j] = __builtin_bit_cast(bf16x8_t, win.check_value(__builtin_bit_cast(u32x4_t, vf[j]), bad));
+    bad = wave_or(bad);
+    const Step sp[1] = {step_of(step_parts(sc, 1.0f), vref, false)};
+#pragma unroll
+    for (int h = 0; h < R; ++h) {
+      if (bad && lim[h] >= t0 + __ffs(int(bad)) - 1) l[h] = NAN;
+      f32x4_t st[2];
+      scores(h, kf, t0, st);
+      rescale(h, softmax_step<1>(st, sp, m[h], l[h]));
+      u32x4_t wh, wl;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = st[e >> 1][2 * (e & 1)], y = st[e >> 1][2 * (e & 1) + 1];
+        wh[e] = f2bf2(x, y);
+        wl[e] = f2bf2(x - __uint_as_float(wh[e] << 16), y - __uint_as_float(wh[e] & 0xffff0000u));
+      }
+#pragma unroll
+      for (int j = 0; j < JD; ++j) {
+        acc[h][j] = mfma(vf[j], __builtin_bit_cast(bf16x8_t, wh), acc[h][j]);
+        acc[h][j] = mfma(vf[j], __builtin_bit_cast(bf16x8_t, wl), acc[h][j]);
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < R; ++h) {
+    l[h] = row_sum(l[h]);
+#pragma unroll
+    for (int j = 0; j < JD; ++j)
+      *reinterpret_cast<f32x4_t*>(&s_o[wave][16 * h + r][16 * j + 4 * g]) = acc[h][j] * (vref / WUNIT);
+    if (g == 0) {
+      s_ml[wave][16 * h + r][0] = m[h];
+      s_ml[wave][16 * h + r][1] = l[h];
+    }
+  }
+  __syncthreads();
+  const Out out = out_of(O, LSE, part, splits, split, H, c.T, int64_t(c.n_seq) * c.Hkv, int64_t(i) * c.Hkv + u, 16 * R, DH);
+  for (int e = tid; e < 4 * R * DH; e += 256) {          // 16 R rows of DH / 4 fours
+    const int row = e / (DH / 4), c4 = 4 * (e % (DH / 4));
+    if (row >= rows) break;
+    float mm = -INFINITY, ll = 0.0f;
+    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][row][0]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = 0; w < 4; ++w) {
+      const float mw = s_ml[w][row][0], lw = s_ml[w][row][1];
+      const float f = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - mm);
+      ll += mw == -INFINITY ? lw : f * lw;               // (no token, or NaN)
+      const float4 x = *reinterpret_cast<const float4*>(&s_o[w][row][c4]);
+      o = make_float4(o.x + f * x.x, o.y + f * x.y, o.z + f * x.z, o.w + f * x.w);
+    }
+    if (!s.ok) ll = NAN;
+    const int64_t t = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
+    put4(out, row, t, hd, DH, c4, o, ll);
+    if (c4 == 0) put_ml(out, row, t, hd, mm, ll);
+  }
+}
+
+// Tiles of `qw` rows of one key head's rows: the w-th of all sequences' as (sequence,
+// tile), (-1, 0) past the last.  Where up to 32 sequences have several tiles each, the
+// tiles that see the most tokens come first, against an order by place (the k-th tile
+// from the end of each sequence in turn): 16 chunks of up to 512 tokens over up to
+// 4,096, 16 heads, 188 -> 142 us; two of up to 2,048 over up to 4,096, 32 heads, 216
+// -> 202; but 60 chunks of up to 256 tokens 157 -> 172, and 8 of 16 tokens (one tile
+// each) 63 -> 77.  A tile's level is its place from the sequence's beginning, in
+// tiles; from level b up there are sum_i clamp(end_i - b, 0, tiles_i), which 64 lanes
+// evaluate at 64 levels at once.
+enum TileOrder { BY_PLACE, BY_SEARCH, BY_LEVEL };
+OQ_DEV Unit row_tile(const CacheArgs& c, int G, int qw, int rows_min, int w, int order, int levels) {
+  auto tiles = [&](const Seq& s) { return s.n * G < rows_min ? 0 : (s.n * G + qw - 1) / qw; };
+  if (order != BY_LEVEL) {
+    Unit un = unit_of(c.n_seq, w, order == BY_PLACE, [&](int j) { return tiles(seq_of(c, j)); });
+    // a sequence's last tile first
+    if (un.i >= 0) un.k = (order == BY_PLACE ? (c.max_q * G + qw - 1) / qw : tiles(seq_of(c, un.i))) - 1 - un.k;
+    return un;
+  }
+  const int lane = threadIdx.x & 63;
+  int n = 0, first = 0;                                    // the lane's sequence: tiles, the first one's level
+  if (lane < c.n_seq) {
+    const Seq s = seq_of(c, lane);
+    n = tiles(s);
+    first = s.ok ? int(int64_t(s.L) * G / qw) : 0;
+  }
+  const uint64_t some = __ballot(n > 0);
+  auto from = [&](int b) {                                 // tiles of level b and up
+    int sum = 0;
+    for (uint64_t left = some; left; left &= left - 1) {
+      const int i = __ffsll(static_cast<unsigned long long>(left)) - 1;
+      const int ni = __builtin_amdgcn_readlane(n, i), end = __builtin_amdgcn_readlane(first, i) + ni;
+      sum += min(max(end - b, 0), ni);
+    }
+    return sum;
+  };
+  int lo = 0, hi = levels;                                 // the level is in [lo, hi)
+  while (true) {
+    const int step = (hi - lo + 63) / 64, b = lo + lane * step, over = from(b);
+    const uint64_t past = __ballot(b < hi && over > w);
+    if (!past) return {-1, 0};
+    lo += (__popcll(past) - 1) * step;
+    if (step == 1) break;
+    hi = min(hi, lo + step);
+  }
+  uint64_t at = __ballot(n > 0 && first <= lo && lo < first + n);
+  for (int j = w - from(lo + 1); j > 0; --j) at &= at - 1;
+  const int i = __ffsll(static_cast<unsigned long long>(at)) - 1;
+  return {i, lo - __builtin_amdgcn_readlane(first, i)};
+}
+
+// Many rows (prompts): one workgroup of four waves takes 64 R rows of one key head,
+// 16 R per wave, over tiles of 64 tokens.  The waves turn a tile's codes into f16
+// operands once, in LDS, a tile ahead; the raw codes of the one after are in
+// flight meanwhile.  Two workgroups to a compute unit.  Neither unit is busy all the
+// time: over a whole launch the vector units (softmax, conversion) 48%, the matrix
+// units 26%, at 1.5 of 2 waves a SIMD, so a wave's products, softmax and products again
+// mostly follow one another, and a quarter of the wave slots is empty at the ends.  Two
+// chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 203 us, 652 TFLOP/s;
+// 4,096 tokens at 64 heads, 8 key heads, 339 us, 812 TFLOP/s.
+//
+// Queries enter Q K^T as f16 too, each row scaled by a power of two that puts its
+// largest entry between 2^14 and 2^15: bf16's 8 bits fit, and what is lost is below
+// 2^-39 of that entry.  (Of a row below 2^-71 what is lost is below 2^-110: a smaller
+// factor times KS_MIN would leave fp32.)
+//
+// TWO: pages of 32 tokens, a tile's chunks lie in two pages.  A row's unit of the weights
+// is its own then: rows that see only the first chunk must not lose bits to the other
+// page's V step (two chunks of up to 2,048 tokens over up to 4,096, 32 heads of 128, 210
+// -> 217 us).  Larger pages hold both chunks: one step and one unit for all rows.
+template <int DH, int R, bool TWO>
+__global__ __launch_bounds__(256, 2) void cache_attend_tile_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
+                                                                       int64_t ldq, int H,
+                                                                       uint16_t* __restrict__ O,
+                                                                       float* __restrict__ LSE,
+                                                                       float* __restrict__ part, int splits,
+                                                                       int rows_min, int units, int order, int levels) {
+  constexpr int KS = DH / 32, JD = DH / 16, QW = 64 * R;
+  constexpr int TILE = 64 * DH / 8;                      // 16-byte pieces of one operand's tile
+  constexpr int CW = 2, LPW = JD / CW;                   // waves of a chunk, loads of a wave
+  static_assert(LPW == KS, "half a chunk's keys are one 16-token tile");
+  __shared__ u32x4_t s_k[2][TILE], s_v[2][TILE];
+  __shared__ float4 s_step[2][2];                        // [buffer][chunk], step_parts
+  __shared__ unsigned s_bad[2][2][CW];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // key heads fastest (an XCD keeps its heads' pages in its L2)
+  const int G = H / c.Hkv, P = c.P;
+  int x = int(blockIdx.x);
+  const int u = x % c.Hkv;
+  x /= c.Hkv;
+  const int split = x % splits, w = x / splits;
+  const Unit un = row_tile(c, G, QW, rows_min, w, order, levels);
+  if (un.i < 0) return;
+  const int i = un.i;
+  const Seq s = seq_of(c, i);
+  const int rows = s.n * G, row0 = un.k * QW;
+  if (rows < rows_min || row0 >= rows) return;
+  const int total = s.ok ? s.L + s.n : 0, closed = total & ~(P - 1);
+  const float sc = 1.4426950408889634f / sqrtf(float(DH));
+
+  bf16x8_t qf[R][KS];                                    // f16 (times 1 / qs), bf16 for the open page
+  float qs[R];
+  int lim[R];                                            // the last token this lane's row sees
+  f32x4_t acc[R][JD];
+  float m[R], l[R], vref[TWO ? R : 1];
+  auto row_of = [&](int h) { return min(row0 + 16 * (R * wave + h) + r, rows - 1); };
+#pragma unroll
+  for (int h = 0; h < R; ++h) {
+    lim[h] = s.L + row_of(h) / G;
+    load_q<DH>(qf[h], Q, ldq, s, u, G, row_of(h), g);
+    float top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(float(qf[h][k][e])));
+    const int e = min(max(int(__float_as_uint(row_max(top)) >> 23), 56), 253);
+    const float up = __uint_as_float(uint32_t(268 - e) << 23);   // 2^(14 - exponent)
+    qs[h] = __uint_as_float(uint32_t(e - 14) << 23);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      u32x4_t w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = pack_f16(float(qf[h][k][2 * q]) * up, float(qf[h][k][2 * q + 1]) * up);
+      qf[h][k] = __builtin_bit_cast(bf16x8_t, w);
+    }
+    m[h] = -INFINITY;
+    l[h] = 0.0f;
+    vref[TWO ? h : 0] = VREF0;
+#pragma unroll
+    for (int j = 0; j < JD; ++j) acc[h][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const int first_lim = s.L + row0 / G;                  // what every row of the tile sees
+  const int seen = s.ok ? s.L + min(row0 + QW - 1, rows - 1) / G + 1 : 0;
+  const int nt = (seen + 63) / 64, per = (nt + splits - 1) / splits;
+  const int k0 = split * per, k1 = min(nt, (split + 1) * per);
+  const int ntc = closed / 64;                           // tiles of full pages only
+  // this wave's share of a tile: the keys or the values of chunk cc
+  const int cc = wave >> 1, hw = wave & 1;
+  const bool vals = hw != 0;
+  u32x4_t raw[LPW];
+  float ks = 0.0f, vs = 0.0f;
+  // The page of this wave's chunk of tile t (a page number is a load of its own: it
+  // is fetched a tile before the codes are).  Page numbers and steps come by vector
+  // loads, though the whole wave reads one word: scalar loads share a counter with
+  // the LDS reads, whose waits would then last until memory has answered.
+  int zero = 0;
+  asm("" : "+v"(zero));
+  auto id_of = [&](int t) {
+    return t < k1 && 64 * t + 32 * cc < closed
+               ? c.table[int64_t(i) * c.max_pages + ((64 * t + 32 * cc) >> c.lgP) + zero]
+               : -1;
+  };
+  int idn = id_of(k0);
+  auto load = [&](int t) __attribute__((always_inline)) {   // tile t, if its chunk is in a full page
+    const int t0 = 64 * t + 32 * cc, id = page_in(c, __builtin_amdgcn_readfirstlane(idn));
+    if (t0 < closed) {
+      const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
+      if (hw == 0) {
+        ks = id < 0 ? NAN : c.ks[blk + zero];
+        vs = id < 0 ? NAN : c.vs[blk + zero];
+      }
+      const u32x4_t* p = reinterpret_cast<const u32x4_t*>((vals ? c.vc : c.kc) + blk * P * DH + (t0 & (P - 1)) * DH) + lane;
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) raw[j] = p[64 * j];
+      idn = id_of(t + 1);
+    }
+  };
+  auto steps = [&](int b) {
+    if (hw == 0 && lane == 0) {
+      const bool fine = ks < INFINITY && vs < INFINITY;
+      s_step[b][cc] = step_parts(fine ? fmaxf(ks, KS_MIN) * sc : sc, fine ? fmaxf(vs, VS_MIN) : 1.0f);
+      s_bad[b][cc][0] = fine ? 0u : 1u;
+    }
+    if (hw > 0 && lane == 0) s_bad[b][cc][hw] = 0u;
+  };
+  // Operands of tile t into buffer b, fragment f of a chunk (64 lanes) at 64 f: f16,
+  // or bf16 where the tile reaches into the open page (from ntc on).
+  auto store = [&](int t, int b) __attribute__((always_inline)) {
+    const int t0 = 64 * t + 32 * cc;
+    u32x4_t* dst = (vals ? s_v[b] : s_k[b]) + cc * JD * 64 + lane;
+    if (t0 < closed) {
+      if (t < ntc) {
+#pragma unroll
+        for (int j = 0; j < 2 * LPW; ++j)
+          dst[64 * j] = __builtin_bit_cast(u32x4_t, codes_f16(raw[j / 2][2 * (j & 1)], raw[j / 2][2 * (j & 1) + 1]));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2 * LPW; ++j)
+          dst[64 * j] = __builtin_bit_cast(u32x4_t, codes_bf16(raw[j / 2][2 * (j & 1)], raw[j / 2][2 * (j & 1) + 1]));
+      }
+      steps(b);
+    } else {
+      // (past every row's limit zeros, any finite operands)
+      unsigned bad = 0;
+      if (t0 < seen) {
+        const Window<DH> win(c, s, u, t0, total, lane);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          u32x4_t w[LPW];
+#pragma unroll
+          for (int j = 0; j < LPW; ++j) w[j] = vals ? win.value(LPW * half + j) : win.key(half, j);
+#pragma unroll
+          for (int j = 0; j < LPW; ++j) {
+            if (vals) w[j] = win.check_value(w[j], bad);
+            else win.check_key(w[j], half, bad);
+            dst[64 * (half * LPW + j)] = w[j];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int f = 0; f < 2 * LPW; ++f) dst[64 * f] = u32x4_t{0u, 0u, 0u, 0u};
+      }
+      bad = wave_or(bad);
+      if (lane == 0) {
+        if (hw == 0) s_step[b][cc] = step_parts(sc, 1.0f);
+        s_bad[b][cc][hw] = bad;
+      }
+    }
+  };
+  if (k0 < k1) {
+    load(k0);
+    store(k0, 0);
+    if (k0 + 1 < k1) load(k0 + 1);
+  }
+  // OPEN: the tile reaches into the open page; the weights enter as pairs of bf16 terms.
+  auto tile = [&](int t, auto open) __attribute__((always_inline)) {
+    constexpr bool OPEN = decltype(open)::value;
+    const int b = (t - k0) & 1, t0 = 64 * t;
+    __syncthreads();                                     // tile t is in buffer b, the other is free
+    // operands are read from LDS AH ahead of their products
+    constexpr int AH = 4;
+    const u32x4_t *sk = &s_k[b][lane], *sv = &s_v[b][lane];
+    u32x4_t kf[AH];
+#pragma unroll
+    for (int x = 0; x < AH; ++x) kf[x] = sk[64 * x];
+    if (t + 1 < k1) {
+      store(t + 1, b ^ 1);
+      if (t + 2 < k1) load(t + 2);
+    }
+    f32x4_t st[R][4];
+#pragma unroll
+    for (int x = 0; x < 4 * KS; ++x) {
+      const int a = x / KS, k = x % KS;
+      const u32x4_t f = kf[x % AH];
+#pragma unroll
+      for (int h = 0; h < R; ++h) {
+        if (k == 0) st[h][a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if constexpr (OPEN) st[h][a] = mfma(__builtin_bit_cast(bf16x8_t, f), qf[h][k], st[h][a]);
+        else st[h][a] = mfma_h(__builtin_bit_cast(f16x8_t, f), __builtin_bit_cast(f16x8_t, qf[h][k]), st[h][a]);
+      }
+      if (x + AH < 4 * KS) kf[x % AH] = sk[64 * (x + AH)];
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (t0 + 63 > first_lim) {
+#pragma unroll
+      for (int h = 0; h < R; ++h)
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (t0 + 16 * a + 4 * g + q > lim[h]) st[h][a][q] = -INFINITY;
+    }
+    unsigned bad0 = 0, bad1 = 0;
+#pragma unroll
+    for (int w = 0; w < CW; ++w) {
+      bad0 |= s_bad[b][0][w];
+      bad1 |= s_bad[b][1][w];
+    }
+    if (bad0 | bad1) {
+      // (a full page that stands for NaN: from its chunk's first token on)
+#pragma unroll
+      for (int h = 0; h < R; ++h) {
+        if (bad0 && lim[h] >= t0 + __ffs(int(bad0)) - 1) l[h] = NAN;
+        if (bad1 && lim[h] >= t0 + 32 + __ffs(int(bad1)) - 1) l[h] = NAN;
+      }
+    }
+    const float4 q0 = s_step[b][0], q1 = TWO ? s_step[b][1] : q0;
+    float shrink;
+    Step s0, s1;
+    auto unit = [&](float& vref, bool both) {
+      const float vr = fmaxf(vref, TWO && both ? fmaxf(pow2_above(q0.y), pow2_above(q1.y)) : pow2_above(q0.y));
+      shrink = vref * pow2_inv(vr);
+      vref = vr;
+      s0 = step_of(q0, vr, !OPEN || (TWO && t0 < closed));
+      s1 = TWO ? step_of(q1, vr, !OPEN) : s0;
+    };
+    if constexpr (!TWO) unit(vref[0], true);
+    u32x4_t vf[AH];
+#pragma unroll
+    for (int x = 0; x < AH; ++x) vf[x] = sv[64 * x];
+#pragma unroll
+    for (int h = 0; h < R; ++h) {
+      if constexpr (TWO) unit(vref[h], lim[h] >= t0 + 32);
+      Step sp[2] = {s0, s1};
+      if constexpr (!OPEN) {
+        sp[0].f *= qs[h];
+        sp[1].f *= qs[h];
+      }
+      const float alpha = softmax_step<2>(st[h], sp, m[h], l[h]) * shrink;
+      if (__any(alpha != 1.0f)) {
+#pragma unroll
+        for (int j = 0; j < JD; ++j) acc[h][j] = acc[h][j] * alpha;
+      }
+    }
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      u32x4_t ph[R], pl[OPEN ? R : 1];
+#pragma unroll
+      for (int h = 0; h < R; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = st[h][2 * k2 + (e >> 1)][2 * (e & 1)], p1 = st[h][2 * k2 + (e >> 1)][2 * (e & 1) + 1];
+          if constexpr (OPEN) {
+            ph[h][e] = f2bf2(p0, p1);
+            pl[h][e] = f2bf2(p0 - __uint_as_float(ph[h][e] << 16), p1 - __uint_as_float(ph[h][e] & 0xffff0000u));
+          } else {
+            ph[h][e] = pack_f16(p0, p1);
+          }
+        }
+#pragma unroll
+      for (int j = 0; j < JD; ++j) {
+        const int x = k2 * JD + j;
+        const u32x4_t v = vf[x % AH];
+#pragma unroll
+        for (int h = 0; h < R; ++h) {
+          if constexpr (OPEN) {
+            acc[h][j] = mfma(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, ph[h]), acc[h][j]);
+            acc[h][j] = mfma(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, pl[h]), acc[h][j]);
+          } else {
+            acc[h][j] = mfma_h(__builtin_bit_cast(f16x8_t, v), __builtin_bit_cast(f16x8_t, ph[h]), acc[h][j]);
+          }
+        }
+        if (x + AH < 2 * JD) vf[x % AH] = sv[64 * (x + AH)];
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  int t = k0;
+  for (; t < min(k1, ntc); ++t) tile(t, std::false_type{});
+  if (t < k1) {
+#pragma unroll
+    for (int h = 0; h < R; ++h) load_q<DH>(qf[h], Q, ldq, s, u, G, row_of(h), g);
+  }
+  for (; t < k1; ++t) tile(t, std::true_type{});
+  const Out out = out_of(O, LSE, part, splits, split, H, c.T, int64_t(units) * c.Hkv, int64_t(w) * c.Hkv + u, QW, DH);
+#pragma unroll
+  for (int h = 0; h < R; ++h) {
+    l[h] = row_sum(l[h]);
+    const int row = row0 + 16 * (R * wave + h) + r;
+    if (row >= rows) continue;
+    if (!s.ok) l[h] = NAN;
+    const int64_t tok = int64_t(s.b) + row / G, hd = int64_t(u) * G + row % G;
+#pragma unroll
+    for (int j = 0; j < JD; ++j) {
+      const f32x4_t o = acc[h][j] * (vref[TWO ? h : 0] / WUNIT);
+      put4(out, row - row0, tok, hd, DH, 16 * j + 4 * g, make_float4(o[0], o[1], o[2], o[3]), l[h]);
+    }
+    if (g == 0) put_ml(out, row - row0, tok, hd, m[h], l[h]);
+  }
+}
+
+// Joins a row's splits: DH / 4 lanes of four output values each, NG groups of them
+// dealing the splits among themselves; 256 threads take RW rows of a unit, of the
+// row kernel's first.
+struct JoinArgs {
+  const float *few, *many;           // shares of the two kernels
+  int few_splits, many_splits, row_rows, tile_rows, units;
+  int few_rows;                      // rows of a unit of the row kernel that can be in use
+  int few_blocks;
+  int order, levels;
+};
+template <int DH, int NG>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs c, int H, JoinArgs a, uint16_t* __restrict__ O,
+                                                         float* __restrict__ LSE) {
+  constexpr int Q4 = DH / 4, RW = 256 / (Q4 * NG);
+  __shared__ float4 s_o[NG][RW][Q4];
+  __shared__ float2 s_ml[NG][RW];
+  const int G = H / c.Hkv;
+  const bool few = int(blockIdx.x) < a.few_blocks;
+  const int unit_rows = few ? a.row_rows : a.tile_rows, blocks = ((few ? a.few_rows : a.tile_rows) + RW - 1) / RW;
+  const int bid = int(blockIdx.x) - (few ? 0 : a.few_blocks), unit = bid / blocks, u = unit % c.Hkv;
+  const Unit un = few ? Unit{unit / c.Hkv, 0}
+                      : row_tile(c, G, a.tile_rows, a.row_rows + 1, unit / c.Hkv, a.order, a.levels);
+  if (un.i < 0) return;
+  const Seq s = seq_of(c, un.i);
+  const int rows = s.n * G, row0 = un.k * unit_rows;
+  const int lane = threadIdx.x % Q4, ng = (threadIdx.x / Q4) % NG, rw = threadIdx.x / (Q4 * NG);
+  const int at0 = (bid % blocks) * RW;                     // the block's first row of the unit
+  if (few != (rows <= a.row_rows) || row0 + at0 >= rows) return;
+  const bool in = at0 + rw < unit_rows && row0 + at0 + rw < rows;
+  const int row = in ? row0 + at0 + rw : row0 + at0, j = row / G, hd = u * G + row % G;
+  const int splits = few ? a.few_splits : a.many_splits;
+  const int64_t units = int64_t(few ? c.n_seq : a.units) * c.Hkv, at = int64_t(unit) * unit_rows + (row - row0);
+  const float* part = few ? a.few : a.many;
+  const float2* ml = reinterpret_cast<const float2*>(part + splits * units * unit_rows * DH);
+  float m = -INFINITY, l = 0.0f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto join = [&](float mk, float lk, float4 x) {
+    const float mn = fmaxf(m, mk);
+    const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+    const float fk = mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - mn);
+    // (without a token l is 0 or, for a NaN row, NaN: it stays)
+    l = (m == -INFINITY ? l : f * l) + (mk == -INFINITY ? lk : fk * lk);
+    o = make_float4(f * o.x + fk * x.x, f * o.y + fk * x.y, f * o.z + fk * x.z, f * o.w + fk * x.w);
+    m = mn;
+  };
+#pragma unroll 4
+  for (int k = ng; k < splits; k += NG) {
+    const int64_t p = k * units * unit_rows + at;
+    const float2 w = ml[p];
+    join(w.x, w.y, *reinterpret_cast<const float4*>(part + p * DH + 4 * lane));
+  }
+  if constexpr (NG > 1) {
+    s_o[ng][rw][lane] = o;
+    if (lane == 0) s_ml[ng][rw] = make_float2(m, l);
+    __syncthreads();
+    if (ng > 0) return;
+#pragma unroll
+    for (int k = 1; k < NG; ++k) {
+      const float2 w = s_ml[k][rw];
+      join(w.x, w.y, s_o[k][rw][lane]);
+    }
+  }
+  if (!in) return;
+  const float inv = 1.0f / l;
+  const int64_t t = int64_t(s.b) + j;
+  *reinterpret_cast<uint2*>(O + (t * H + hd) * DH + 4 * lane) =
+      make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
+  if (LSE && lane == 0) LSE[hd * c.T + t] = lse_of(m, l);
+}
+
 }  // namespace
 
 hipError_t cache_append(const CacheArgs& c, const void* Q, int64_t ldq, const void* K, int64_t ldk,
@@ -355,7 +986,48 @@ AttendPlan cache_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_
 
 hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int H, uint16_t* O, float* LSE,
                         float* ws, const AttendPlan& p, hipStream_t st) {
-  return attend_launch<false>(c, Q, ldq, H, O, LSE, ws, p, st);
+  const int G = H / c.Hkv;
+  float* ws_many = ws + p.few_floats;
+  auto few = [&](auto dh, auto rr) {
+    constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
+    const dim3 grid(unsigned(p.few), unsigned(c.Hkv), unsigned(c.n_seq));
+    hipLaunchKernelGGL((cache_attend_kernel<DH, R>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, p.few);
+  };
+  auto many_of = [&](auto dh, auto rr, auto two) {
+    constexpr int DH = decltype(dh)::value, R = decltype(rr)::value;
+    constexpr bool TWO = decltype(two)::value;
+    const dim3 grid(unsigned(p.units * p.many * c.Hkv));
+    hipLaunchKernelGGL((cache_attend_tile_kernel<DH, R, TWO>), grid, dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws_many,
+                       p.many, p.row_rows + 1, int(p.units), p.order, int(p.levels));
+  };
+  auto many = [&](auto dh, auto rr) {
+    if (c.P == 32) many_of(dh, rr, std::true_type{});
+    else many_of(dh, rr, std::false_type{});
+  };
+  auto join = [&](auto dh, auto ng) {
+    constexpr int DH = decltype(dh)::value, NG = decltype(ng)::value, RW = 1024 / (DH * NG);
+    const int few_rows = int(std::min<int64_t>(p.row_rows, int64_t(c.max_q) * G));
+    const int64_t few_blocks = p.few > 1 ? int64_t((few_rows + RW - 1) / RW) * c.Hkv * c.n_seq : 0;
+    const int64_t many_blocks = p.many > 1 ? p.units * c.Hkv * (p.tile_rows / RW) : 0;
+    const JoinArgs a{ws, ws_many, p.few, p.many, p.row_rows, p.tile_rows, int(p.units), few_rows, int(few_blocks),
+                     p.order, int(p.levels)};
+    hipLaunchKernelGGL((cache_join_kernel<DH, NG>), dim3(unsigned(few_blocks + many_blocks)), dim3(256), 0, st, c, H,
+                       a, O, LSE);
+  };
+  auto run = [&](auto dh) {
+    const std::integral_constant<int, 1> i1{};
+    const std::integral_constant<int, 2> i2{};
+    if (p.tile_rows == 64) many(dh, i1);
+    else if (p.tile_rows) many(dh, i2);
+    if (p.row_rows == 16) few(dh, std::integral_constant<int, 1>{});
+    else if (p.row_rows) few(dh, std::integral_constant<int, 2>{});
+    const int splits = std::max(p.few, p.many);
+    if (splits > 8) join(dh, std::integral_constant<int, 8>{});
+    else if (splits > 1) join(dh, std::integral_constant<int, 1>{});
+  };
+  if (c.d == 64) run(std::integral_constant<int, 64>{});
+  else run(std::integral_constant<int, 128>{});
+  return hipGetLastError();
 }
 
 }  // namespace oq

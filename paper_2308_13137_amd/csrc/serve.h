@@ -75,8 +75,17 @@ hipError_t cache_attend(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int 
 hipError_t cache_append_tree(const CacheArgs& c, const void* Q, int64_t ldq, const void* K, int64_t ldk,
                              const void* V, int64_t ldv, bool in_bf16, int H, const float* rope, int64_t n_rope,
                              const float* s_a, uint16_t* Qout, hipStream_t st);
+struct TreePlan {
+  int row_tiles;   // 16-row tiles of a workgroup (1, 2, 4)
+  bool one_tile;   // no sequence has more rows
+  int nw, least;   // workgroups of a key head, their smallest share
+  int shift;       // chunks of a step, as a power of two
+  int64_t tiles;   // row tiles of a key head, of all sequences, at most
+  size_t part_floats, bytes;   // pieces' results; with where they are, the workspace
+};
+TreePlan tree_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d);
 hipError_t cache_attend_tree(const CacheArgs& c, const uint16_t* Q, int64_t ldq, int H, uint16_t* O, float* LSE,
-                             float* ws, const AttendPlan& p, hipStream_t st);
+                             float* ws, const TreePlan& p, hipStream_t st);
 hipError_t cache_commit(const CacheArgs& c, const int32_t* path, int max_path, const int32_t* count, hipStream_t st);
 
 // ---------------------------------------------------------------- drafted tokens against the target
