@@ -621,7 +621,8 @@ OQ_DEV uint32_t lanes_upto(uint32_t v) {
 // line that the nw workgroups of a key head cut into equal shares: the lengths are on the
 // device, and a ragged batch is as evenly spread as one long sequence.  A tile's steps are of
 // 2^shift chunks (one, unless the line would pass 31 bits); a step belongs to the share that it
-// begins in.  A tile that several workgroups have goes to slots of the workspace (a share
+// begins in, but for a tile's first and last few, which go with their
+// neighbours: a piece costs more than they do.  A tile that several workgroups have goes to slots of the workspace (a share
 // begins with at most one such piece and ends with at most one) and is joined by
 // tree_join_kernel, whom the workgroup where it begins tells so.
 struct Cut {
@@ -664,6 +665,7 @@ __global__ __launch_bounds__(256, 2) void tree_attend_kernel(CacheArgs c, const 
     there += uint32_t(__builtin_amdgcn_readlane(int(lanes_upto(tiles_of(x))), 63));
   }
   const uint32_t share = max((whole + nw - 1) / uint32_t(nw), uint32_t(least)), lo = w * share, hi = lo + share;
+  const uint32_t snap = min(uint32_t(TILE_MORE) >> shift, share / 24);
   // (a tile's entry is written where it begins; of tiles that the host allowed for and that are not there, here)
   for (int k = int(there) + w * 256 + threadIdx.x; k < tiles; k += nw * 256) cuts[int64_t(k) * c.Hkv + u] = Cut{0, 0, 0, 0, 0};
   // from tile to tile: where the next one is looked for, what lies before `base`
@@ -692,15 +694,17 @@ __global__ __launch_bounds__(256, 2) void tree_attend_kernel(CacheArgs c, const 
     // the steps that begin in [lo, hi)
     auto steps_below = [&](uint32_t p) {
       const uint32_t d = min(max(p, t0), t1) - t0 + cost1 - 1;
-      return min(cost1 == 3 ? d / 3 : cost1 == 4 ? d / 4 : d / 6, steps);
+      const uint32_t n = min(cost1 == 3 ? d / 3 : cost1 == 4 ? d / 4 : d / 6, steps);
+      return n == steps ? n : n < snap ? 0u : n + snap > steps ? steps : n;
     };
     const uint32_t s0 = steps_below(lo), s1 = steps_below(hi);
     if (s0 >= s1) continue;
     const int64_t slot = (int64_t(w) * c.Hkv + u) * 2 + (s0 == 0);
     if (s0 == 0) {
+      const uint32_t end = (t0 + (steps - 1) * cost1) / share, to = steps_below(end * share) < steps ? end : end - 1;
       const uint32_t tile = run_tiles + uint32_t(of(int(lanes_upto(tiles_of(x)) - tiles_of(x)))) + row0 / TILE_ROWS;
       if (threadIdx.x == 0)
-        cuts[int64_t(tile) * c.Hkv + u] = Cut{s.b + row0 / G, row0 % G, n, w, int((t0 + (steps - 1) * cost1) / share) - w};
+        cuts[int64_t(tile) * c.Hkv + u] = Cut{s.b + row0 / G, row0 % G, n, w, int(to) - w};
     }
     const Out out{O, LSE, part, s0 > 0 || s1 < steps ? 2 : 1, H, c.T, slot * (16 * RMAX),
                   int64_t(nw) * c.Hkv * 2 * (16 * RMAX) * DH};

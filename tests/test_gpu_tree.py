@@ -164,6 +164,19 @@ def test_many_small_trees_beside_a_large_one():
     b.check_rows()
 
 
+@pytest.mark.parametrize("H,Hkv,lengths,n_max", [(16, 16, (0, 90), 5), (32, 16, (1, 300), 32), (64, 8, (0, 600), 20),
+                                                 (40, 8, (400, 410), 17)])
+def test_short_sequences_share_workgroups(H, Hkv, lengths, n_max):
+    """Whole tiles of many sequences in one share, and cuts near the ends of tiles."""
+    r = random.Random(H)
+    n = 70
+    b = Trees(n, H, Hkv, 64, 32, 700, seed=H, s_a=False, rope=False)
+    b.step([r.randint(*lengths) for _ in range(n)], attend=False)
+    parents = [some_tree(r.randint(0, n_max), i) if i % 9 else [] for i in range(n)]
+    parents[40] = some_tree(n_max, 3)
+    b.tree_step(parents, [some_path(p, i) for i, p in enumerate(parents)])
+
+
 @pytest.mark.parametrize("H,Hkv,n", [(4, 4, 1), (4, 4, 20), (16, 2, 6), (16, 2, 30)])
 def test_a_chain_is_a_batch_of_new_tokens(H, Hkv, n):
     """Where no page fills up a chain's queries and rows are append's, bit for bit, and its outputs attend's
