@@ -784,9 +784,9 @@ __global__ __launch_bounds__(256) void tree_join_kernel(CacheArgs c, int H, cons
 hipError_t cache_append_tree(const CacheArgs& c, const void* Q, int64_t ldq, const void* K, int64_t ldk,
                              const void* V, int64_t ldv, bool in_bf16, int H, const float* rope, int64_t n_rope,
                              const float* s_a, uint16_t* Qout, hipStream_t st) {
-  // query slices: eight items of a thread each
-  const int64_t items = int64_t(c.max_q) * H * (c.d / 8);
-  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(items / (8 * 256), 65535 - c.Hkv));
+  // query slices: eight items of a thread each where that fills the card, else two
+  const int64_t items = int64_t(c.max_q) * H * (c.d / 8), each = c.n_seq * items >= 1024 * 8 * 256 ? 8 : 2;
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(items / (each * 256), 65535 - c.Hkv));
   const dim3 grid(unsigned(c.n_seq), unsigned(c.Hkv + slices));
   auto go = [&](auto ti) {
     using TI = decltype(ti);

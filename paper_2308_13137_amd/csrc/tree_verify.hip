@@ -124,18 +124,36 @@ __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int
 // After m rejections r(x) follows from p(x), q(x) and the masses of each step alone,
 // so a child's test reads two numbers (all of them are fetched at the start), and only a
 // mass needs a pass over the vocabulary: before a further sibling, and for the draw.
-template <bool CERTAIN>
-OQ_DEV double residual(float p, float q, int x, int levels, const double* s_ir, const double* s_iz, const int* s_rej) {
-  double r = p;
-  if constexpr (CERTAIN) {
-    for (int t = 0; t < levels; ++t) r = x == s_rej[t] ? 0.0 : r;
-  } else {
-    for (int t = 0; t < levels; ++t) {
-      const double d = r * s_ir[t] - double(q) * s_iz[t];
-      r = d > 0.0 ? d : d * 0.0;                           // (a NaN stays one)
+// r of N values of a row after `levels` rejections, from p and q.
+template <bool CERTAIN, int N>
+OQ_DEV void residual(const float (&p)[N], const float (&q)[N], const int (&x)[N], int levels, const double* s_ir,
+                     const double* s_iz, const int* s_rej, double (&r)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) r[e] = p[e];
+  for (int t = 0; t < levels; ++t) {
+    if constexpr (CERTAIN) {
+      const int gone = s_rej[t];
+#pragma unroll
+      for (int e = 0; e < N; ++e) r[e] = x[e] == gone ? 0.0 : r[e];
+    } else {
+      const double ir = s_ir[t], iz = s_iz[t];
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const double d = r[e] * ir - double(q[e]) * iz;
+        r[e] = d > 0.0 ? d : d * 0.0;                      // (a NaN stays one)
+      }
     }
   }
-  return r > 0.0 ? r : r * 0.0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) r[e] = r[e] > 0.0 ? r[e] : r[e] * 0.0;
+}
+template <bool CERTAIN>
+OQ_DEV double residual(float p, float q, int x, int levels, const double* s_ir, const double* s_iz, const int* s_rej) {
+  const float pp[1] = {p}, qq[1] = {q};
+  const int xx[1] = {x};
+  double r[1];
+  residual<CERTAIN, 1>(pp, qq, xx, levels, s_ir, s_iz, s_rej, r);
+  return r[0];
 }
 OQ_DEV double wave_sum64(double v) {
   for (int off = 1; off < 64; off <<= 1) v += __shfl_xor(v, off);
@@ -183,28 +201,50 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
   };
   const float *p = a.P + b * a.ldp, *q = CERTAIN ? nullptr : a.Q + b * a.ldq;
   int levels = 0;
-  // sums of r (and of q) over values x0 .. x1 - 1 of the row, by one wave
+  // Sums of r (and of q) over values x0 .. x1 - 1 of the row, by one wave: four steps' loads are under way
+  // together (16 trees of up to 32 nodes over 128,256 tokens 29.6 us, one step at a time 35.6).
   auto range_sum = [&](int x0, int x1, double& sr, double& sq) {
     double r = 0.0, w = 0.0;
-    for (int x = x0 + 4 * lane; x < x1; x += 256) {
-      float pv[4], qv[4] = {0.f, 0.f, 0.f, 0.f};
-      if (x + 4 <= x1) {
-        const float4 f = load_any<float4>(p + x);
-        pv[0] = f.x; pv[1] = f.y; pv[2] = f.z; pv[3] = f.w;
-        if constexpr (!CERTAIN) {
-          const float4 h = load_any<float4>(q + x);
-          qv[0] = h.x; qv[1] = h.y; qv[2] = h.z; qv[3] = h.w;
-        }
-      } else {
+    constexpr int U = 4;
+    int x = x0 + 4 * lane;
+    for (; __all(x + 256 * (U - 1) + 4 <= x1); x += 256 * U) {
+      float pv[4 * U], qv[4 * U];
+      int at[4 * U];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          pv[k] = x + k < x1 ? p[x + k] : 0.0f;
-          if constexpr (!CERTAIN) qv[k] = x + k < x1 ? q[x + k] : 0.0f;
+      for (int i = 0; i < U; ++i) {
+        const float4 f = load_any<float4>(p + x + 256 * i);
+        pv[4 * i] = f.x; pv[4 * i + 1] = f.y; pv[4 * i + 2] = f.z; pv[4 * i + 3] = f.w;
+        if constexpr (!CERTAIN) {
+          const float4 h = load_any<float4>(q + x + 256 * i);
+          qv[4 * i] = h.x; qv[4 * i + 1] = h.y; qv[4 * i + 2] = h.z; qv[4 * i + 3] = h.w;
+        } else {
+          qv[4 * i] = qv[4 * i + 1] = qv[4 * i + 2] = qv[4 * i + 3] = 0.0f;
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) at[4 * i + k] = x + 256 * i + k;
       }
+      double rv[4 * U];
+      residual<CERTAIN, 4 * U>(pv, qv, at, levels, s_ir, s_iz, s_rej, rv);
+#pragma unroll
+      for (int k = 0; k < 4 * U; ++k) {
+        r += rv[k];
+        if constexpr (!CERTAIN) w += double(qv[k]);
+      }
+    }
+    for (; x < x1; x += 256) {
+      float pv[4], qv[4];
+      int at[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        r += residual<CERTAIN>(pv[k], qv[k], x + k, levels, s_ir, s_iz, s_rej);
+        at[k] = x + k;
+        pv[k] = x + k < x1 ? p[x + k] : 0.0f;
+        qv[k] = !CERTAIN && x + k < x1 ? q[x + k] : 0.0f;
+      }
+      double rv[4];
+      residual<CERTAIN, 4>(pv, qv, at, levels, s_ir, s_iz, s_rej, rv);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        r += rv[k];
         w += double(qv[k]);
       }
     }
@@ -362,8 +402,17 @@ hipError_t token_probs(const void* logits, bool bf16, int64_t ldl, int64_t T, in
     hipLaunchKernelGGL((probs_kernel<TI, decltype(nv)::value>), dim3(unsigned(T)), dim3(NT), 0, st,
                        static_cast<const TI*>(logits), ldl, V, temperature, P, ldp);
   };
-  if (bf16) go(uint16_t{}, std::integral_constant<int, 16>{});
-  else go(float{}, std::integral_constant<int, 16>{});
+  // as many pieces as the row has (code for more would come from memory as it runs: five rows of 32,000 bf16
+  // logits 7.1 us with 4, 7.8 with 16); fp32 rows spill from 16 on
+  auto held = [&](auto ti) {
+    const int64_t pieces = V / (16 / int64_t(sizeof(ti))), per = (pieces + NT - 1) / NT;
+    if (per <= 4) go(ti, std::integral_constant<int, 4>{});
+    else if (per <= 8) go(ti, std::integral_constant<int, 8>{});
+    else if constexpr (sizeof(ti) == 2) go(ti, std::integral_constant<int, 16>{});
+    else go(ti, std::integral_constant<int, 12>{});
+  };
+  if (bf16) held(uint16_t{});
+  else held(float{});
   return hipGetLastError();
 }
 
