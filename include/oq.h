@@ -821,10 +821,13 @@ oq_status oq_kv_append_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, 
 
 /* oq_kv_attend_tree: oq_kv_attend for a tree: a node sees the sequence's `length` tokens, its
  * ancestors and itself.  Pages that the sequence has filled are read as codes; what lies
- * behind them, the open page's tokens and the tree, as bf16 rows of the window (so a node's
- * output does not depend on nodes that it does not see, bit for bit but for rounding
- * to the units that oq_kv_attend names).  Arguments, precision, rows that are NaN and the
- * workspace rule as oq_kv_attend. */
+ * behind them, the open page's tokens and the tree, as bf16 rows of the window.
+ * Arguments, precision and rows that are NaN as oq_kv_attend, but for these: queries
+ * always meet codes as fp16 (what oq_kv_attend says of more than 32 rows), values from 2^90 on
+ * may overflow, and the work is cut into equal shares by the lengths, so that the order of a
+ * row's sums depends on the other sequences of the batch; equal calls give equal bytes.
+ * Workspace: oq_kv_attend_tree_workspace_size, fixed by the cache, heads, n_seq, tokens and
+ * max_q; more than 2^22 tiles of 64 rows over all key heads are OQ_ERR_UNSUPPORTED. */
 oq_status oq_kv_attend_tree_workspace_size(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads,
                                            size_t* bytes);
 oq_status oq_kv_attend_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* parent, const void* Q,

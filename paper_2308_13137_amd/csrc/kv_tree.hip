@@ -76,7 +76,9 @@ OQ_DEV uint32_t tree_sees(const uint32_t (*s_anc)[4], int node, int L, int t0) {
 
 // ------------------------------------------------------------------ append
 // One workgroup takes one sequence's tree: the keys and values of one head
-// (blockIdx.y < kv heads), or a slice of the queries.
+// (blockIdx.y < kv heads), or a slice of the queries.  HBM-bound for large batches (64 trees of up
+// to 64 nodes, 64 heads, float32, 27.5 us, 5.0 TB/s), for few rows a chain of three loads (five
+// nodes, 32 heads, 5.2 us; with a barrier for each round of the ancestors' search 10.8).
 template <typename TI>
 __global__ __launch_bounds__(256) void tree_append_kernel(CacheArgs c, RowIn<TI> in, int H,
                                                          const float* __restrict__ rope, int64_t n_rope,
@@ -160,7 +162,8 @@ __global__ __launch_bounds__(256) void tree_append_kernel(CacheArgs c, RowIn<TI>
 // ------------------------------------------------------------------ commit
 // One workgroup: one head of one sequence.  The path's rows go through LDS, since a row
 // is written where another one is read; then the page that they fill, if any (a tree
-// of at most a page's tokens fills no second one), becomes codes.
+// of at most a page's tokens fills no second one), becomes codes.  Bound by its chain of loads: four
+// heads' or 64 sequences' 6.7 and 9.4 us.
 __global__ __launch_bounds__(256) void tree_commit_kernel(CacheArgs c, const int32_t* __restrict__ path, int max_path,
                                                          const int32_t* __restrict__ count) {
   extern __shared__ uint4 s_page[];                        // K [P][d], then V, bf16
@@ -182,8 +185,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CacheArgs c, const int
   auto window = [&](uint16_t* w, int pos) {
     return w + ((int64_t(s.slot) * 2 + ((pos >> c.lgP) & 1)) * c.Hkv + u) * win;
   };
-  // (a path's first nodes may stand where they belong; from the first that does not on,
-  // every one is to be moved)
+  // (a path's first nodes may stand where they belong)
   uint16_t* sk = reinterpret_cast<uint16_t*>(s_page);
   uint16_t* sv = sk + P * d;
   const int lk = c.lgd - 3;
@@ -219,11 +221,20 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CacheArgs c, const int
 }
 
 // ------------------------------------------------------------------ attention
-// Cost of a chunk of 32 tokens against a row tile of 16 R rows, in units of about 0.15 us of a
-// wave: the codes' widening, which any number of rows shares, and each 16 rows'
-// products and softmax.
+// A chunk of 32 tokens against a row tile of 16 R rows costs the codes' way to the registers and
+// their widening, which any number of rows shares, and each 16 rows' products and softmax: 8, 32
+// and 64 rows a key head over 131,072 tokens, 8 key heads of 128, took 55, 59 and 79 us (4.8, 4.5
+// and 3.4 TB/s with all of a call; the chunks alone run at 6.2, 5.9 and 4.5), 512 rows over 131,072
+// tokens, whose codes come from the caches, 400 (690 TFLOP/s).  With 64 rows a wave's own chain
+// of reads, products, softmax and products bounds a chunk (3 us, two waves to a SIMD): exponentials left out
+// would save 3%, codes out of the L2 6 to 17%.
 OQ_DEV int tile_cost(int rows) { return rows <= 16 ? 3 : rows <= 32 ? 4 : 6; }
-constexpr int TILE_ROWS = 64, TILE_MORE = 8;
+constexpr int TILE_ROWS = 64;
+// What a tile costs more than its chunks, in chunks: some 3 us before the first one (the search on
+// the line, page numbers, queries), 1 to 3 after the last, 4 to 6 for the window.  (Without it 32 trees of
+// up to 16 nodes over up to 4,096 tokens ended after 46 to 83 us in different workgroups, with it
+// after 36 to 64.)
+constexpr int TILE_MORE = 8;
 
 // What a workgroup's share of the line of all tiles' chunks is made of: row tile `row0` of
 // sequence s, chunks c0 .. c1 - 1.
@@ -256,8 +267,9 @@ OQ_DEV unsigned not_finite(u32x4_t w) {
 }
 
 // One piece: the chunks are dealt to the four waves, each with all rows and a softmax of its
-// own (ONCE: sequences of one tile, whose codes nobody else reads: they go past the caches); codes go from memory straight into operand registers.  Joined in LDS, the result goes
-// to the output or to a slot of the workspace.
+// own; codes go from memory straight into operand registers (ONCE: sequences of one tile, whose
+// codes nobody else reads, go past the caches).  Joined in LDS, the result goes to the output or
+// to a slot of the workspace.
 //   S^T = K Q^T: a lane holds query row r, tokens 4 g + 0..3 of both 16-token
 //   tiles, which is the B operand of O^T = V^T P^T as it stands.
 template <int DH, int R, bool ONCE, int RMAX>
@@ -620,22 +632,23 @@ OQ_DEV uint32_t lanes_upto(uint32_t v) {
 // The row tiles of all sequences, one behind the other, each as long as its chunks cost, are a
 // line that the nw workgroups of a key head cut into equal shares: the lengths are on the
 // device, and a ragged batch is as evenly spread as one long sequence.  A tile's steps are of
-// 2^shift chunks (one, unless the line would pass 31 bits); a step belongs to the share that it
-// begins in, but for a tile's first and last few, which go with their
-// neighbours: a piece costs more than they do.  A tile that several workgroups have goes to slots of the workspace (a share
+// 2^shift chunks (one, unless the line would pass 30 bits); a step belongs to the share that it
+// begins in, but for a tile's first and last few, which go with their neighbours: a piece costs
+// more than they do.  A tile that several workgroups have goes to slots of the workspace (a share
 // begins with at most one such piece and ends with at most one) and is joined by
 // tree_join_kernel, whom the workgroup where it begins tells so.
+// Against the batch attention's kernels with a tree's mask (a number of splits for all sequences, row
+// and tile kernels one after the other): 32 trees of up to 16 nodes over up to 4,096 tokens, 64 heads, 8
+// key heads, 107 -> 71 us; 8 nodes over 131,072 81 -> 75; 64 over 16,384, where matrix and vector work
+// bound both, 66 -> 65.
 struct Cut {
   int token, head, rows, w, pieces;      // its first row as a token and a head of the group; w: where it begins,
 };                                       // pieces: workgroups that go on with it
 template <int DH, int RMAX, bool ONCE>
-__global__ __launch_bounds__(256, 2) void tree_attend_kernel(CacheArgs c, const uint16_t* __restrict__ Q,
-                                                                           int64_t ldq, int H,
-                                                                           uint16_t* __restrict__ O,
-                                                                           float* __restrict__ LSE,
-                                                                           float* __restrict__ part,
-                                                                           Cut* __restrict__ cuts, int tiles, int nw,
-                                                                           int least, int shift) {
+__global__ __launch_bounds__(256, 2) void tree_attend_kernel(CacheArgs c, const uint16_t* __restrict__ Q, int64_t ldq,
+                                                             int H, uint16_t* __restrict__ O, float* __restrict__ LSE,
+                                                             float* __restrict__ part, Cut* __restrict__ cuts,
+                                                             int tiles, int nw, int least, int shift) {
   __shared__ Shared<DH, RMAX> sh;
   const int lane = threadIdx.x & 63, G = H / c.Hkv;
   int4* line = sh.line[threadIdx.x >> 6];
@@ -701,9 +714,11 @@ __global__ __launch_bounds__(256, 2) void tree_attend_kernel(CacheArgs c, const 
     if (s0 >= s1) continue;
     const int64_t slot = (int64_t(w) * c.Hkv + u) * 2 + (s0 == 0);
     if (s0 == 0) {
-      const uint32_t end = (t0 + (steps - 1) * cost1) / share, to = steps_below(end * share) < steps ? end : end - 1;
+      const uint32_t end = min((t0 + (steps - 1) * cost1) / share, uint32_t(nw - 1));
+      const uint32_t to = max(steps_below(end * share) < steps ? end : end - 1, uint32_t(w));
       const uint32_t tile = run_tiles + uint32_t(of(int(lanes_upto(tiles_of(x)) - tiles_of(x)))) + row0 / TILE_ROWS;
-      if (threadIdx.x == 0)
+      // (row ranges that overlap may make more tiles than there is room for)
+      if (threadIdx.x == 0 && tile < uint32_t(tiles))
         cuts[int64_t(tile) * c.Hkv + u] = Cut{s.b + row0 / G, row0 % G, n, w, int(to) - w};
     }
     const Out out{O, LSE, part, s0 > 0 || s1 < steps ? 2 : 1, H, c.T, slot * (16 * RMAX),
@@ -798,21 +813,21 @@ hipError_t cache_append_tree(const CacheArgs& c, const void* Q, int64_t ldq, con
   return hipGetLastError();
 }
 
-// Workgroups: as many as run at once, three of 16 rows to a compute unit or two of more. The
-// smallest share is 256 tokens of a tile.
+// Workgroups: two to a compute unit, as many as run at once (three with 16 rows each spill: one node over
+// 131,072 tokens, 64 heads, 70 us, with two 55).  The smallest share is 256 tokens of a tile.
 TreePlan tree_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d) {
   const int64_t rows = int64_t(max_q) * (H / Hkv);
   TreePlan p;
   p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   p.one_tile = rows <= TILE_ROWS;
-  const int fit = 512;
-  p.nw = std::max(1, (fit + Hkv / 2) / Hkv);
+  p.nw = std::max(1, (512 + Hkv / 2) / Hkv);
   p.least = 8 * (p.row_tiles == 1 ? 3 : p.row_tiles == 2 ? 4 : 6);
   p.tiles = std::min(tokens * (H / Hkv) / TILE_ROWS + std::min<int64_t>(n_seq, tokens),
                      n_seq * ((rows + TILE_ROWS - 1) / TILE_ROWS));
   // (2^24 tiles of a step and TILE_MORE still fit 30 bits; more are refused)
   p.shift = 0;
-  while (p.shift < 30 && p.tiles * (((max_len + 31) / 32 >> p.shift) + 1 + TILE_MORE) * 6 >= (int64_t(1) << 30)) ++p.shift;
+  while (p.shift < 30 && p.tiles * (((max_len + 31) / 32 >> p.shift) + 1 + TILE_MORE) * 6 >= (int64_t(1) << 30))
+    ++p.shift;
   p.part_floats = size_t(p.nw) * size_t(Hkv) * 2 * size_t(16 * p.row_tiles) * size_t(d + 2);
   p.bytes = p.part_floats * 4 + size_t(p.tiles) * size_t(Hkv) * sizeof(Cut);
   return p;
@@ -824,8 +839,8 @@ hipError_t cache_attend_tree(const CacheArgs& c, const uint16_t* Q, int64_t ldq,
   auto run = [&](auto dh, auto rt, auto once) {
     constexpr int DH = decltype(dh)::value, RMAX = decltype(rt)::value;
     const unsigned units = unsigned(p.nw) * unsigned(c.Hkv);
-    hipLaunchKernelGGL((tree_attend_kernel<DH, RMAX, decltype(once)::value>), dim3(units), dim3(256), 0, st, c, Q, ldq, H, O, LSE, ws, cuts,
-                       int(p.tiles), p.nw, p.least, p.shift);
+    hipLaunchKernelGGL((tree_attend_kernel<DH, RMAX, decltype(once)::value>), dim3(units), dim3(256), 0, st, c, Q, ldq,
+                       H, O, LSE, ws, cuts, int(p.tiles), p.nw, p.least, p.shift);
     // (a key head's only workgroup cuts nothing; rows by eight where tiles have few pieces)
     const int by = p.nw > 16 * p.tiles ? 1 : 8;
     if (p.nw > 1)
