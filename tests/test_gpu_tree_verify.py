@@ -300,6 +300,10 @@ def test_verify_rows_that_are_none():
         for i in (0, 7):
             for a, b in zip(got, want):
                 assert torch.equal(a[i], b[i])
+    # a draw from the target's own row does not look at the draft's
+    q = torch.full_like(Q, float("nan"))
+    leaf = oq.tree_verify(token[:1].cuda(), i32([-1]), i32([0, 1]), 1, P[:1].cuda(), u[:1].cuda(), un[:1].cuda(), Q=q[:1].cuda())
+    assert leaf[2].item() == tree_ref.verify64([0], [-1], P[:1], None, [0], un[0], True)[1]
     # trees without nodes; parents that hang on the sequence are never kept
     empty = oq.tree_verify(token.cuda(), i32(sum(trees, [])), i32([0, 0, 8]), 8, P.cuda(), u.cuda(), un[:2].cuda())
     assert empty[1][0] == 0 and empty[2][0] == -1 and (empty[0][0] == -1).all() and empty[1][1] >= 1
