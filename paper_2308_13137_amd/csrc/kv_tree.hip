@@ -231,10 +231,10 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CacheArgs c, const int
 OQ_DEV int tile_cost(int rows) { return rows <= 16 ? 3 : rows <= 32 ? 4 : 6; }
 constexpr int TILE_ROWS = 64;
 // What a tile costs more than its chunks, in chunks: some 3 us before the first one (the search on
-// the line, page numbers, queries), 1 to 3 after the last, 4 to 6 for the window.  (Without it 32 trees of
-// up to 16 nodes over up to 4,096 tokens ended after 46 to 83 us in different workgroups, with it
-// after 36 to 64.)
-constexpr int TILE_MORE = 8;
+// the line, page numbers, queries), 1 to 3 after the last, 4 to 6 for the window.  In a graph 32 trees of
+// up to 16 and of up to 8 nodes over up to 4,096 tokens, 64 heads, 8 key heads, took 75 and 59 us with 8, 69
+// and 54 with 16, 76 and 53 with 24, 79 and 57 with 32; without it workgroups ended after 46 to 83 us.
+constexpr int TILE_MORE = 16;
 
 // What a workgroup's share of the line of all tiles' chunks is made of: row tile `row0` of
 // sequence s, chunks c0 .. c1 - 1.
