@@ -827,7 +827,8 @@ oq_status oq_kv_append_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, 
  * may overflow, and the work is cut into equal shares by the lengths, so that the order of a
  * row's sums depends on the other sequences of the batch; equal calls give equal bytes.
  * Workspace: oq_kv_attend_tree_workspace_size, fixed by the cache, heads, n_seq, tokens and
- * max_q; more than 2^22 tiles of 64 rows over all key heads are OQ_ERR_UNSUPPORTED. */
+ * max_q; more than 2^22 tiles of 64 rows over all key heads, or 2^23 of one key head with every
+ * tree at max_q nodes, are OQ_ERR_UNSUPPORTED. */
 oq_status oq_kv_attend_tree_workspace_size(const oq_kv_cache* cache, const oq_kv_batch* batch, int heads,
                                            size_t* bytes);
 oq_status oq_kv_attend_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, const int32_t* parent, const void* Q,
@@ -880,7 +881,8 @@ oq_status oq_token_probs(const void* logits, oq_dtype dt, int64_t ld, int64_t n_
  * with r(x) > 0, should rounding leave none).  In fp64; rows are taken to sum to one.
  * `next` is -1 where r has no mass or is not finite.  A sequence without nodes, or that
  * does not fit (its rows, a parent), has count 0 and next -1.  Trees of at most 128 nodes, vocab at most 2^20
- * (else OQ_ERR_UNSUPPORTED); pointers 4-byte aligned. */
+ * (else OQ_ERR_UNSUPPORTED); pointers 4-byte aligned; outputs overlap neither inputs nor each
+ * other. */
 oq_status oq_tree_verify(int n_seq, int max_q, int64_t tokens, const int32_t* q_start, const int32_t* parent,
                          const int32_t* token, const float* P, int64_t ld_p, const float* Q, int64_t ld_q,
                          int64_t vocab, int replace, const float* u, const float* u_next, int32_t* path, int max_path,

@@ -2533,9 +2533,9 @@ oq_status oq_kv_attend_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, 
   OQ_TRY(check_queries(cache, batch, Q, ld_q, heads, O, LSE, ws));
   if (batch->n_seq == 0 || batch->max_q == 0) return OQ_OK;
   const TreePlan plan = tree_plan(cache, batch, heads);
-  if (plan.tiles * cache->kv_heads > (1 << 22))
-    return fail(OQ_ERR_UNSUPPORTED, "%lld row tiles of %d key heads: too many for one call", (long long)plan.tiles,
-                cache->kv_heads);
+  if (plan.tiles * cache->kv_heads > (1 << 22) || plan.all_tiles > (1 << 23))
+    return fail(OQ_ERR_UNSUPPORTED, "%d trees of up to %d nodes, %d heads on %d key heads: too many for one call",
+                batch->n_seq, batch->max_q, heads, cache->kv_heads);
   if (!ws || ws_bytes < plan.bytes)
     return fail(OQ_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws ? ws_bytes : size_t(0), plan.bytes);
   ProfScope ps(PK_CACHE_ATTN, st, 4.0 * double(batch->tokens) * heads * cache->head_dim);
@@ -2601,6 +2601,23 @@ oq_status oq_tree_verify(int n_seq, int max_q, int64_t tokens, const int32_t* q_
                         static_cast<const void*>(path), static_cast<const void*>(count),
                         static_cast<const void*>(next)})
     OQ_REQ(aligned4(p), "pointers must be 4-byte aligned");
+  // an output over an input that other workgroups still read
+  struct Span {
+    const void* p;
+    __int128 bytes;
+  };
+  const __int128 row_p = (__int128(tokens - 1) * ld_p + vocab) * 4, row_q = (__int128(tokens - 1) * ld_q + vocab) * 4;
+  const Span in[] = {{q_start, __int128(n_seq + 1) * 4}, {parent, tokens * 4}, {token, tokens * 4}, {u, tokens * 4},
+                     {u_next, __int128(n_seq) * 4},      {P, row_p},           {Q, row_q}};
+  const Span res[] = {{path, __int128(n_seq) * max_path * 4}, {count, __int128(n_seq) * 4}, {next, __int128(n_seq) * 4}};
+  for (const Span& r : res)
+    for (const Span& x : in)
+      OQ_REQ(x.bytes <= 0 || r.bytes <= 0 || !rows_meet(x.p, 1, x.bytes, x.bytes, r.p, r.bytes),
+             "path, count and next must not overlap the inputs");
+  OQ_REQ(!rows_meet(path, 1, res[0].bytes + 1, res[0].bytes, count, res[1].bytes) &&
+             !rows_meet(path, 1, res[0].bytes + 1, res[0].bytes, next, res[2].bytes) &&
+             !rows_meet(count, 1, res[1].bytes, res[1].bytes, next, res[2].bytes),
+         "path, count and next must not overlap each other");
   ProfScope ps(PK_OTHER, st, double(n_seq) * vocab * (Q ? 8 : 4));
   const VerifyArgs a{q_start, parent, token,  P,    Q,    u,     u_next, path,    count,
                      next,    tokens, vocab, ld_p, ld_q, n_seq, max_q,  max_path, replace != 0};

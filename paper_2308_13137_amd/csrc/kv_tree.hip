@@ -822,11 +822,12 @@ TreePlan tree_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, 
   p.one_tile = rows <= TILE_ROWS;
   p.nw = std::max(1, (512 + Hkv / 2) / Hkv);
   p.least = 8 * (p.row_tiles == 1 ? 3 : p.row_tiles == 2 ? 4 : 6);
-  p.tiles = std::min(tokens * (H / Hkv) / TILE_ROWS + std::min<int64_t>(n_seq, tokens),
-                     n_seq * ((rows + TILE_ROWS - 1) / TILE_ROWS));
-  // (2^24 tiles of a step and TILE_MORE still fit 30 bits; more are refused)
+  p.all_tiles = n_seq * ((rows + TILE_ROWS - 1) / TILE_ROWS);
+  p.tiles = std::min(tokens * (H / Hkv) / TILE_ROWS + std::min<int64_t>(n_seq, tokens), p.all_tiles);
+  // (2^23 tiles of a step and TILE_MORE still fit 30 bits, more are refused; all_tiles, since row ranges that
+  // overlap may make more tiles than the tokens do, and the line must not wrap for them either)
   p.shift = 0;
-  while (p.shift < 30 && p.tiles * (((max_len + 31) / 32 >> p.shift) + 1 + TILE_MORE) * 6 >= (int64_t(1) << 30))
+  while (p.shift < 30 && p.all_tiles * (((max_len + 31) / 32 >> p.shift) + 1 + TILE_MORE) * 6 >= (int64_t(1) << 30))
     ++p.shift;
   p.part_floats = size_t(p.nw) * size_t(Hkv) * 2 * size_t(16 * p.row_tiles) * size_t(d + 2);
   p.bytes = p.part_floats * 4 + size_t(p.tiles) * size_t(Hkv) * sizeof(Cut);

@@ -81,6 +81,7 @@ struct TreePlan {
   int nw, least;   // workgroups of a key head, their smallest share
   int shift;       // chunks of a step, as a power of two
   int64_t tiles;   // row tiles of a key head, of all sequences, at most
+  int64_t all_tiles;   // .. if every sequence had max_q rows
   size_t part_floats, bytes;   // pieces' results; with where they are, the workspace
 };
 TreePlan tree_attend_plan(int n_seq, int Hkv, int H, int64_t tokens, int max_q, int64_t max_len, int d);

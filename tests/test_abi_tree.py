@@ -42,7 +42,7 @@ def probs(**kw):
 
 def verify(**kw):
     a = dict(n=2, max_q=3, T=5, qs=FAKE, parent=FAKE, token=FAKE, P=FAKE, ldp=100, Q=None, ldq=0, V=100, replace=1,
-             u=FAKE, un=FAKE, path=FAKE, max_path=3, count=FAKE, next=FAKE, st=None)
+             u=FAKE, un=FAKE, path=FAR, max_path=3, count=FAR + 64, next=FAR + 128, st=None)
     a.update(kw)
     return oq.lib().oq_tree_verify(*a.values())
 
@@ -82,6 +82,12 @@ def test_append_and_attend_reject():
     assert L.oq_kv_attend_tree_workspace_size(C.byref(cache()), C.byref(b), 4, None) == INVALID
 
 
+def test_too_many_tiles():
+    for b, heads in ((batch(n_seq=65535, max_q=64, tokens=2 ** 22, max_pages=8), 2 ** 17),
+                     (batch(n_seq=65535, max_q=64, tokens=65535 * 64, max_pages=8), 256)):
+        assert attend(None, b, heads=heads, lq=heads * 128) == UNSUPPORTED
+
+
 def test_commit_rejects():
     for kw in (dict(path=None), dict(path=HALF), dict(count=None), dict(count=HALF), dict(max_path=-1)):
         assert commit(**kw) == INVALID, kw
@@ -104,6 +110,12 @@ def test_verify_rejects():
                *(dict(**{k: HALF}) for k in ("qs", "parent", "token", "P", "Q", "u", "un", "path", "count", "next")
                  if k != "Q"), dict(Q=HALF, ldq=100)):
         assert verify(**kw) == INVALID, kw
+    # outputs over inputs, or over each other: the last byte of P (5 rows of 100), the first of u, inside path
+    far = dict(qs=FAKE, parent=FAKE + 4096, token=FAKE + 8192, u=FAKE + 12288, un=FAKE + 16384, P=FAKE + (1 << 20))
+    for kw in (dict(path=FAKE + 8), dict(count=FAKE + 4096 + 16), dict(next=FAKE + 8192 - 4), dict(path=FAKE + 12288 - 20),
+               dict(count=FAKE + 16384 + 4), dict(next=FAKE + (1 << 20) + 1996), dict(Q=FAR + (1 << 20), ldq=100, path=FAR + (1 << 20)),
+               dict(count=FAR + 20), dict(next=FAR + 68), dict(path=FAR + 128)):
+        assert verify(**{**far, **kw}) == INVALID, kw
     assert verify(max_q=129, T=500, max_path=129) == UNSUPPORTED
     assert verify(V=2 ** 20 + 1, ldp=2 ** 21) == UNSUPPORTED
     assert verify(n=0, qs=None, path=None, count=None, next=None, u=None, un=None, P=None) == OK
