@@ -2575,6 +2575,8 @@ oq_status oq_token_probs(const void* logits, oq_dtype dt, int64_t ld, int64_t n_
   OQ_REQ(!rows_meet(logits, n_rows, __int128(ld) * esize(dt), __int128(vocab) * esize(dt), P,
                     (__int128(n_rows - 1) * ld_p + vocab) * 4),
          "P must not overlap the logits");
+  OQ_REQ(!temperature || !rows_meet(P, n_rows, __int128(ld_p) * 4, __int128(vocab) * 4, temperature, __int128(n_rows) * 4),
+         "P must not overlap temperature");
   ProfScope ps(PK_OTHER, st, double(n_rows) * vocab * (esize(dt) + 4));
   OQ_HIP(token_probs(logits, dt == OQ_BF16, ld, n_rows, vocab, temperature, P, ld_p, st), "token_probs");
   return OQ_OK;

@@ -103,6 +103,14 @@ def test_probs_rejects():
     assert probs(T=0, X=None, P=None) == OK
 
 
+def test_probs_over_their_temperature():
+    """A row's workgroups each read its temperature: no row of P lies over one."""
+    for kw in (dict(temp=FAR), dict(temp=FAR + 1596), dict(temp=FAR - 12), dict(temp=FAR + 396, ldp=110),
+               dict(temp=FAR + 436, ldp=110), dict(temp=FAR, T=1)):
+        assert probs(**kw) == INVALID and b"temperature" in oq.lib().oq_last_error(), kw
+    assert probs(T=0, temp=FAR) == OK
+
+
 def test_verify_rejects():
     for kw in (dict(n=-1), dict(max_q=-1), dict(T=-1), dict(max_q=6, max_path=6), dict(max_path=2), dict(V=0), dict(ldp=99),
                dict(Q=FAKE, ldq=99), dict(qs=None), dict(parent=None), dict(token=None), dict(P=None), dict(u=None),
