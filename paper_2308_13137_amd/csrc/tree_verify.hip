@@ -2,6 +2,7 @@
 // of drafts that keeps the target's distribution.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -23,7 +24,10 @@ OQ_DEV T load_any(const void* p) {
 // ------------------------------------------------------------------ probabilities
 // P = softmax(logits / t) = 2^((x - max x) log2(e) / t) over their sum.  One workgroup
 // a row: up to NV 16-byte pieces a thread stay in registers between the maximum, the sum
-// and the output; what is beyond them is read again.
+// and the output; what is beyond them is read again.  Many rows are bound by HBM (512 of 128,256
+// bf16 logits: 87 us in the kernel, 4.5 TB/s; 108 us a call, and 116 with half the pieces held and
+// two workgroups on a compute unit).  With few rows gridDim.y workgroups read the same row, sum it
+// in the same order and write a part each (five rows of 128,256: 19 us a call with one, 15 with eight).
 template <typename TI, int NV>
 __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int64_t ldx, int64_t V,
                                                    const float* __restrict__ temperature, float* __restrict__ P,
@@ -36,6 +40,7 @@ __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int
   const TI* x = X + int64_t(blockIdx.x) * ldx;
   float* out = P + int64_t(blockIdx.x) * ldp;
   const int n = int(V / E), rest = int(V) - n * E;         // whole pieces, values behind them
+  const int y = blockIdx.y, S = gridDim.y;                 // steps of NT pieces that are y modulo S
   const float t = temperature ? temperature[blockIdx.x] : 1.0f;
   auto value = [&](raw_t w, int e) {
     if constexpr (E == 8) return __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
@@ -69,7 +74,7 @@ __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int
   for (int w = 0; w < NW; ++w) m = fmaxf(m, s_a[w]);
   // a row without a maximum, or without a temperature, is no distribution
   if (odd || m == -INFINITY || !(t >= 0.0f && t < INFINITY)) {
-    for (int64_t i = tid; i < V; i += NT) out[i] = NAN;
+    for (int64_t i = tid + NT * y; i < V; i += NT * S) out[i] = NAN;
     return;
   }
   if (t == 0.0f) {                                         // all of it on the first maximum
@@ -84,7 +89,7 @@ __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) first = min(first, s_i[w]);
-    for (int64_t i = tid; i < V; i += NT) out[i] = i == first ? 1.0f : 0.0f;
+    for (int64_t i = tid + NT * y; i < V; i += NT * S) out[i] = i == first ? 1.0f : 0.0f;
     return;
   }
   const float k = fminf(1.4426950408889634f / t, 3.0e38f);
@@ -103,12 +108,13 @@ __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int
   for (int w = 0; w < NW; ++w) sum += s_a[w];
   const float inv = 1.0f / sum;
   pieces([&](int i, raw_t w) {
-    float y[E];
+    if (i / NT % S != y) return;
+    float p[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) y[e] = weight(value(w, e)) * inv;
-    __builtin_memcpy(out + int64_t(i) * E, y, sizeof(y));
+    for (int e = 0; e < E; ++e) p[e] = weight(value(w, e)) * inv;
+    __builtin_memcpy(out + int64_t(i) * E, p, sizeof(p));
   });
-  if (tid < rest) out[int64_t(n) * E + tid] = weight(tail) * inv;
+  if (y == 0 && tid < rest) out[int64_t(n) * E + tid] = weight(tail) * inv;
 }
 
 // ------------------------------------------------------------------ verification
@@ -400,7 +406,12 @@ hipError_t token_probs(const void* logits, bool bf16, int64_t ldl, int64_t T, in
                        float* P, int64_t ldp, hipStream_t st) {
   auto go = [&](auto ti, auto nv) {
     using TI = decltype(ti);
-    hipLaunchKernelGGL((probs_kernel<TI, decltype(nv)::value>), dim3(unsigned(T)), dim3(NT), 0, st,
+    // parts of a row: one for each of its steps of NT pieces, as long as all workgroups have a compute unit
+    // and rows get four or more (us a call with parts | one: 64 rows of 128,256 21.2 | 24.1, but 100 rows of
+    // 128,256 in two parts 28.0 | 27.0)
+    const int64_t steps = V / (16 / int64_t(sizeof(ti))) / NT;
+    const int64_t parts = T > 64 ? 1 : std::max<int64_t>(1, std::min<int64_t>({8, 256 / T, steps}));
+    hipLaunchKernelGGL((probs_kernel<TI, decltype(nv)::value>), dim3(unsigned(T), unsigned(parts)), dim3(NT), 0, st,
                        static_cast<const TI*>(logits), ldl, V, temperature, P, ldp);
   };
   // as many pieces as the row has (code for more would come from memory as it runs: five rows of 32,000 bf16

@@ -45,6 +45,23 @@ def test_probs_at_temperature_zero(V, dt):
     assert torch.equal(got, torch.nn.functional.one_hot(first, V).float())
 
 
+@pytest.mark.parametrize("V", [8191, 8192, 16383, 16385, 70001, 128256, 200003])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_probs_of_few_rows_are_those_of_many(V, dt):
+    """Rows that several workgroups share have the bits of rows that one has, whatever their kind, and
+    nothing beside them is written."""
+    many = rand(V, 130, V, scale=3.0, dtype=dt)
+    many[1, V - 1], many[2, :], many[3, V // 2] = float("nan"), -float("inf"), 90.0
+    t = torch.ones(130, device="cuda")
+    t[3], t[4], t[5], t[6] = 0.0, 0.0, -1.0, 0.4
+    want = oq.token_probs(many, t)
+    for T in (1, 7, 33, 70):
+        out = torch.full((T + 1, V + 5), 7.0, device="cuda")
+        oq.token_probs(many[:T], t[:T], out=out[:T, 3:3 + V])
+        assert torch.equal(out[:T, 3:3 + V].view(torch.int32), want[:T].view(torch.int32)), T
+        assert (out[:T, :3] == 7).all() and (out[:T, 3 + V:] == 7).all() and (out[T] == 7).all()
+
+
 def test_probs_strides_and_rows_that_are_none():
     V = 1003
     wide = rand(1, 12, 2000, dtype=BF)
