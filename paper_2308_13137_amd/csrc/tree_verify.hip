@@ -25,8 +25,8 @@ OQ_DEV T load_any(const void* p) {
 // P = softmax(logits / t) = 2^((x - max x) log2(e) / t) over their sum.  One workgroup
 // a row: up to NV 16-byte pieces a thread stay in registers between the maximum, the sum
 // and the output; what is beyond them is read again.  Many rows are bound by HBM (512 of 128,256
-// bf16 logits: 87 us in the kernel, 4.5 TB/s; 108 us a call, and 116 with half the pieces held and
-// two workgroups on a compute unit).  With few rows gridDim.y workgroups read the same row, sum it
+// bf16 logits: 86 us at best, 105 at the median of six launches, 3.8 TB/s; 108 us a call, and 116
+// with half the pieces held and two workgroups on a compute unit).  With few rows gridDim.y workgroups read the same row, sum it
 // in the same order and write a part each (five rows of 128,256: 19 us a call with one, 15 with eight).
 template <typename TI, int NV>
 __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int64_t ldx, int64_t V,

@@ -1055,7 +1055,10 @@ class KVCache:
     :meth:`attend`, both with ``length`` as before the step, and then adds the new
     tokens to ``length``.  All index tensors are int32 on the GPU and are read
     when the kernels run.  The newest tokens are dropped by lowering ``length``, at
-    most back to the start of the page before the furthest one begun."""
+    most back to the start of the page before the furthest one begun.
+
+    Drafted tokens take :meth:`append_tree` and :meth:`attend_tree`, which leave ``length``
+    and the pages alone, then :func:`tree_verify` and :meth:`commit` of what it kept."""
 
     def __init__(self, n_pages, page, kv_heads, head_dim, n_slots, device="cuda"):
         blk = page * head_dim
