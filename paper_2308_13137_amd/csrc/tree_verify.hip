@@ -213,8 +213,8 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
   };
   const float *p = a.P + b * a.ldp, *q = CERTAIN ? nullptr : a.Q + b * a.ldq;
   int levels = 0;
-  // Sums of r (and of q) over values x0 .. x1 - 1 of the row, by one wave: four steps' loads are under way
-  // together (16 trees of up to 32 nodes over 128,256 tokens 29.6 us, one step at a time 35.6).
+  // Sums of r (and of q without the rejected tokens) over values x0 .. x1 - 1 of the row, by one wave: four steps' loads are
+  // under way together (16 trees of up to 32 nodes over 128,256 tokens 29.6 us, one step at a time 35.6).
   auto range_sum = [&](int x0, int x1, bool of_q, double& sr, double& sq) {
     double r = 0.0, w = 0.0;
     float finite = 0.0f;                                   // NaN once a value is not
@@ -231,8 +231,18 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
         finite = __builtin_fmaf(pv[k], 0.0f, __builtin_fmaf(qv[k], 0.0f, finite));
       }
       if (!CERTAIN && of_q) {
+        // (what is left is summed itself: a sum of all of q, less what has left it, would hold nothing of it
+        // where one token had all but 2^-53 of the mass)
+        float left[4] = {qv[0], qv[1], qv[2], qv[3]};
+        for (int t = 0; t < levels; ++t) {
+          const int gone = s_rej[t] - at;
+          if (unsigned(gone) < 4u) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w += double(qv[k]);
+            for (int k = 0; k < 4; ++k) left[k] = k == gone ? 0.0f : left[k];
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w += double(left[k]);
       }
     };
     for (; __all(x + 256 * (U - 1) + 4 <= x1); x += 256 * U) {
@@ -277,7 +287,7 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
     }
   };
   int cur = 0, count = 1;
-  double R = 1.0, Z = 1.0, gone = 0.0;                     // gone: what has left q
+  double R = 1.0, Z = 1.0;
   if (tid == 0) s_path[0] = 0;
   for (int j = child_after(0, 0); j < n;) {
     const int x = s_tok[j];
@@ -298,7 +308,6 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
       if constexpr (!CERTAIN) q = a.Q + (b + j) * a.ldq;
       levels = 0;
       R = Z = 1.0;
-      gone = 0.0;
       j = child_after(j, j);
       continue;
     }
@@ -314,13 +323,12 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
     if constexpr (CERTAIN) {
       R -= r;
     } else {
-      if (!again) gone += double(qx);
       if (j < n) {
         double sr, sq;
         row_sums(!a.replace, sr, sq);
         if (sr == 0.0) break;                              // nothing is left: the draw steps back
         R = sr;
-        if (!a.replace) Z = sq - gone;
+        if (!a.replace) Z = sq;
       }
     }
   }

@@ -1,0 +1,52 @@
+"""Edges of the operators for drafted tokens, against plain 64-bit references."""
+import pytest
+import torch
+
+from tests.test_gpu_tree import star
+from tests.test_gpu_tree_verify import check_verify
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ verification
+@pytest.mark.parametrize("V", [300, 32000])
+@pytest.mark.parametrize("gap", [17.0, 36.0, 40.0, 45.0, 60.0, 80.0])
+@pytest.mark.parametrize("place", [1, 2, 4])
+def test_verify_siblings_of_a_peak(V, gap, place):
+    """Without replacement: all of q but 2^-24 to 2^-115 lies on one sibling's token.  Once that is rejected, what
+    q has left is the sum of the others, not what a sum of all of them leaves."""
+    n, g = 9, torch.Generator().manual_seed(int(gap) + V + place)
+    kept = 0
+    for seed in range(4):
+        x = torch.randn(n, V, generator=g)
+        y = x + 0.3 * torch.randn(n, V, generator=g)
+        y[:, 7] += gap + 8.0
+        P, Q = torch.softmax(x, 1), torch.softmax(y, 1)
+        rest = Q[0].clone()
+        rest[7] = 0.0
+        others = torch.multinomial(rest / rest.max(), n - 2, generator=g).tolist()
+        P[:, others[:place - 1]] = 0.0                       # siblings before the peak are rejected
+        token = torch.tensor([0] + others[:place - 1] + [7] + others[place - 1:], dtype=torch.int32)
+        u = torch.rand(n, generator=g) * (1.0, 0.5, 1.0, 0.1)[seed]
+        u[place] = 0.9                                       # the peak is rejected: the target's share is a 300th
+        kept += check_verify([star(n)], [0, n], token, P, Q, u, torch.rand(1, generator=g), replace=False) - 1
+    assert kept > 0
+
+
+@pytest.mark.parametrize("V", [5, 64, 1003])
+def test_verify_rejected_tokens_side_by_side(V):
+    """Long chains of rejections whose tokens are neighbours, and one of them twice."""
+    g = torch.Generator().manual_seed(V)
+    n = min(V, 40)
+    for first in (0, max(0, V - n)):
+        Q = torch.softmax(3 * torch.randn(n, V, generator=g), 1)
+        P = torch.softmax(3 * torch.randn(n, V, generator=g), 1)
+        token = torch.arange(first - 1, first - 1 + n, dtype=torch.int32)
+        P[:, first:first + 3 * n // 4] = 0.0                 # rejected whatever u
+        for seed in range(4):
+            u, un = 1.0 - torch.rand(n, generator=g) * (0.5, 1e-2, 1e-4, 1.0)[seed], torch.rand(1, generator=g)
+            u = u.clamp(max=1 - 2.0 ** -24)
+            check_verify([star(n)], [0, n], token, P, Q, u, un, replace=False)
+            twice = token.clone()
+            twice[n // 2:] = token[1:1 + n - n // 2]
+            check_verify([star(n)], [0, n], twice, P, Q, u, un, replace=False)
