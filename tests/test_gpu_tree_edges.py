@@ -2,10 +2,14 @@
 import pytest
 import torch
 
+from paper_2308_13137_amd import oq
+from tests import tree_ref
+from tests.test_gpu_serve import rand
 from tests.test_gpu_tree import star
 from tests.test_gpu_tree_verify import check_verify
 
 pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
 
 
 # ------------------------------------------------------------------ verification
@@ -50,3 +54,32 @@ def test_verify_rejected_tokens_side_by_side(V):
             twice = token.clone()
             twice[n // 2:] = token[1:1 + n - n // 2]
             check_verify([star(n)], [0, n], twice, P, Q, u, un, replace=False)
+
+
+# ------------------------------------------------------------------ probabilities
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("V", [4, 1003, 70001])
+def test_probs_of_differences_that_pass_fp32(V, dt):
+    """The type's ends at temperatures that bring them near each other again: (x - max) / t is finite though
+    x - max is not."""
+    big = torch.finfo(dt).max
+    x = rand(V, 7, V, dtype=dt) * 1e30
+    x[:, 1], x[:, 2], x[:, V - 1] = big, -big, -big / 2
+    x[6, 0] = -float("inf")
+    t = torch.tensor([1.0, 1.0000001, 1e30, 3e37, 1e38, torch.finfo(F32).max, 1e38], device="cuda")
+    want, tol = tree_ref.probs64(x, t)
+    got = oq.token_probs(x, t).cpu().double()
+    assert ((got - want).abs() <= tol).all() and got[6, 0] == 0
+    assert (got[4:6, 2] > 0).all()
+
+
+def test_probs_of_differences_below_fp32s_normal_numbers():
+    """Logits and temperatures that are tiny alike."""
+    step = 2.0 ** -149
+    x = torch.tensor([[0.0, -1.0, 3.0, 2.0, -700.0], [5.0, 5.0, -5.0, 4.0, 0.0], [8e6, 8e6 - 3, 8e6 - 1, 0.0, 8e6 - 2]],
+                     dtype=torch.float64)
+    x = torch.cat([(x * step).float(), x[:2].float() * 2.0 ** -100, x[:1].float() * 2.0 ** 100]).cuda()
+    assert (x[0] != 0).sum() == 4
+    t = torch.tensor([2 * step, 7 * step, step, 2.0 ** -100, 2.0 ** -101, step], device="cuda")
+    want, tol = tree_ref.probs64(x, t)
+    assert ((oq.token_probs(x, t).cpu().double() - want).abs() <= tol).all()
