@@ -840,7 +840,9 @@ oq_status oq_kv_attend_tree(const oq_kv_cache* cache, const oq_kv_batch* batch, 
  *   path  : int32 [n_seq, max_path] node numbers, ascending; entries from count[i] on are
  *           not read
  *   count : int32 [n_seq], 0 .. the tree's nodes
- * `batch` is the append's (length before the tree).  For a path from a root down (a node
+ * `batch` is the append's (length before the tree, tokens the rows of the append's tensors).
+ * Parents are not looked at again: of a tree whose parents do not fit `count` has to be 0, as
+ * oq_tree_verify leaves it.  For a path from a root down (a node
  * without a parent, then a child each) the cache is then, bit for bit, what oq_kv_append of
  * those tokens leaves, codes, steps and the window's rows up to length + count.  Of a
  * sequence that does not fit (as in oq_kv_batch; a count or a path that is not as above)

@@ -1185,17 +1185,22 @@ class KVCache:
             _check(L.oq_kv_attend_tree(cache, b, _arg(parent, "parent", _I32, (T,), dev), *rest))
         return (out, lse) if want_lse else out
 
-    def commit(self, path, count, table, length, q_start, max_q, slots=None, stream=None):
+    def commit(self, path, count, table, length, q_start, max_q, slots=None, stream=None, tokens=None):
         """Keeps part of the trees that :meth:`append_tree` left (oq_kv_commit): node path[i, k] of
         sequence i becomes its token length[i] + k, for k < count[i] (:func:`tree_verify`'s
-        outputs).  Pages that fill up become codes.  The caller then adds ``count`` to ``length``."""
+        outputs).  Pages that fill up become codes.  The caller then adds ``count`` to ``length``.
+
+        ``tokens``: T, the rows that the step's tensors have; nothing is kept of a sequence whose
+        rows leave them, as nothing of it was appended.  Without it ``count`` has to be 0 there
+        (:func:`tree_verify`'s is)."""
         dev = self.dev
         if stream is not None or dev != _cur_device():
             with _placed(dev, stream):
-                return self.commit(path, count, table, length, q_start, max_q, slots)
+                return self.commit(path, count, table, length, q_start, max_q, slots, None, tokens)
         n, m = path.shape
-        # (the batch's rows themselves are not touched: any count holds them)
-        b = KVBatch(n, table.shape[1], max_q, 0x7fff0000, _arg(table, "table", _I32, (n, table.shape[1]), dev),
+        # (the rows themselves are not touched: without their number any range of q_start fits)
+        T = 0x7fff0000 if tokens is None else tokens
+        b = KVBatch(n, table.shape[1], max_q, T, _arg(table, "table", _I32, (n, table.shape[1]), dev),
                     None if slots is None else _arg(slots, "slots", _I32, (n,), dev),
                     _arg(length, "length", _I32, (n,), dev), _arg(q_start, "q_start", _I32, (n + 1,), dev))
         _check(lib().oq_kv_commit(C.byref(self.desc), C.byref(b), _arg(path, "path", _I32, (n, m), dev), m,

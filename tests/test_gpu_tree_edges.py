@@ -4,8 +4,8 @@ import torch
 
 from paper_2308_13137_amd import oq
 from tests import tree_ref
-from tests.test_gpu_serve import rand
-from tests.test_gpu_tree import star
+from tests.test_gpu_serve import i32, rand
+from tests.test_gpu_tree import chain, star
 from tests.test_gpu_tree_verify import check_verify
 
 pytestmark = pytest.mark.gpu
@@ -83,3 +83,35 @@ def test_probs_of_differences_below_fp32s_normal_numbers():
     t = torch.tensor([2 * step, 7 * step, step, 2.0 ** -100, 2.0 ** -101, step], device="cuda")
     want, tol = tree_ref.probs64(x, t)
     assert ((oq.token_probs(x, t).cpu().double() - want).abs() <= tol).all()
+
+
+# ------------------------------------------------------------------ what is kept
+def split(r, H, Hkv, d):
+    return r[:, :H * d], r[:, H * d:(H + Hkv) * d], r[:, (H + Hkv) * d:]
+
+
+def test_commit_of_rows_behind_the_step():
+    """A sequence whose rows leave the step's tensors was not appended, and nothing of it is kept or moved, whatever
+    its count; the others' paths are."""
+    H, Hkv, d, P, n = 2, 1, 64, 32, 6
+    cache = oq.KVCache(6, P, Hkv, d, 3)
+    for w, v in ((cache.k_window, 3.0), (cache.v_window, 4.0)):
+        w.copy_(v + torch.randn(w.shape, generator=torch.Generator().manual_seed(1)))
+    x = rand(1, 2 * n + 3, (H + 2 * Hkv) * d, dtype=BF)      # three rows less than the third tree has
+    T = len(x)
+    table, length = i32([[0, 1], [2, 3], [4, 5]]), i32([29, 3, 29])
+    args = (table, length, i32([0, n, 2 * n, 3 * n]), n)
+    q = cache.append_tree(*split(x, H, Hkv, d), *args, i32(chain(n) + star(n) + [-1] * 3))
+    assert torch.isnan(q[2 * n:].float()).all() and torch.isfinite(q[:2 * n].float()).all()
+    before = [t.clone() for t in (cache.k_window, cache.v_window, cache.k_codes, cache.v_codes, cache.k_scale)]
+    path = i32([[0, 1, 2, 3, 4, 5], [0, 4, 9, 9, 9, 9], [0, 2, 3, 4, 5, 9]])
+    cache.commit(path, i32([6, 2, 5]), *args, tokens=T)
+    now = (cache.k_window, cache.v_window, cache.k_codes, cache.v_codes, cache.k_scale)
+    for a, b, of_pages in zip(now, before, (False, False, True, True, True)):
+        rest = slice(4, 6) if of_pages else slice(2, 3)
+        assert torch.equal(a[rest], b[rest])
+    assert cache.k_scale[0, 0] > 0 and not torch.equal(now[0][1], before[0][1])
+    k, v = cache.read(table, i32([29, 3, 0]), i32([35, 5, 0]), i32([0, 0, 0, 0]), i32([0, 6, 8, 8]), 8, 6)
+    kept = torch.cat([torch.arange(3, 6), torch.tensor([n, n + 4])])
+    want_k, want_v = (t[kept.cuda()] for t in split(x, H, Hkv, d)[1:])
+    assert torch.equal(k[3:], want_k) and torch.equal(v[3:], want_v)      # (the first three are in a page's codes)
