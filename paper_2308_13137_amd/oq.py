@@ -1190,9 +1190,10 @@ class KVCache:
         sequence i becomes its token length[i] + k, for k < count[i] (:func:`tree_verify`'s
         outputs).  Pages that fill up become codes.  The caller then adds ``count`` to ``length``.
 
-        ``tokens``: T, the rows that the step's tensors have; nothing is kept of a sequence whose
-        rows leave them, as nothing of it was appended.  Without it ``count`` has to be 0 there
-        (:func:`tree_verify`'s is)."""
+        ``tokens``: T, the rows that the step's tensors have.  ``max_q`` is a bound as in the
+        step's other calls, then, and nothing is kept of a sequence whose rows leave them, as
+        nothing of it was appended.  Without it ``max_q`` is at most ``page``, and ``count`` has
+        to be 0 there (:func:`tree_verify`'s is)."""
         dev = self.dev
         if stream is not None or dev != _cur_device():
             with _placed(dev, stream):
@@ -1200,7 +1201,7 @@ class KVCache:
         n, m = path.shape
         # (the rows themselves are not touched: without their number any range of q_start fits)
         T = 0x7fff0000 if tokens is None else tokens
-        b = KVBatch(n, table.shape[1], max_q, T, _arg(table, "table", _I32, (n, table.shape[1]), dev),
+        b = KVBatch(n, table.shape[1], min(max_q, T), T, _arg(table, "table", _I32, (n, table.shape[1]), dev),
                     None if slots is None else _arg(slots, "slots", _I32, (n,), dev),
                     _arg(length, "length", _I32, (n,), dev), _arg(q_start, "q_start", _I32, (n + 1,), dev))
         _check(lib().oq_kv_commit(C.byref(self.desc), C.byref(b), _arg(path, "path", _I32, (n, m), dev), m,

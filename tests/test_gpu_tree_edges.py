@@ -115,3 +115,29 @@ def test_commit_of_rows_behind_the_step():
     kept = torch.cat([torch.arange(3, 6), torch.tensor([n, n + 4])])
     want_k, want_v = (t[kept.cuda()] for t in split(x, H, Hkv, d)[1:])
     assert torch.equal(k[3:], want_k) and torch.equal(v[3:], want_v)      # (the first three are in a page's codes)
+
+
+def test_commit_with_a_bound_of_nodes_above_the_page():
+    """max_q is a bound: like the step's other calls, commit takes one that passes the page, where the step's rows do
+    not."""
+    H, Hkv, d, P, n = 2, 1, 64, 32, 5
+    x = rand(2, n, (H + 2 * Hkv) * d, dtype=BF)
+    got = []
+    for max_q in (n, 64):
+        c = oq.KVCache(2, P, Hkv, d, 1)
+        tree = [-1, 0, 0, 1, 1]
+        args, parent = (i32([[0, 1]]), i32([30]), i32([0, n]), max_q), i32(tree)
+        q = c.append_tree(*split(x, H, Hkv, d), *args, parent)
+        c.attend_tree(q, *args, parent)
+        P1 = torch.eye(8, device="cuda")[[2, 3, 1, 1, 5]].contiguous()
+        path, count, nxt = oq.tree_verify(i32([0, 2, 4, 6, 3]), parent, i32([0, n]), max_q, P1, torch.zeros(n, device="cuda"),
+                                          torch.zeros(1, device="cuda"))
+        assert path.shape == (1, max_q) and count.item() == 3 and nxt.item() == 5
+        c.commit(path, count, *args, tokens=n)
+        got.append((c.k_codes, c.v_codes, c.k_scale, c.k_window[0, 1, :, :d], c.v_window[0, 1]))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    with pytest.raises(oq.OQError):
+        c.commit(path, count, *args, tokens=33)
+    with pytest.raises(oq.OQError):
+        c.commit(path, count, *args, tokens=-1)
