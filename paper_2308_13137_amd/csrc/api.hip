@@ -2556,7 +2556,9 @@ oq_status oq_kv_commit(const oq_kv_cache* cache, const oq_kv_batch* batch, const
   OQ_REQ(max_path >= 0, "bad max_path=%d", max_path);
   if (batch->n_seq == 0 || batch->max_q == 0 || max_path == 0) return OQ_OK;
   OQ_REQ(path && count && aligned4(path) && aligned4(count), "path and count (4-byte aligned) are required");
-  ProfScope ps(PK_OTHER, st, 8.0 * double(batch->tokens) * cache->kv_heads * cache->head_dim);
+  // (a caller may not know how many rows there are, and allow for any)
+  const double rows = std::min(double(batch->tokens), double(batch->n_seq) * batch->max_q);
+  ProfScope ps(PK_OTHER, st, 8.0 * rows * cache->kv_heads * cache->head_dim);
   OQ_HIP(cache_commit(cache_args(cache, batch), path, max_path, count, st), "kv_commit");
   return OQ_OK;
 }

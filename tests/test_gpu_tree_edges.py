@@ -141,3 +141,18 @@ def test_commit_with_a_bound_of_nodes_above_the_page():
         c.commit(path, count, *args, tokens=33)
     with pytest.raises(oq.OQError):
         c.commit(path, count, *args, tokens=-1)
+
+
+def test_commits_in_the_profile():
+    """A commit counts its rows' bytes, not those of every row that a batch may have."""
+    c = oq.KVCache(4, 32, 2, 64, 2)
+    oq.profile_enable()
+    try:
+        for kw in ({}, dict(tokens=7)):
+            oq.profile_reset()
+            c.commit(i32([[0], [0]]), i32([0, 0]), i32([[0, 1], [2, 3]]), i32([0, 0]), i32([0, 5, 7]), 5, **kw)
+            work = sum(w for _, _, w in oq.profile_read().values())
+            assert 0 < work <= 8 * 2 * 5 * 2 * 64, kw
+    finally:
+        oq.profile_enable(False)
+        oq.profile_reset()
