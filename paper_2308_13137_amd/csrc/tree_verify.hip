@@ -430,6 +430,9 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
 
 }  // namespace
 
+// A launch's threads are below 2^32: as many workgroups of NT as one of them has.
+constexpr int64_t AT_ONCE = int64_t(1) << 21;
+
 hipError_t token_probs(const void* logits, bool bf16, int64_t ldl, int64_t T, int64_t V, const float* temperature,
                        float* P, int64_t ldp, hipStream_t st) {
   auto go = [&](auto ti, auto nv) {
@@ -439,8 +442,10 @@ hipError_t token_probs(const void* logits, bool bf16, int64_t ldl, int64_t T, in
     // 128,256 in two parts 28.0 | 27.0)
     const int64_t steps = V / (16 / int64_t(sizeof(ti))) / NT;
     const int64_t parts = T > 64 ? 1 : std::max<int64_t>(1, std::min<int64_t>({8, 256 / T, steps}));
-    hipLaunchKernelGGL((probs_kernel<TI, decltype(nv)::value>), dim3(unsigned(T), unsigned(parts)), dim3(NT), 0, st,
-                       static_cast<const TI*>(logits), ldl, V, temperature, P, ldp);
+    for (int64_t t = 0; t < T; t += AT_ONCE)
+      hipLaunchKernelGGL((probs_kernel<TI, decltype(nv)::value>), dim3(unsigned(std::min(T - t, AT_ONCE)), unsigned(parts)),
+                         dim3(NT), 0, st, static_cast<const TI*>(logits) + t * ldl, ldl, V,
+                         temperature ? temperature + t : nullptr, P + t * ldp, ldp);
   };
   // as many pieces as the row has (code for more would come from memory as it runs: five rows of 32,000 bf16
   // logits 7.1 us with 4, 7.8 with 16); fp32 rows spill from 16 on
@@ -457,8 +462,17 @@ hipError_t token_probs(const void* logits, bool bf16, int64_t ldl, int64_t T, in
 }
 
 hipError_t tree_verify(const VerifyArgs& a, hipStream_t st) {
-  if (a.Q) hipLaunchKernelGGL(verify_kernel<false>, dim3(unsigned(a.n_seq)), dim3(NT), 0, st, a);
-  else hipLaunchKernelGGL(verify_kernel<true>, dim3(unsigned(a.n_seq)), dim3(NT), 0, st, a);
+  for (int64_t i = 0; i < a.n_seq; i += AT_ONCE) {
+    VerifyArgs b = a;
+    b.q_start += i;
+    b.u_next += i;
+    b.path += i * a.max_path;
+    b.count += i;
+    b.next += i;
+    const dim3 grid(unsigned(std::min(a.n_seq - i, AT_ONCE)));
+    if (a.Q) hipLaunchKernelGGL(verify_kernel<false>, grid, dim3(NT), 0, st, b);
+    else hipLaunchKernelGGL(verify_kernel<true>, grid, dim3(NT), 0, st, b);
+  }
   return hipGetLastError();
 }
 

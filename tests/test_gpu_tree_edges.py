@@ -156,3 +156,25 @@ def test_commits_in_the_profile():
     finally:
         oq.profile_enable(False)
         oq.profile_reset()
+
+
+# ------------------------------------------------------------------ very many rows
+def test_probs_of_more_rows_than_a_launch_has_workgroups():
+    """2^22 workgroups of 1,024 threads are more than a launch can have."""
+    T, V = 2 ** 22 + 5, 3
+    x = rand(1, T, V, dtype=BF)
+    t = torch.ones(T, device="cuda")
+    t[-2:] = torch.tensor([0.0, 2.0])
+    got = oq.token_probs(x, t)
+    for rows in (slice(0, 70), slice(2 ** 21 - 40, 2 ** 21 + 40), slice(2 ** 22 - 40, T)):
+        assert torch.equal(got[rows], oq.token_probs(x[rows].clone(), t[rows].clone()))
+    assert ((got.sum(1) - 1).abs() < 1e-6).all()
+
+
+def test_verify_more_trees_than_a_launch_has_workgroups():
+    n, V = 2 ** 22 + 3, 2
+    P = torch.eye(V, device="cuda")[torch.arange(n, device="cuda") % V].contiguous()
+    start = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    zero = torch.zeros(n, device="cuda")
+    path, count, nxt = oq.tree_verify(torch.zeros_like(start[:n]), torch.full_like(start[:n], -1), start, 1, P, zero, zero)
+    assert (path == 0).all() and (count == 1).all() and torch.equal(nxt, start[:n] % V)
