@@ -852,7 +852,8 @@ oq_status oq_kv_commit(const oq_kv_cache* cache, const oq_kv_batch* batch, const
 
 /* oq_token_probs: P[t, :] = softmax(logits[t, :] / temperature[t]).
  *   logits [n_rows, vocab] (dt), rows ld apart; P fp32, rows ld_p apart, over neither logits nor
- *   temperature; both aligned to their elements only; vocab at most 2^20 (else OQ_ERR_UNSUPPORTED)
+ *   temperature (rows as many bytes apart as the logits' may lie beside them, others not between
+ *   them); both aligned to their elements only; vocab at most 2^20 (else OQ_ERR_UNSUPPORTED)
  *   temperature : fp32 [n_rows] | NULL (ones); 0 puts all of it on the first of the largest
  *   logits
  * A logit of -inf has probability 0.  A row with a NaN or +inf, one of -inf alone, and one whose

@@ -2210,6 +2210,17 @@ bool rows_meet(const void* rows, int64_t n, __int128 ld, __int128 width, const v
   return lo < r * ld + width || (r + 1 < n && hi > (r + 1) * ld);
 }
 
+// Whether two sets of n rows, of `wa` and `wb` bytes, share a byte: exact where their rows are as far apart, else
+// rows of `b` count as one piece from the first to the last.
+bool row_sets_meet(const void* a, __int128 lda, __int128 wa, const void* b, __int128 ldb, __int128 wb, int64_t n) {
+  if (lda != ldb) return rows_meet(a, n, lda, wa, b, (n - 1) * ldb + wb);
+  const __int128 by = __int128(reinterpret_cast<uintptr_t>(b)) - __int128(reinterpret_cast<uintptr_t>(a));
+  // row i of b lies `by` + k lda from row i - k of a
+  for (__int128 k = -(by / lda) - 1; k <= -(by / lda) + 1; ++k)
+    if (k > -n && k < n && by + k * lda < wa && by + k * lda > -wb) return true;
+  return false;
+}
+
 oq_status check_cache(const oq_kv_cache* c, const oq_kv_batch* b) {
   OQ_REQ(c && b, "cache and batch are required");
   if ((c->head_dim != 64 && c->head_dim != 128) || (c->page != 32 && c->page != 64 && c->page != 128))
@@ -2574,8 +2585,8 @@ oq_status oq_token_probs(const void* logits, oq_dtype dt, int64_t ld, int64_t n_
   OQ_REQ(logits && P, "logits and P are required");
   OQ_REQ((reinterpret_cast<uintptr_t>(logits) & (esize(dt) - 1)) == 0 && aligned4(temperature) && aligned4(P),
          "pointers must be aligned to their elements");
-  OQ_REQ(!rows_meet(logits, n_rows, __int128(ld) * esize(dt), __int128(vocab) * esize(dt), P,
-                    (__int128(n_rows - 1) * ld_p + vocab) * 4),
+  OQ_REQ(!row_sets_meet(logits, __int128(ld) * esize(dt), __int128(vocab) * esize(dt), P, __int128(ld_p) * 4,
+                        __int128(vocab) * 4, n_rows),
          "P must not overlap the logits");
   OQ_REQ(!temperature || !rows_meet(P, n_rows, __int128(ld_p) * 4, __int128(vocab) * 4, temperature, __int128(n_rows) * 4),
          "P must not overlap temperature");
@@ -2606,17 +2617,27 @@ oq_status oq_tree_verify(int n_seq, int max_q, int64_t tokens, const int32_t* q_
                         static_cast<const void*>(next)})
     OQ_REQ(aligned4(p), "pointers must be 4-byte aligned");
   // an output over an input that other workgroups still read
+  struct Rows {
+    const void* p;
+    int64_t n;
+    __int128 ld, bytes;
+  };
   struct Span {
     const void* p;
     __int128 bytes;
   };
-  const __int128 row_p = (__int128(tokens - 1) * ld_p + vocab) * 4, row_q = (__int128(tokens - 1) * ld_q + vocab) * 4;
-  const Span in[] = {{q_start, __int128(n_seq + 1) * 4}, {parent, tokens * 4}, {token, tokens * 4}, {u, tokens * 4},
-                     {u_next, __int128(n_seq) * 4},      {P, row_p},           {Q, row_q}};
+  auto flat = [](const void* p, __int128 values) { return Rows{p, 1, values * 4, values * 4}; };
+  const Rows in[] = {flat(q_start, __int128(n_seq) + 1),
+                     flat(parent, tokens),
+                     flat(token, tokens),
+                     flat(u, tokens),
+                     flat(u_next, n_seq),
+                     {P, tokens, __int128(ld_p) * 4, __int128(vocab) * 4},
+                     {Q, tokens, __int128(ld_q) * 4, __int128(vocab) * 4}};
   const Span res[] = {{path, __int128(n_seq) * max_path * 4}, {count, __int128(n_seq) * 4}, {next, __int128(n_seq) * 4}};
   for (const Span& r : res)
-    for (const Span& x : in)
-      OQ_REQ(x.bytes <= 0 || r.bytes <= 0 || !rows_meet(x.p, 1, x.bytes, x.bytes, r.p, r.bytes),
+    for (const Rows& x : in)
+      OQ_REQ(x.n == 0 || x.bytes == 0 || r.bytes == 0 || !rows_meet(x.p, x.n, x.ld, x.bytes, r.p, r.bytes),
              "path, count and next must not overlap the inputs");
   OQ_REQ(!rows_meet(path, 1, res[0].bytes + 1, res[0].bytes, count, res[1].bytes) &&
              !rows_meet(path, 1, res[0].bytes + 1, res[0].bytes, next, res[2].bytes) &&

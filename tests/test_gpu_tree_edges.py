@@ -178,3 +178,48 @@ def test_verify_more_trees_than_a_launch_has_workgroups():
     zero = torch.zeros(n, device="cuda")
     path, count, nxt = oq.tree_verify(torch.zeros_like(start[:n]), torch.full_like(start[:n], -1), start, 1, P, zero, zero)
     assert (path == 0).all() and (count == 1).all() and torch.equal(nxt, start[:n] % V)
+
+
+# ------------------------------------------------------------------ rows side by side
+def test_probs_beside_their_logits():
+    """Probabilities in the columns behind (or before) the logits: they share rows, but no value."""
+    T, V = 70, 129
+    wide = torch.full((T, 2 * V + 3), 7.0, device="cuda")
+    x = rand(1, T, V)
+    want = oq.token_probs(x)
+    for a, b in ((0, V), (V + 3, 0), (0, V + 3), (V, 0)):
+        wide.fill_(7.0)
+        wide[:, a:a + V] = x
+        oq.token_probs(wide[:, a:a + V], out=wide[:, b:b + V])
+        assert torch.equal(wide[:, b:b + V], want) and torch.equal(wide[:, a:a + V], x) and (wide == 7).sum() == 3 * T
+    for b in (V - 1, 1, 0):
+        with pytest.raises(oq.OQError, match="overlap"):
+            oq.token_probs(wide[:, :V], out=wide[:, b:b + V])
+
+
+def test_verify_outputs_beside_the_rows():
+    """An output in the columns behind P's."""
+    n, V, m = 3, 50, 2
+    parent, start = i32([-1, 0] * n), i32([0, 2, 4, 6])
+    wide = torch.full((2 * n, V + 4), 7.0, device="cuda")
+    wide[:, :V] = torch.softmax(rand(1, 2 * n, V), 1)
+    token, u, un = i32([0, 3] * n), torch.full((2 * n,), 0.1, device="cuda"), torch.full((n,), 0.5, device="cuda")
+    path, count, nxt = oq.tree_verify(token, parent, start, m, wide[:, :V], u, un)
+    rest = torch.zeros(3 * n, dtype=torch.int32, device="cuda")
+    keep = wide.clone()
+
+    def call(at):                                            # count: three values from column `at` of the first row
+        wide.copy_(keep)
+        torch.cuda.synchronize()
+        r = oq.lib().oq_tree_verify(n, m, 2 * n, start.data_ptr(), parent.data_ptr(), token.data_ptr(), wide.data_ptr(),
+                                    V + 4, None, 0, V, 1, u.data_ptr(), un.data_ptr(), rest.data_ptr(), m,
+                                    wide.data_ptr() + 4 * at, rest[2 * n:].data_ptr(), None)
+        torch.cuda.synchronize()
+        return r
+
+    for at in (V, V + 1, V + 4 + V):
+        assert call(at) == 0
+        assert torch.equal(rest[:2 * n].view(n, m), path) and torch.equal(rest[2 * n:], nxt)
+        assert torch.equal(wide.view(-1)[at:at + n].view(torch.int32), count) and torch.equal(wide[:, :V], keep[:, :V])
+    for at in (V - 1, V - n, V + 2, 0):
+        assert call(at) != 0
