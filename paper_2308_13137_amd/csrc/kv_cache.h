@@ -45,38 +45,6 @@ OQ_DEV Seq seq_of(const CacheArgs& c, int i) {
   if (int64_t(s.L) + s.n > int64_t(c.max_pages) * c.P) s.ok = false;
   return s;
 }
-// Ragged batches: unit w of all sequences' units (pages, row tiles), in the order of
-// the sequences, as (sequence, its unit); (-1, 0) past the last.  By every wave for
-// itself.  Batches whose grid of n_seq times the longest sequence's units is no
-// larger than the units' bound, or small, are numbered directly instead (a search
-// costs some 4 us: 15 chunks of up to 152 tokens 26 us, searched 30).  With 63
-// decoding sequences beside a prompt of 4,096 tokens at 64 heads the empty
-// workgroups of the direct grid took most of the time: attention 2,340 us, searched
-// 390; the append 786 and 45.
-struct Unit {
-  int i, k;
-};
-template <typename F>
-OQ_DEV Unit unit_of(int n_seq, int w, bool direct, F units) {
-  if (direct) return {w % n_seq, w / n_seq};
-  const int lane = threadIdx.x & 63;
-  for (int i0 = 0; i0 < n_seq; i0 += 64) {
-    const int n = i0 + lane < n_seq ? units(i0 + lane) : 0;
-    int sum = min(n, 0x3fffffff);                          // (row ranges may overlap: no sum overflows)
-    for (int off = 1; off < 64; off <<= 1) {
-      const int o = __shfl_up(sum, off);
-      if (lane >= off) sum = min(sum + o, 0x3fffffff);
-    }
-    const uint64_t past = __ballot(sum > w);
-    if (past) {
-      const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
-      const int before = l > 0 ? __shfl(sum, l - 1) : 0;
-      return {__builtin_amdgcn_readfirstlane(i0 + l), __builtin_amdgcn_readfirstlane(w - before)};
-    }
-    w -= __shfl(sum, 63);
-  }
-  return {-1, 0};
-}
 
 OQ_DEV int page_in(const CacheArgs& c, int p) { return p >= 0 && p < c.n_pages ? p : -1; }
 OQ_DEV int page_of(const CacheArgs& c, int i, int pg) { return page_in(c, c.table[int64_t(i) * c.max_pages + pg]); }
@@ -253,18 +221,6 @@ typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 OQ_DEV f32x4_t mfma_h(f16x8_t a, f16x8_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
-// int8 -> bf16, exact: eight codes of two dwords.
-OQ_DEV bf16x8_t codes_bf16(unsigned a, unsigned b) {
-  u32x4_t w;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned v = i < 2 ? a : b;
-    const int sh = 16 * (i & 1);
-    const float lo = float(int8_t(v >> sh)), hi = float(int8_t(v >> (sh + 8)));
-    w[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
-  }
-  return __builtin_bit_cast(bf16x8_t, w);
-}
 // int8 -> f16, exact: code + 128 as the low bits of 1024, then minus 1152.
 OQ_DEV f16x8_t codes_f16(unsigned a, unsigned b) {
   u32x4_t w;
@@ -286,28 +242,6 @@ OQ_DEV float pow2_above(float x) { return __uint_as_float((__float_as_uint(x) + 
 OQ_DEV float pow2_inv(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
 constexpr float VREF0 = 7.62939453125e-06f;              // 2^-17, below any step
 constexpr float WUNIT = 32768.0f;                        // weights are in units of vref / WUNIT
-
-// 32 tokens of a full page as they lie in memory, with the page's steps.
-template <int DH>
-struct Codes {
-  u32x4_t k[DH / 32], v[DH / 32];
-  float ks, vs;
-  // (entry: the table's, checked here: at its load the check would wait for memory)
-  OQ_DEV void load(const CacheArgs& c, int entry, int u, int tin, int lane) {
-    const int id = page_in(c, entry);
-    const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
-    ks = id < 0 ? NAN : c.ks[blk];
-    vs = id < 0 ? NAN : c.vs[blk];
-    const int64_t at = blk * c.P * DH + tin * DH;
-    const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(c.kc + at) + lane;
-    const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(c.vc + at) + lane;
-    // read once: past the caches (64 sequences of up to 8,192 tokens 130 -> 111 us)
-#pragma unroll
-    for (int j = 0; j < DH / 32; ++j) k[j] = __builtin_nontemporal_load(kp + 64 * j);
-#pragma unroll
-    for (int j = 0; j < DH / 32; ++j) v[j] = __builtin_nontemporal_load(vp + 64 * j);
-  }
-};
 
 // 32 tokens of the open page, one bf16 operand at a time.  Rows behind the
 // sequence's end are whatever the window holds: their values become zeros (their
@@ -481,10 +415,6 @@ struct Out {
   int splits, H;
   int64_t T, at, ml;                 // at: the workgroup's first share; ml: where the pairs begin, in floats
 };
-OQ_DEV Out out_of(uint16_t* O, float* LSE, float* part, int splits, int split, int H, int64_t T, int64_t units,
-                  int64_t unit, int unit_rows, int DH) {
-  return {O, LSE, part, splits, H, T, (split * units + unit) * unit_rows, splits * units * unit_rows * DH};
-}
 // A row whose every score is -inf (an infinite query) is NaN, like its output 0 / 0.
 OQ_DEV float lse_of(float m, float l) { return l > 0.0f ? m + log2f(l) : NAN; }
 OQ_DEV void put_ml(const Out& o, int row, int64_t t, int64_t hd, float m, float l) {

@@ -20,6 +20,39 @@
 namespace oq {
 namespace {
 
+// Ragged batches: unit w of all sequences' units (pages, row tiles), in the order of
+// the sequences, as (sequence, its unit); (-1, 0) past the last.  By every wave for
+// itself.  Batches whose grid of n_seq times the longest sequence's units is no
+// larger than the units' bound, or small, are numbered directly instead (a search
+// costs some 4 us: 15 chunks of up to 152 tokens 26 us, searched 30).  With 63
+// decoding sequences beside a prompt of 4,096 tokens at 64 heads the empty
+// workgroups of the direct grid took most of the time: attention 2,340 us, searched
+// 390; the append 786 and 45.
+struct Unit {
+  int i, k;
+};
+template <typename F>
+OQ_DEV Unit unit_of(int n_seq, int w, bool direct, F units) {
+  if (direct) return {w % n_seq, w / n_seq};
+  const int lane = threadIdx.x & 63;
+  for (int i0 = 0; i0 < n_seq; i0 += 64) {
+    const int n = i0 + lane < n_seq ? units(i0 + lane) : 0;
+    int sum = min(n, 0x3fffffff);                          // (row ranges may overlap: no sum overflows)
+    for (int off = 1; off < 64; off <<= 1) {
+      const int o = __shfl_up(sum, off);
+      if (lane >= off) sum = min(sum + o, 0x3fffffff);
+    }
+    const uint64_t past = __ballot(sum > w);
+    if (past) {
+      const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      const int before = l > 0 ? __shfl(sum, l - 1) : 0;
+      return {__builtin_amdgcn_readfirstlane(i0 + l), __builtin_amdgcn_readfirstlane(w - before)};
+    }
+    w -= __shfl(sum, 63);
+  }
+  return {-1, 0};
+}
+
 // ------------------------------------------------------------------ append
 // One workgroup takes one page's worth of one sequence's new tokens: the keys and
 // values of one head (blockIdx.y < kv heads), or a slice of the queries.  A thread
@@ -247,6 +280,46 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c, const int3
 }
 
 // ------------------------------------------------------------------ attention
+// int8 -> bf16, exact: eight codes of two dwords.
+OQ_DEV bf16x8_t codes_bf16(unsigned a, unsigned b) {
+  u32x4_t w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned v = i < 2 ? a : b;
+    const int sh = 16 * (i & 1);
+    const float lo = float(int8_t(v >> sh)), hi = float(int8_t(v >> (sh + 8)));
+    w[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+  }
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+
+// 32 tokens of a full page as they lie in memory, with the page's steps.
+template <int DH>
+struct Codes {
+  u32x4_t k[DH / 32], v[DH / 32];
+  float ks, vs;
+  // (entry: the table's, checked here: at its load the check would wait for memory)
+  OQ_DEV void load(const CacheArgs& c, int entry, int u, int tin, int lane) {
+    const int id = page_in(c, entry);
+    const int64_t blk = int64_t(max(id, 0)) * c.Hkv + u;
+    ks = id < 0 ? NAN : c.ks[blk];
+    vs = id < 0 ? NAN : c.vs[blk];
+    const int64_t at = blk * c.P * DH + tin * DH;
+    const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(c.kc + at) + lane;
+    const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(c.vc + at) + lane;
+    // read once: past the caches (64 sequences of up to 8,192 tokens 130 -> 111 us)
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j) k[j] = __builtin_nontemporal_load(kp + 64 * j);
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j) v[j] = __builtin_nontemporal_load(vp + 64 * j);
+  }
+};
+
+OQ_DEV Out out_of(uint16_t* O, float* LSE, float* part, int splits, int split, int H, int64_t T, int64_t units,
+                  int64_t unit, int unit_rows, int DH) {
+  return {O, LSE, part, splits, H, T, (split * units + unit) * unit_rows, splits * units * unit_rows * DH};
+}
+
 // Few rows (decoding): one workgroup takes 16 R rows of one key head and a split's
 // tokens, dealt to its four waves in chunks of 32.  Codes go from memory straight
 // into operand registers, the next chunk's in flight meanwhile; each wave has a
