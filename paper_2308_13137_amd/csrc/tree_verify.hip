@@ -235,12 +235,33 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
   int levels = 0;
   // Sums of r (and of q without the rejected tokens) over values x0 .. x1 - 1 of the row, by one wave: four steps' loads are
   // under way together (16 trees of up to 32 nodes over 128,256 tokens 29.6 us, one step at a time 35.6).
-  auto range_sum = [&](int x0, int x1, bool of_q, double& sr, double& sq) {
+  // (`walk`: for a further sibling; the draw's code has no use for q's sum)
+  auto range_sum = [&](auto walk, int x0, int x1, double& sr, double& sq) {
+    constexpr bool WALK = !CERTAIN && decltype(walk)::value;
+    const bool of_q = WALK && !a.replace;
     double r = 0.0, w = 0.0;
     float finite = 0.0f;                                   // NaN once a value is not
     constexpr int U = 4;
-    const bool with_q = !CERTAIN && (levels > 0 || of_q);
+    const bool with_q = !CERTAIN && levels > 0;
     int x = x0 + 4 * lane;
+    // What is left of q is summed itself: a sum of all of it, less what has left it, would hold nothing of it where
+    // one token had all but 2^-53 of the mass.  So the rejected tokens among these values, a few at most, are struck
+    // out of both rows (r has nothing there, either).  (16 trees with many rejections 59 us a call with and without;
+    // compared at every four values these tokens made it 62, all rejected tokens 67.)
+    auto among = [&](int t) { return __ballot(of_q && t < levels && s_rej[t] >= x0 && s_rej[t] < x1); };
+    const uint64_t here0 = WALK ? among(lane) : 0, here1 = WALK && levels > 64 ? among(lane + 64) : 0;
+    auto strike = [&](int width, auto each) {              // each(token) of those in x .. x + width - 1 (lane 0's x)
+      const int base = __builtin_amdgcn_readfirstlane(x);
+      auto in = [&](uint64_t here, int t0) {
+        for (; here; here &= here - 1) {
+          const int t = t0 + __ffsll(static_cast<unsigned long long>(here)) - 1;
+          const int tok = __builtin_amdgcn_readfirstlane(s_rej[t]);
+          if (unsigned(tok - base) < unsigned(width)) each(tok);
+        }
+      };
+      in(here0, 0);
+      in(here1, 64);
+    };
     auto four = [&](const float (&pv)[4], const float (&qv)[4], int at) {
       const int xx[4] = {at, at + 1, at + 2, at + 3};
       double rv[4];
@@ -250,19 +271,9 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
         r += rv[k];
         finite = __builtin_fmaf(pv[k], 0.0f, __builtin_fmaf(qv[k], 0.0f, finite));
       }
-      if (!CERTAIN && of_q) {
-        // (what is left is summed itself: a sum of all of q, less what has left it, would hold nothing of it
-        // where one token had all but 2^-53 of the mass)
-        float left[4] = {qv[0], qv[1], qv[2], qv[3]};
-        for (int t = 0; t < levels; ++t) {
-          const int gone = s_rej[t] - at;
-          if (unsigned(gone) < 4u) {
+      if (of_q) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) left[k] = k == gone ? 0.0f : left[k];
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w += double(left[k]);
+        for (int k = 0; k < 4; ++k) w += double(qv[k]);
       }
     };
     for (; __all(x + 256 * (U - 1) + 4 <= x1); x += 256 * U) {
@@ -272,6 +283,19 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
 #pragma unroll
       for (int i = 0; i < U; ++i)
         h[i] = with_q ? load_any<float4>(q + x + 256 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if constexpr (WALK) strike(256 * U, [&](int tok) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int k = tok - (x + 256 * i);
+          const float gp = k == 0 ? f[i].x : k == 1 ? f[i].y : k == 2 ? f[i].z : k == 3 ? f[i].w : 0.0f;
+          const float gq = k == 0 ? h[i].x : k == 1 ? h[i].y : k == 2 ? h[i].z : k == 3 ? h[i].w : 0.0f;
+          finite = __builtin_fmaf(gp, 0.0f, __builtin_fmaf(gq, 0.0f, finite));
+          f[i] = make_float4(k == 0 ? 0.0f : f[i].x, k == 1 ? 0.0f : f[i].y, k == 2 ? 0.0f : f[i].z,
+                             k == 3 ? 0.0f : f[i].w);
+          h[i] = make_float4(k == 0 ? 0.0f : h[i].x, k == 1 ? 0.0f : h[i].y, k == 2 ? 0.0f : h[i].z,
+                             k == 3 ? 0.0f : h[i].w);
+        }
+      });
 #pragma unroll
       for (int i = 0; i < U; ++i)
         four({f[i].x, f[i].y, f[i].z, f[i].w}, {h[i].x, h[i].y, h[i].z, h[i].w}, x + 256 * i);
@@ -283,6 +307,15 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
         pv[k] = x + k < x1 ? p[x + k] : 0.0f;
         qv[k] = with_q && x + k < x1 ? q[x + k] : 0.0f;
       }
+      if constexpr (WALK) strike(256, [&](int tok) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const bool it = x + k == tok;
+          finite = it ? __builtin_fmaf(pv[k], 0.0f, __builtin_fmaf(qv[k], 0.0f, finite)) : finite;
+          pv[k] = it ? 0.0f : pv[k];
+          qv[k] = it ? 0.0f : qv[k];
+        }
+      });
       four(pv, qv, x);
     }
     sr = wave_sum64(r + double(finite));
@@ -290,10 +323,10 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
   };
   // Values of a wave: sixteenths of the row, in whole steps of a wave.
   const int part = ((V + NW - 1) / NW + 255) / 256 * 256;
-  auto row_sums = [&](bool of_q, double& sr, double& sq) {
+  auto row_sums = [&](auto walk, double& sr, double& sq) {
     __syncthreads();
     double r, w;
-    range_sum(min(V, wave * part), min(V, (wave + 1) * part), of_q, r, w);
+    range_sum(walk, min(V, wave * part), min(V, (wave + 1) * part), r, w);
     if (lane == 0) {
       s_sum[wave] = r;
       s_sumq[wave] = w;
@@ -345,7 +378,7 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
     } else {
       if (j < n) {
         double sr, sq;
-        row_sums(!a.replace, sr, sq);
+        row_sums(std::true_type{}, sr, sq);
         if (sr == 0.0) break;                              // nothing is left: the draw steps back
         R = sr;
         if (!a.replace) Z = sq;
@@ -356,7 +389,7 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
   int next = -1;
   while (true) {
     double total, sq;
-    row_sums(false, total, sq);
+    row_sums(std::false_type{}, total, sq);
     if (total == 0.0 && levels > 0) {                      // no mass: from the distribution before
       --levels;
       continue;
@@ -381,7 +414,7 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
     __syncthreads();
     const int x0 = at * part, sub = part / NW;             // (a multiple of 16)
     double r, w;
-    range_sum(min(V, x0 + wave * sub), min(V, x0 + (wave + 1) * sub), false, r, w);
+    range_sum(std::false_type{}, min(V, x0 + wave * sub), min(V, x0 + (wave + 1) * sub), r, w);
     if (lane == 0) s_sum[wave] = r;
     __syncthreads();
     upto = before;

@@ -37,11 +37,10 @@ def test_verify_siblings_of_a_peak(V, gap, place):
     assert kept > 0
 
 
-@pytest.mark.parametrize("V", [5, 64, 1003])
-def test_verify_rejected_tokens_side_by_side(V):
+@pytest.mark.parametrize("V,n", [(5, 5), (64, 40), (1003, 40), (130, 120), (20011, 128)])
+def test_verify_rejected_tokens_side_by_side(V, n):
     """Long chains of rejections whose tokens are neighbours, and one of them twice."""
     g = torch.Generator().manual_seed(V)
-    n = min(V, 40)
     for first in (0, max(0, V - n)):
         Q = torch.softmax(3 * torch.randn(n, V, generator=g), 1)
         P = torch.softmax(3 * torch.randn(n, V, generator=g), 1)
@@ -54,6 +53,28 @@ def test_verify_rejected_tokens_side_by_side(V):
             twice = token.clone()
             twice[n // 2:] = token[1:1 + n - n // 2]
             check_verify([star(n)], [0, n], twice, P, Q, u, un, replace=False)
+
+
+@pytest.mark.parametrize("V", [40, 5000])
+def test_verify_siblings_of_a_token_that_is_not_finite(V):
+    """A rejected token's probability that is NaN, or infinite in the draft: nothing is drawn, and no sibling is
+    kept."""
+    n, g = 4, torch.Generator().manual_seed(V)
+    P, Q = (torch.softmax(torch.randn(n, V, generator=g), 1) for _ in range(2))
+    un, parent, start = torch.full((1,), 0.5, device="cuda"), i32(star(n)), i32([0, n])
+    for token in ([0, 9, 3, 4], [0, V - 1, 9, 7]):
+        bad = token[1]
+        for p, q in ((float("nan"), None), (None, float("nan")), (None, float("inf"))):
+            a, b = P.clone(), Q.clone()
+            if p is not None:
+                a[0, bad] = p
+            if q is not None:
+                b[0, bad] = q
+            for replace in (False, True):
+                path, count, nxt = oq.tree_verify(i32(token), parent, start, n, a.cuda(),
+                                                  torch.tensor([0, 0.9, 0.0, 0.0], device="cuda"), un, Q=b.cuda(),
+                                                  replace=replace)
+                assert count.item() == 1 and nxt.item() == -1, (token, p, q, replace)
 
 
 # ------------------------------------------------------------------ probabilities
