@@ -800,6 +800,9 @@ oq_status oq_kv_read(const oq_kv_cache* cache, const oq_kv_batch* batch, const i
  *   ... -> oq_kv_append_tree -> oq_kv_attend_tree -> ... (every block) -> the logits ->
  *   oq_token_probs -> oq_tree_verify -> oq_kv_commit (every block's cache);
  *   then length[i] += count[i], and next[i] is the first node of the next tree.
+ * The tokens that come of it are distributed as the block's own, but for one difference: a node
+ * behind a page that only the tree fills sees that page's tokens as bf16 rows, where decoding
+ * token by token would see their codes.
  * None of them allocates, and all can be captured into a graph.
  *
  * A sequence's new tokens in oq_kv_batch are its tree's nodes, at most a page's
@@ -862,7 +865,7 @@ oq_status oq_token_probs(const void* logits, oq_dtype dt, int64_t ld, int64_t n_
                          const float* temperature, float* P, int64_t ld_p, hipStream_t stream);
 
 /* oq_tree_verify: which of the drafted tokens are kept, and the token after them, such that
- * the sequence of tokens is distributed as the target's.
+ * the sequence of tokens is distributed as P has the target's.
  *   q_start, parent : the trees, as above; node 0 of a tree is the token that is known
  *           already (the last one drawn), and is kept; other nodes without a parent never are
  *   token : int32 [tokens], the nodes' tokens (node 0's is not read; one outside

@@ -76,9 +76,10 @@ OQ_DEV uint32_t tree_sees(const uint32_t (*s_anc)[4], int node, int L, int t0) {
 
 // ------------------------------------------------------------------ append
 // One workgroup takes one sequence's tree: the keys and values of one head
-// (blockIdx.y < kv heads), or a slice of the queries.  HBM-bound for large batches (64 trees of up
-// to 64 nodes, 64 heads, float32, 27.5 us, 5.0 TB/s), for few rows a chain of three loads (five
-// nodes, 32 heads, 5.2 us; with a barrier for each round of the ancestors' search 10.8).
+// (blockIdx.y < kv heads), or a slice of the queries.  Large batches are bound by HBM (64 trees of up
+// to 64 nodes, 64 heads, float32, 137 MB: 38 us, 3.6 TB/s, of which reading the rotation, again for
+// every head, is 3; 27 us with inputs that the last-level cache holds), few rows by a chain of three
+// loads (five nodes, 32 heads, 5.2 us; with a barrier for each round of the ancestors' search 10.8).
 template <typename TI>
 __global__ __launch_bounds__(256) void tree_append_kernel(CacheArgs c, RowIn<TI> in, int H,
                                                          const float* __restrict__ rope, int64_t n_rope,
@@ -639,8 +640,9 @@ OQ_DEV uint32_t lanes_upto(uint32_t v) {
 // tree_join_kernel, whom the workgroup where it begins tells so.
 // Against the batch attention's kernels with a tree's mask (a number of splits for all sequences, row
 // and tile kernels one after the other): 32 trees of up to 16 nodes over up to 4,096 tokens, 64 heads, 8
-// key heads, 107 -> 71 us; 8 nodes over 131,072 81 -> 75; 64 over 16,384, where matrix and vector work
-// bound both, 66 -> 65.
+// key heads, 107 -> 71 us (65 with TILE_MORE); 8 nodes over 131,072 81 -> 75; 64 over 16,384, where
+// matrix and vector work bound both, 66 -> 65.  No instance spills vector registers; 57 to 91 scalar
+// ones (the line's and the piece's numbers) wait in lanes of vector registers.
 struct Cut {
   int token, head, rows, w, pieces;      // its first row as a token and a head of the group; w: where it begins,
 };                                       // pieces: workgroups that go on with it

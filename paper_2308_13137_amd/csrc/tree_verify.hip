@@ -25,9 +25,10 @@ OQ_DEV T load_any(const void* p) {
 // P = softmax(logits / t) = 2^((x - max x) log2(e) / t) over their sum.  One workgroup
 // a row: up to NV 16-byte pieces a thread stay in registers between the maximum, the sum
 // and the output; what is beyond them is read again.  Many rows are bound by HBM (512 of 128,256
-// bf16 logits: 86 us at best, 105 at the median of six launches, 3.8 TB/s; 108 us a call, and 116
-// with half the pieces held and two workgroups on a compute unit).  With few rows gridDim.y workgroups read the same row, sum it
-// in the same order and write a part each (five rows of 128,256: 19 us a call with one, 15 with eight).
+// bf16 logits 104 us, 3.8 TB/s, 7% longer with half the pieces held and two workgroups on a compute
+// unit; fp32 logits, of which 49,152 a row stay in registers, 153 us).  With few rows gridDim.y
+// workgroups read the same row, sum it in the same order and write a part each (five rows of 128,256:
+// 19 us a call with one, 14.6 with eight).
 template <typename TI, int NV>
 __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int64_t ldx, int64_t V,
                                                    const float* __restrict__ temperature, float* __restrict__ P,
@@ -149,7 +150,10 @@ __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int
 //
 // After m rejections r(x) follows from p(x), q(x) and the masses of each step alone,
 // so a child's test reads two numbers (all of them are fetched at the start), and only a
-// mass needs a pass over the vocabulary: before a further sibling, and for the draw.
+// mass needs a pass over the vocabulary: before a further sibling, and for the draw.  That pass repeats
+// the rejections at every value, so many siblings cost their square: 8 rejected ones of 128,256 tokens
+// 221 us, 32 of them 2,260 (without Q, one pass in all, 40 and 115).  With Q the kernel needs 15 registers
+// more than 1,024 threads have (56 bytes a lane are spilled).
 // r of N values of a row after `levels` rejections, from p and q.  (A NaN counts as zero here: sums over
 // a row tell by themselves whether it holds values that are not finite.  With that in every value's own
 // fp64 arithmetic, and sums of q that nobody asked for, 16 trees of up to 32 nodes over 128,256 tokens
