@@ -799,7 +799,8 @@ oq_status oq_kv_read(const oq_kv_cache* cache, const oq_kv_batch* batch, const i
  * kept.  A step, in place of oq_kv_append and oq_kv_attend:
  *   ... -> oq_kv_append_tree -> oq_kv_attend_tree -> ... (every block) -> the logits ->
  *   oq_token_probs -> oq_tree_verify -> oq_kv_commit (every block's cache);
- *   then length[i] += count[i], and next[i] is the first node of the next tree.
+ *   then length[i] += count[i], and next[i] is the first node of the next tree.  (Where a tree did
+ *   not fit the cache nothing is kept: its rows are NaN, next[i] is -1, and count[i] is not added.)
  * The tokens that come of it are distributed as the block's own, but for one difference: a node
  * behind a page that only the tree fills sees that page's tokens as bf16 rows, where decoding
  * token by token would see their codes.

@@ -103,12 +103,12 @@ __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int
     for (int w = 0; w < NW; ++w) v += s_a[w];
     return v;
   };
-  // Above a temperature of one x - max may pass fp32's range where its quotient does not, and at tiny ones
-  // differences below fp32's normal numbers count, whose scale would be infinite: both are scaled by a power of two
-  // first.  (Loops of their own: with the factor in the ones below, 512 rows of 128,256 bf16 logits took 104.6 us a
+  // Above a temperature of one x - max may pass fp32's range where its quotient does not, at huge ones the scale
+  // itself lies below fp32's normal numbers, and at tiny ones differences there count, whose scale would be infinite:
+  // all are scaled by a power of two first.  (Loops of their own: with the factor in the ones below, 512 rows of 128,256 bf16 logits took 104.6 us a
   // call instead of 104.2, five 14.7 instead of 14.5.)
   const bool tiny = t < 0x1p-100f;
-  if (tiny || (t > 1.0f && m > 0x1p100f)) {
+  if (tiny || (t > 1.0f && fmaxf(m, t) > 0x1p100f)) {
     const bool far = tiny && fabsf(m) >= 0x1p90f;          // every difference that is not zero is 2^66 or more
     const float h = far ? 1.0f : tiny ? 0x1p32f : 0x1p-3f;
     const float k = far ? 3.0e38f : (1.4426950408889634f / h) / t;

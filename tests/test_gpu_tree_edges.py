@@ -94,6 +94,17 @@ def test_probs_of_differences_that_pass_fp32(V, dt):
     assert (got[4:6, 2] > 0).all()
 
 
+def test_probs_at_huge_temperatures():
+    """Largest logits of any size below values near the type's lowest: the scale log2(e) / t is below fp32's normal
+    numbers."""
+    big = torch.finfo(F32).max
+    x = torch.tensor([[1.0, -big, -big / 3, 0.0, -big / 7]], device="cuda").repeat(8, 1)
+    x[4:6, 0], x[6:, 0] = 1e28, 1e35
+    t = torch.tensor([big, 3.1e38, 2.0 ** 127, 2.0 ** 101, big, 2.0 ** 126, big, 2.0 ** 100], device="cuda")
+    want, tol = tree_ref.probs64(x, t)
+    assert ((oq.token_probs(x, t).cpu().double() - want).abs() <= tol).all()
+
+
 def test_probs_of_differences_below_fp32s_normal_numbers():
     """Logits and temperatures that are tiny alike."""
     step = 2.0 ** -149
