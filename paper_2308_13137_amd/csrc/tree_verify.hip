@@ -105,8 +105,8 @@ __global__ __launch_bounds__(NT) void probs_kernel(const TI* __restrict__ X, int
   };
   // Above a temperature of one x - max may pass fp32's range where its quotient does not, at huge ones the scale
   // itself lies below fp32's normal numbers, and at tiny ones differences there count, whose scale would be infinite:
-  // all are scaled by a power of two first.  (Loops of their own: with the factor in the ones below, 512 rows of 128,256 bf16 logits took 104.6 us a
-  // call instead of 104.2, five 14.7 instead of 14.5.)
+  // all are scaled by a power of two first.  (Loops of their own: with the factor in the ones below, 512 rows of
+  // 128,256 bf16 logits took 104.6 us a call instead of 104.2, five 14.7 instead of 14.5.)
   const bool tiny = t < 0x1p-100f;
   if (tiny || (t > 1.0f && fmaxf(m, t) > 0x1p100f)) {
     const bool far = tiny && fabsf(m) >= 0x1p90f;          // every difference that is not zero is 2^66 or more
@@ -237,8 +237,8 @@ __global__ __launch_bounds__(NT) void verify_kernel(VerifyArgs a) {
   };
   const float *p = a.P + b * a.ldp, *q = CERTAIN ? nullptr : a.Q + b * a.ldq;
   int levels = 0;
-  // Sums of r (and of q without the rejected tokens) over values x0 .. x1 - 1 of the row, by one wave: four steps' loads are
-  // under way together (16 trees of up to 32 nodes over 128,256 tokens 29.6 us, one step at a time 35.6).
+  // Sums of r (and of q without the rejected tokens) over values x0 .. x1 - 1 of the row, by one wave: four steps'
+  // loads are under way together (16 trees of up to 32 nodes over 128,256 tokens 29.6 us, one step at a time 35.6).
   // (`walk`: for a further sibling; the draw's code has no use for q's sum)
   auto range_sum = [&](auto walk, int x0, int x1, double& sr, double& sq) {
     constexpr bool WALK = !CERTAIN && decltype(walk)::value;
